@@ -403,6 +403,88 @@ PC_API int32_t pc_parallel_attn_static(int32_t B, int32_t w, int32_t Hq, int32_t
                                 const void* k_cache, const void* v_cache, const void* k_win, const void* v_win,
                                 void* out, float* lse_out, int32_t* status_word, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Caches in 8 bits.  The paper compresses the cache by evicting entries (Sec. 3.1); these calls also shrink what an
+ * entry takes, from 2 d to d + 4 bytes for keys and for values (no counterpart in the paper).
+ *
+ * A cache holds `capacity` entries for each of B sequences and Hkv kv-heads: k, v [B,Hkv,capacity,d], contiguous, 16-byte
+ * aligned.  PC_KV_BF16: bf16, no scales.  PC_KV_INT8 (two's complement) and PC_KV_E4M3 (1-4-3 bits, largest 448, no
+ * infinities): codes, with a fp32 scale for the keys and one for the values of every entry, k_scale, v_scale [B,Hkv,capacity].
+ * An entry stands for code * scale.  With Q = 127 (int8) or 448 (e4m3), a row x of d values is held as
+ *     a = max |x|,   r = Q / a,   scale = a / Q,   code = x * r rounded to the format (to nearest, ties to even),
+ * each of the three operations one fp32 operation.  A row whose a is below 2^-100 is held as zeros with scale 0; one
+ * that holds a NaN or an infinity has codes 0 and scale NaN, so that it reads back as NaN.
+ *
+ * The descriptor is HOST memory, its pointers are device memory.  capacity <= 2^28.
+ */
+enum { PC_KV_BF16 = 0, PC_KV_INT8 = 1, PC_KV_E4M3 = 2 };
+
+typedef struct {
+  int32_t format, B, Hkv, d;
+  int64_t capacity;
+  void *k, *v;
+  float *k_scale, *v_scale;                      /* NULL for PC_KV_BF16 */
+} pc_kv_cache;
+
+/* Writes n new tokens of every sequence: token i of sequence b becomes entry at0 + (at ? at[b] : 0) + i.
+ * k_src, v_src [B,n,Hkv,d] bf16 through element strides (sequence, token, head; host arrays of 3; 0,0,0 -> contiguous),
+ * multiples of 8; at: device int32 [B] or NULL.  An entry outside [0, capacity) is not written, and status_word (may be
+ * NULL) then gets the code 401 (without `at` such a call is refused).  8-bit formats only.
+ */
+PC_API int32_t pc_kv_quantize(const pc_kv_cache* cache, const void* k_src, const int64_t* k_stride, const void* v_src,
+                       const int64_t* v_stride, int32_t n, int32_t at0, const int32_t* at, int32_t* status_word, void* stream);
+
+/* pc_gather_kv into an 8-bit cache of one sequence (cache->B = 1, cache->Hkv kv-heads): entry r * k + t of head h holds row
+ * idx[r,h,t] of chunk kept[r]; k_src, v_src, kv_stride, kept, idx, pos_out as there.  Entries with idx < 0 are zeros with
+ * scale 0 and position -1.  pos_out [Hkv, m*k] or NULL.  PC_ERR_INVALID_ARG if m * k > capacity.
+ */
+PC_API int32_t pc_gather_kv_quantize(const void* k_src, const void* v_src, const int64_t* kv_stride, const int32_t* kept,
+                              const int32_t* idx, int32_t m, int32_t k, const pc_kv_cache* cache, int32_t* pos_out,
+                              void* stream);
+
+/* Reads n entries of every sequence back: k_out, v_out [B,Hkv,n,d] bf16 contiguous get code * scale rounded to bf16 of the
+ * entries at0 + (at ? at[b] : 0) + i; entries outside [0, capacity) read as zeros.  8-bit formats only.
+ */
+PC_API int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0, const int32_t* at, void* k_out, void* v_out,
+                         void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * Attention of a batch over a prefix that its sequences share, their own caches and themselves.  Paper: Sec. 3.1 "Global
+ * attention", Eq. 9-11, for many continuations of one compressed prompt (no counterpart there for the sharing).
+ * For each of B sequences, w new tokens (queries [B,w,Hq,d]; w = 1: a decoding step) attend to
+ *   - the n_prefix first entries of `prefix` (a cache of one sequence; NULL or n_prefix = 0: none), read once for all sequences,
+ *   - the first n_own entries of the sequence's own cache in `own` (NULL or n_own = 0: none), of which only the first
+ *     own_len[b], clamped into [0, n_own], where own_len (device int32 [B]) is given,
+ *   - causally to the new tokens' own keys and values k_win, v_win [B,w,Hkv,d] (both NULL: not; a program that has written
+ *     them to its cache already).
+ * One softmax over all of them.  prefix and own may have different formats; entries behind those named are never used, whatever
+ * they hold.  Keys are rotated already; token i of sequence b is rotated here at position q_pos0 + (q_pos ? q_pos[b] : 0) + i and
+ * rounded to bf16, as in pc_parallel_attn; rope_theta = 0: queries come rotated.  q, k_win and v_win through element
+ * strides (sequence, token, head; 0,0,0 -> contiguous), multiples of 8.  A row that sees nothing gets zeros and lse -infinity.
+ * out [B,w,Hq,d] bf16 and lse [B,Hq,w] fp32 (natural log; may be NULL) contiguous.
+ * 1 <= w <= 128, d in {64, 128}, any Hq / Hkv.  Workspace: pc_cache_attn_workspace_bytes(args) (reads the sizes alone).
+ */
+typedef struct {
+  int32_t B, w, Hq, Hkv, d;
+  int32_t n_prefix, n_own, q_pos0;
+  float rope_theta, softmax_scale;               /* softmax_scale 0 -> 1/sqrt(d) */
+  const void* q;
+  int64_t q_stride[3];
+  const void *k_win, *v_win;
+  int64_t k_win_stride[3], v_win_stride[3];
+  const int32_t *q_pos, *own_len;
+  const pc_kv_cache *prefix, *own;
+  void* out;
+  float* lse;
+  int32_t* status_word;
+  void* workspace;
+  size_t workspace_bytes;
+} pc_cache_attn_args;
+
+PC_API size_t pc_cache_attn_workspace_bytes(const pc_cache_attn_args* args);
+
+PC_API int32_t pc_cache_attn(const pc_cache_attn_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

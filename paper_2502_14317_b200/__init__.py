@@ -11,4 +11,5 @@ from .binding import (  # noqa: F401
     select_chunks, score_select_chunks, select_tokens, select_tokens_calibrated, gather_kv, parallel_attn, parallel_attn_append, parallel_attn_workspace_bytes,
     parallel_attn_static, parallel_attn_static_scratch_bytes, hot_path, hot_path_from_host,
     queue_init, queue_update, queue_gather, queue_select_gather, queue_emit, hot_path_streaming,
+    kv_cache, kv_quantize, gather_kv_quantize, kv_dequantize, cache_attn,
 )

@@ -14,6 +14,7 @@ static std::atomic<unsigned long long> g_launches{0};
 void note_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 static std::atomic<int> g_wait_kcycles{1 << 21};            // limit of the device-side waits, units of 1024 cycles (~1 s)
 static std::atomic<int> g_skip_final_publication{0};        // test hook, see pc_debug_bounded_wait_test
+int wait_limit_kcycles() { return g_wait_kcycles.load(); }
 }  // namespace pc
 
 namespace {
@@ -85,6 +86,10 @@ int32_t check_prefill_desc(const pc_prefill_desc* d) {
 
 }  // namespace
 
+namespace pc {
+int sm100_count() { const DeviceInfo& dev = device_info(); return dev.ok == 1 ? dev.sm_count : 0; }
+}  // namespace pc
+
 extern "C" {
 
 const char* pc_status_string(int32_t status) {
@@ -100,7 +105,7 @@ const char* pc_status_string(int32_t status) {
   }
 }
 
-int32_t pc_version(void) { return 1001; }
+int32_t pc_version(void) { return 1002; }
 
 uint64_t pc_launch_count(void) { return pc::g_launches.load(std::memory_order_relaxed); }
 

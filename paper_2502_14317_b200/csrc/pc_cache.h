@@ -1,0 +1,84 @@
+// Parameter blocks and launchers of the 8-bit caches and of the attention over shared and own caches (internal).
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <cstdint>
+
+namespace pc {
+
+// Rows that go into an 8-bit cache (pc_kv_quant.cu).
+struct KvWrite {
+  const void *k_src, *v_src;
+  long long k_stride[3], v_stride[3];            // elements: sequence (chunk), token, head
+  uint8_t *k, *v;
+  float *k_scale, *v_scale;
+  long long capacity;
+  int B, Hkv, n;                                 // append: sequences, kv-heads, tokens; gather: 1, kv-heads, entries m * k
+  int at0;
+  const int* at;                                 // append: [B] or null
+  const int *kept, *idx;                         // gather: chunk ids [m], positions [m,Hkv,per_chunk]
+  int per_chunk;
+  int* pos_out;                                  // gather: [Hkv,n] or null
+  int* status;
+};
+cudaError_t launch_kv_quantize(const KvWrite& w, int format, int d, bool gather, int sm_count, cudaStream_t st);
+
+struct KvRead {
+  const uint8_t *k, *v;
+  const float *k_scale, *v_scale;
+  long long capacity;
+  int B, Hkv, n, at0;
+  const int* at;
+  void *k_out, *v_out;
+};
+cudaError_t launch_kv_dequantize(const KvRead& r, int format, int d, int sm_count, cudaStream_t st);
+
+// Queries of pc_cache_attn as rows: rows[hkv][(b * w + i) * G + g][d], rotated and rounded to bf16 (theta 0: as they are).
+struct CacheRows {
+  const void* q;
+  long long stride[3];
+  int B, w, Hq, Hkv, pos0;
+  const int* pos;
+  double theta;
+  void* rows;
+};
+cudaError_t launch_cache_rows(const CacheRows& p, int d, cudaStream_t st);
+
+// One phase of pc_cache_attn: the rows of each of `seqs` sequences (prefix: one, all rows; own caches: B, w * G rows) over a cache.
+// A split's result of a row goes to slot slot0 + split of its n_slots: the unnormalised output, and (maximum in log2 units,
+// sum); a split without keys leaves (-inf, 0) and no output.
+struct CachePhase {
+  int seqs, rows, Hkv, n_keys;                   // n_keys: entries, or their most
+  const int* len;                                // [seqs] or null: n_keys each
+  const float *k_scale, *v_scale;                // [seqs,Hkv,capacity] (8-bit formats)
+  long long capacity;
+  int n_rg, n_split, slot0, n_slots, total_rows; // row groups of a sequence, key splits; total_rows = rows of a kv-head over all sequences
+  float scale_log2;
+  const __nv_bfloat16* q_rows;                   // [Hkv,total_rows,d]
+  float* part_o;                                 // [Hkv,total_rows,n_slots,d]
+  float2* part_ml;                               // [Hkv,total_rows,n_slots]
+  int* status;
+  int wait_kcycles;
+};
+// maps of the cache's keys and values: boxes of few_keys() entries
+int few_keys(int format, int d, int rows);       // keys of a stage
+int few_rows(int rows);                          // rows of a row group
+int few_ctas_per_sm(int rows);
+cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, int format, int d, cudaStream_t st);
+
+// Joins the slots of a row and the new tokens' own keys.
+struct CacheMerge {
+  int B, w, Hq, Hkv, n_slots, total_rows;
+  const float* part_o;
+  const float2* part_ml;
+  const __nv_bfloat16* q_rows;
+  const void *k_win, *v_win;                     // or null
+  long long k_stride[3], v_stride[3];
+  float scale_log2;
+  __nv_bfloat16* out;
+  float* lse;
+};
+cudaError_t launch_cache_merge(const CacheMerge& p, int d, cudaStream_t st);
+
+}  // namespace pc

@@ -1,0 +1,229 @@
+// C ABI of the 8-bit caches and of the attention over shared and own caches: argument checks, plans, launches.
+#include "../../include/pc.h"
+#include "pc_cache.h"
+#include "pc_kernels.h"
+#include "pc_tmap.h"
+
+#include <cmath>
+
+namespace {
+
+constexpr size_t ALIGN = 256;
+size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
+bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+int32_t launched(cudaError_t e) {
+  const cudaError_t pending = cudaGetLastError();
+  return e == cudaSuccess && pending == cudaSuccess ? PC_OK : PC_ERR_CUDA;
+}
+
+// Strides (sequence, token, head) of a tensor [B,n,H,d] in elements; zeros: contiguous.
+bool strides(const int64_t* in, int64_t n, int64_t H, int64_t d, long long out[3]) {
+  if (in == nullptr || (in[0] == 0 && in[1] == 0 && in[2] == 0)) { out[0] = n * H * d; out[1] = H * d; out[2] = d; return true; }
+  for (int i = 0; i < 3; ++i) {
+    if (in[i] < 0 || in[i] % 8 != 0) return false;
+    out[i] = in[i];
+  }
+  return true;
+}
+
+int32_t check_cache(const pc_kv_cache* c, bool only8) {
+  if (c == nullptr) return PC_ERR_INVALID_ARG;
+  if (c->B < 1 || c->Hkv < 1 || c->capacity < 1 || !c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16)) return PC_ERR_INVALID_ARG;
+  if (c->d != 64 && c->d != 128) return PC_ERR_UNSUPPORTED;
+  if (c->capacity > (1ll << 28) || (int64_t)c->B * c->Hkv > (1 << 24)) return PC_ERR_UNSUPPORTED;
+  if (c->format == PC_KV_BF16) return only8 ? PC_ERR_UNSUPPORTED : PC_OK;
+  if (c->format != PC_KV_INT8 && c->format != PC_KV_E4M3) return PC_ERR_INVALID_ARG;
+  if (!c->k_scale || !c->v_scale || !aligned(c->k_scale, 4) || !aligned(c->v_scale, 4)) return PC_ERR_INVALID_ARG;
+  return PC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t pc_kv_quantize(const pc_kv_cache* cache, const void* k_src, const int64_t* k_stride, const void* v_src, const int64_t* v_stride,
+                       int32_t n, int32_t at0, const int32_t* at, int32_t* status_word, void* stream) {
+  if (int32_t rc = check_cache(cache, true); rc != PC_OK) return rc;
+  if (!k_src || !v_src || !aligned(k_src, 16) || !aligned(v_src, 16) || n < 1) return PC_ERR_INVALID_ARG;
+  if (at == nullptr && (at0 < 0 || (int64_t)at0 + n > cache->capacity)) return PC_ERR_INVALID_ARG;
+  pc::KvWrite w = {};
+  if (!strides(k_stride, n, cache->Hkv, cache->d, w.k_stride) || !strides(v_stride, n, cache->Hkv, cache->d, w.v_stride)) return PC_ERR_INVALID_ARG;
+  const int sms = pc::sm100_count();
+  if (sms == 0) return PC_ERR_UNSUPPORTED;
+  w.k_src = k_src; w.v_src = v_src;
+  w.k = static_cast<uint8_t*>(cache->k); w.v = static_cast<uint8_t*>(cache->v);
+  w.k_scale = cache->k_scale; w.v_scale = cache->v_scale;
+  w.capacity = cache->capacity;
+  w.B = cache->B; w.Hkv = cache->Hkv; w.n = n; w.at0 = at0; w.at = at; w.status = status_word;
+  return launched(pc::launch_kv_quantize(w, cache->format, cache->d, false, sms, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t pc_gather_kv_quantize(const void* k_src, const void* v_src, const int64_t* kv_stride, const int32_t* kept, const int32_t* idx,
+                              int32_t m, int32_t k, const pc_kv_cache* cache, int32_t* pos_out, void* stream) {
+  if (int32_t rc = check_cache(cache, true); rc != PC_OK) return rc;
+  if (!k_src || !v_src || !kv_stride || !kept || !idx || !aligned(k_src, 16) || !aligned(v_src, 16) || m < 1 || k < 1) return PC_ERR_INVALID_ARG;
+  if (cache->B != 1 || (int64_t)m * k > cache->capacity) return PC_ERR_INVALID_ARG;
+  pc::KvWrite w = {};
+  for (int i = 0; i < 3; ++i) {
+    if (kv_stride[i] <= 0 || kv_stride[i] % 8 != 0) return PC_ERR_INVALID_ARG;
+    w.k_stride[i] = w.v_stride[i] = kv_stride[i];
+  }
+  const int sms = pc::sm100_count();
+  if (sms == 0) return PC_ERR_UNSUPPORTED;
+  w.k_src = k_src; w.v_src = v_src;
+  w.k = static_cast<uint8_t*>(cache->k); w.v = static_cast<uint8_t*>(cache->v);
+  w.k_scale = cache->k_scale; w.v_scale = cache->v_scale;
+  w.capacity = cache->capacity;
+  w.B = 1; w.Hkv = cache->Hkv; w.n = m * k;
+  w.kept = kept; w.idx = idx; w.per_chunk = k; w.pos_out = pos_out;
+  return launched(pc::launch_kv_quantize(w, cache->format, cache->d, true, sms, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0, const int32_t* at, void* k_out, void* v_out, void* stream) {
+  if (int32_t rc = check_cache(cache, true); rc != PC_OK) return rc;
+  if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16) || n < 1) return PC_ERR_INVALID_ARG;
+  const int sms = pc::sm100_count();
+  if (sms == 0) return PC_ERR_UNSUPPORTED;
+  const pc::KvRead r = {static_cast<const uint8_t*>(cache->k), static_cast<const uint8_t*>(cache->v), cache->k_scale, cache->v_scale,
+                        cache->capacity, cache->B, cache->Hkv, n, at0, at, k_out, v_out};
+  return launched(pc::launch_kv_dequantize(r, cache->format, cache->d, sms, static_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------------------------ attention over shared and own caches
+namespace {
+
+struct PhasePlan { int n_rg, n_split; };
+struct CachePlan {
+  PhasePlan prefix, own;
+  int n_slots;
+  int64_t total_rows;
+  size_t off_rows, off_ml, off_o, total;
+};
+
+// Splits of the keys: rounds of the grid x (some tiles of fixed cost + tiles of a split) is least.
+PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count) {
+  PhasePlan p;
+  const int per = pc::few_rows((int)rows), keys = pc::few_keys(format, d, (int)rows);
+  p.n_rg = (int)((rows + per - 1) / per);
+  const int tiles = (n_keys + keys - 1) / keys;
+  const int64_t items = seqs * Hkv * p.n_rg, units = (int64_t)sm_count * pc::few_ctas_per_sm((int)rows);
+  int64_t least = -1;
+  p.n_split = 1;
+  for (int s = 1; s <= 64 && s <= tiles; ++s) {
+    const int64_t rounds = (items * s + units - 1) / units, cost = rounds * (4 + (tiles + s - 1) / s) * 64 + s;
+    if (least < 0 || cost < least) { least = cost; p.n_split = s; }
+  }
+  return p;
+}
+
+int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
+  if (a->B < 1 || a->w < 1 || a->Hq < 1 || a->Hkv < 1 || a->Hq % a->Hkv != 0 || a->n_prefix < 0 || a->n_own < 0) return PC_ERR_INVALID_ARG;
+  if (a->d != 64 && a->d != 128) return PC_ERR_UNSUPPORTED;
+  if (a->w > 128 || (int64_t)a->B * a->w * a->Hq > (1 << 24)) return PC_ERR_UNSUPPORTED;
+  const int G = a->Hq / a->Hkv;
+  p.total_rows = (int64_t)a->B * a->w * G;
+  p.n_slots = 0;
+  p.prefix = p.own = {0, 0};
+  for (int own = 0; own <= 1; ++own) {
+    const pc_kv_cache* const c = own ? a->own : a->prefix;
+    const int n = own ? a->n_own : a->n_prefix;
+    if (n == 0) continue;
+    if (int32_t rc = check_cache(c, false); rc != PC_OK) return rc;
+    if (c->B != (own ? a->B : 1) || c->Hkv != a->Hkv || c->d != a->d || n > c->capacity) return PC_ERR_INVALID_ARG;
+    PhasePlan& ph = own ? p.own : p.prefix;
+    ph = few_plan(own ? a->B : 1, own ? (int64_t)a->w * G : p.total_rows, a->Hkv, a->d, c->format, n, sm_count);
+    if ((own ? a->B : 1ll) * a->Hkv * ph.n_rg * ph.n_split > 0x7FFFFFFF) return PC_ERR_UNSUPPORTED;
+    p.n_slots += ph.n_split;
+  }
+  size_t off = 0;
+  p.off_rows = off; off += align_up((size_t)p.total_rows * a->Hkv * a->d * 2);
+  p.off_ml = off; off += align_up((size_t)p.total_rows * a->Hkv * p.n_slots * sizeof(float2));
+  p.off_o = off; off += align_up((size_t)p.total_rows * a->Hkv * p.n_slots * a->d * sizeof(float));
+  p.total = off;
+  return PC_OK;
+}
+
+int plan_sms() { const int n = pc::sm100_count(); return n > 0 ? n : 148; }
+
+// tensor maps over the first n entries of a cache, boxes of `keys` entries
+bool cache_maps(const pc_kv_cache* c, int n, int keys, CUtensorMap* tm_k, CUtensorMap* tm_v) {
+  const uint64_t d = (uint64_t)c->d, cap = (uint64_t)c->capacity;
+  const uint64_t dims[4] = {d, (uint64_t)n, (uint64_t)c->Hkv, (uint64_t)c->B}, str[3] = {d, cap * d, (uint64_t)c->Hkv * cap * d};
+  if (c->format == PC_KV_BF16) {
+    const uint32_t box[4] = {64, (uint32_t)keys, 1, 1};
+    return pc::make_tmap_bf16_4d(tm_k, c->k, dims, str, box) && pc::make_tmap_bf16_4d(tm_v, c->v, dims, str, box);
+  }
+  const uint32_t box[4] = {(uint32_t)c->d, (uint32_t)keys, 1, 1};
+  return pc::make_tmap_u8_4d(tm_k, c->k, dims, str, box) && pc::make_tmap_u8_4d(tm_v, c->v, dims, str, box);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t pc_cache_attn_workspace_bytes(const pc_cache_attn_args* a) {
+  CachePlan p;
+  return a != nullptr && cache_plan(a, plan_sms(), p) == PC_OK ? p.total : 0;
+}
+
+int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
+  if (a == nullptr) return PC_ERR_INVALID_ARG;
+  CachePlan plan;
+  const int sms = pc::sm100_count();
+  if (int32_t rc = cache_plan(a, sms > 0 ? sms : 148, plan); rc != PC_OK) return rc;
+  if (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16) || (a->k_win == nullptr) != (a->v_win == nullptr)) return PC_ERR_INVALID_ARG;
+  if (!aligned(a->k_win, 16) || !aligned(a->v_win, 16) || !aligned(a->workspace, 16)) return PC_ERR_INVALID_ARG;
+  if (plan.n_slots == 0 && a->k_win == nullptr) return PC_ERR_INVALID_ARG;              // nothing to attend to
+  if ((a->q_pos == nullptr && a->q_pos0 < 0) || !(a->rope_theta >= 0.0f) || !(a->softmax_scale >= 0.0f)) return PC_ERR_INVALID_ARG;
+  pc::CacheRows rows = {};
+  pc::CacheMerge merge = {};
+  if (!strides(a->q_stride, a->w, a->Hq, a->d, rows.stride) || !strides(a->k_win_stride, a->w, a->Hkv, a->d, merge.k_stride) ||
+      !strides(a->v_win_stride, a->w, a->Hkv, a->d, merge.v_stride))
+    return PC_ERR_INVALID_ARG;
+  if (!a->workspace || a->workspace_bytes < plan.total) return PC_ERR_WORKSPACE;
+  if (sms == 0) return PC_ERR_UNSUPPORTED;
+
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  uint8_t* const ws = static_cast<uint8_t*>(a->workspace);
+  rows.q = a->q; rows.B = a->B; rows.w = a->w; rows.Hq = a->Hq; rows.Hkv = a->Hkv; rows.pos0 = a->q_pos0; rows.pos = a->q_pos;
+  rows.theta = (double)a->rope_theta; rows.rows = ws + plan.off_rows;
+  cudaError_t e = pc::launch_cache_rows(rows, a->d, st);
+
+  const double scale = a->softmax_scale > 0.0f ? (double)a->softmax_scale : 1.0 / std::sqrt((double)a->d);
+  const float scale_log2 = (float)(scale * 1.4426950408889634);
+  int slot = 0;
+  for (int own = 0; own <= 1 && e == cudaSuccess; ++own) {
+    const pc_kv_cache* const c = own ? a->own : a->prefix;
+    const int n = own ? a->n_own : a->n_prefix;
+    if (n == 0) continue;
+    const PhasePlan& ph = own ? plan.own : plan.prefix;
+    pc::CachePhase p = {};
+    p.seqs = own ? a->B : 1;
+    p.rows = own ? a->w * (a->Hq / a->Hkv) : (int)plan.total_rows;
+    p.Hkv = a->Hkv; p.n_keys = n; p.len = own ? a->own_len : nullptr;
+    p.k_scale = c->k_scale; p.v_scale = c->v_scale; p.capacity = c->capacity;
+    p.n_rg = ph.n_rg; p.n_split = ph.n_split; p.slot0 = slot; p.n_slots = plan.n_slots; p.total_rows = (int)plan.total_rows;
+    p.scale_log2 = scale_log2;
+    p.q_rows = reinterpret_cast<const __nv_bfloat16*>(ws + plan.off_rows);
+    p.part_o = reinterpret_cast<float*>(ws + plan.off_o);
+    p.part_ml = reinterpret_cast<float2*>(ws + plan.off_ml);
+    p.status = a->status_word;
+    p.wait_kcycles = pc::wait_limit_kcycles();
+    CUtensorMap tm_k, tm_v;
+    if (!cache_maps(c, n, pc::few_keys(c->format, c->d, p.rows), &tm_k, &tm_v)) { launched(e); return PC_ERR_CUDA; }
+    e = pc::launch_cache_few(tm_k, tm_v, p, c->format, c->d, st);
+    slot += ph.n_split;
+  }
+  if (e != cudaSuccess) return launched(e);
+  merge.B = a->B; merge.w = a->w; merge.Hq = a->Hq; merge.Hkv = a->Hkv; merge.n_slots = plan.n_slots; merge.total_rows = (int)plan.total_rows;
+  merge.part_o = reinterpret_cast<const float*>(ws + plan.off_o);
+  merge.part_ml = reinterpret_cast<const float2*>(ws + plan.off_ml);
+  merge.q_rows = reinterpret_cast<const __nv_bfloat16*>(ws + plan.off_rows);
+  merge.k_win = a->k_win; merge.v_win = a->v_win; merge.scale_log2 = scale_log2;
+  merge.out = static_cast<__nv_bfloat16*>(a->out); merge.lse = a->lse;
+  return launched(pc::launch_cache_merge(merge, a->d, st));
+}
+
+}  // extern "C"

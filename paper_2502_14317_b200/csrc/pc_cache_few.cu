@@ -1,0 +1,463 @@
+// Attention of few query rows over a cache in bf16 or 8 bits (pc_cache_attn): up to 32 rows of a kv-head at a time.
+//
+// With keys, then head-dim columns, as the 16 rows of a product and the query rows as its 8 columns,
+//     S^T [16 keys x 8 rows] = K Q^T,      O^T [16 of d x 8 rows] += V^T P^T,
+// a step computes what its rows need (8, 16 or 32 of them) and no more, and the codes of a cache go from shared memory into
+// the operands' registers on their way: the operand layout asks a thread for 4 consecutive elements of a key at a time (for V: of
+// 4 keys at a time, so that bytes of two keys are interleaved), and which elements of d they are is free as long as Q has
+// them in the same order.  int8 and e4m3 become half precision exactly; the scale of a key multiplies its row of S^T, the scale
+// of a value its probability, so nothing that a cache holds is rounded.  Queries are bf16 numbers; times a power of two of their row
+// they are halves too (elements 2^-22 below the row's largest lose bits).  Probabilities are rounded to half precision (11 bits,
+// bf16 caches: bf16, 8 bits) beside sums and accumulators in fp32; half precision has a short range, so they are held relative to the
+// largest product of probability and scale of their row (c below), raised together with the reference maximum.
+//
+// Bound by reading the cache.  A warp takes 16 keys at a time on its own, with its own maximum, sum and accumulators, and waits for
+// nobody but the copies; a producer warp keeps the ring full.  The maximum is looked at with one vote per 8 rows and raised
+// only where a logit exceeds it by 2^8.  The warps' results are added in shared memory, the splits' by the merge kernel.
+#include "pc_cache.h"
+#include "pc_kernels.h"
+#include "pc_kv8.cuh"
+#include "pc_sm100.cuh"
+#include <cfloat>
+
+namespace pc {
+
+namespace {
+
+template <int D_, int FMT_, int NT8_>
+struct Few {
+  static constexpr int D = D_, FMT = FMT_, NT8 = NT8_;
+  static constexpr int EB = FMT == FMT_BF16 ? 2 : 1;            // bytes of an element
+  static constexpr int ROWB = D * EB, BOXES = ROWB > 128 ? 2 : 1, BOXB = ROWB / BOXES, EPB = BOXB / EB;
+  static constexpr int SWZ = BOXB == 128 ? 7 : 3;
+  static constexpr int WARPS = NT8 <= 2 ? 4 : 8;                // consumer warps
+  static constexpr int CTAS = NT8 <= 2 ? 2 : 1;                 // CTAs of an SM
+  static constexpr int STEPS = NT8 <= 2 && ROWB <= 128 ? 2 : 1;
+  static constexpr int KEYS = 16 * WARPS * STEPS, HALF_BYTES = KEYS * ROWB, STAGE_BYTES = 2 * HALF_BYTES;
+  static constexpr int NS_ = 98304 * (CTAS == 1 ? 2 : 1) / STAGE_BYTES, NS = NS_ > 8 ? 8 : NS_;
+  static constexpr int N = 8 * NT8, KST = D / 16, MT = D / 16;
+  static constexpr int THREADS = 32 * (WARPS + 1);
+  static constexpr int OFF_SCALE = NS * STAGE_BYTES, OFF_Q = OFF_SCALE + (EB == 1 ? NS * 2 * KEYS * 4 : 0), OFF_MISC = OFF_Q + KST * NT8 * 256;
+  static constexpr int CPT = BOXB / 64, EPC = 16 / EB, KPC = EPC / 4;      // 16-byte chunks of a thread in a box row, their elements and k-steps
+  static_assert(WARPS * N * D * 4 <= OFF_SCALE, "partial results of the warps go into the ring");
+};
+template <class C>
+struct __align__(16) FewMisc {
+  uint64_t full[C::NS], empty[C::NS];
+  int abort_flag;                                               // these two words stay adjacent (bounded waits)
+  int wait_kcycles;
+  float qs[C::N];                                               // scale of a row's logits, in log2 units
+  float2 ml[C::WARPS][C::N];
+};
+enum { WF_FULL = 411, WF_EMPTY };
+
+__device__ __forceinline__ uint32_t full_par(uint32_t n) { return n & 1u; }
+__device__ __forceinline__ uint32_t free_par(uint32_t n) { return (n & 1u) ^ 1u; }
+
+template <int FMT>
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (FMT == FMT_BF16)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+template <int FMT>
+__device__ __forceinline__ uint32_t pack_p(float lo, float hi) {
+  if constexpr (FMT == FMT_BF16) return pack_bf16x2(lo, hi);
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float max_over_keys(float x) {
+#pragma unroll
+  for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
+  return x;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+  return v;
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, bool there) {      // zero where there is no entry
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {                             // once this thread's copies have landed
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
+}  // namespace
+
+template <class C>
+__global__ void __launch_bounds__(C::THREADS, C::CTAS)
+cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CachePhase prm) {
+  constexpr int D = C::D, FMT = C::FMT, NT8 = C::NT8, N = C::N, KEYS = C::KEYS, NS = C::NS;
+  constexpr bool Q8 = FMT != FMT_BF16;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  FewMisc<C>& mi = *reinterpret_cast<FewMisc<C>*>(smem + C::OFF_MISC);
+  volatile int* const abort_flag = &mi.abort_flag;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  int x = blockIdx.x;
+  const int split = x % prm.n_split; x /= prm.n_split;
+  const int rg = x % prm.n_rg; x /= prm.n_rg;
+  const int hkv = x % prm.Hkv, seq = x / prm.Hkv;
+
+  if (tid == 0) {
+    for (int i = 0; i < NS; ++i) { mbar_init(&mi.full[i], Q8 ? 33 : 1); mbar_init(&mi.empty[i], C::WARPS); }
+    mi.abort_flag = 0;
+    mi.wait_kcycles = prm.wait_kcycles;
+    fence_mbar_init();
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
+  __syncthreads();
+  chain();
+  int n = prm.n_keys;                                            // entries of this sequence
+  if (prm.len != nullptr) { n = prm.len[seq]; n = n < 0 ? 0 : n > prm.n_keys ? prm.n_keys : n; }
+  const int n_all = (n + KEYS - 1) / KEYS;
+  const int j0 = (int)((long long)n_all * split / prm.n_split), nt = (int)((long long)n_all * (split + 1) / prm.n_split) - j0;
+  const int row0 = seq * prm.rows + rg * N, n_rows = prm.rows - rg * N < N ? prm.rows - rg * N : N;      // rows of the kv-head
+  const size_t part0 = ((size_t)hkv * prm.total_rows + row0) * prm.n_slots + prm.slot0 + split;
+
+  if (nt == 0) {                                                 // nothing for this split: the merge leaves it out
+    if (tid < n_rows) prm.part_ml[part0 + (size_t)tid * prm.n_slots] = make_float2(-INFINITY, 0.0f);
+    return;
+  }
+
+  // copies of tile i into its stage; the whole producer warp calls
+  auto load = [&](int i) {
+    const int st = i % NS, key = (j0 + i) * KEYS;
+    if (lane == 0) {
+      mbar_arrive_expect_tx(&mi.full[st], C::STAGE_BYTES);
+#pragma unroll
+      for (int b = 0; b < C::BOXES; ++b) {
+        tma_load_4d(smem + st * C::STAGE_BYTES + b * KEYS * C::BOXB, &tm_k, &mi.full[st], b * C::EPB, key, hkv, seq);
+        tma_load_4d(smem + st * C::STAGE_BYTES + C::HALF_BYTES + b * KEYS * C::BOXB, &tm_v, &mi.full[st], b * C::EPB, key, hkv, seq);
+      }
+    }
+    if constexpr (Q8) {
+      const size_t at = ((size_t)seq * prm.Hkv + hkv) * prm.capacity;
+      const uint32_t dst = smem_u32(smem + C::OFF_SCALE) + st * (2 * KEYS * 4);
+      for (int k = lane; k < KEYS; k += 32) {
+        const bool there = key + k < n;
+        const size_t e = at + (there ? key + k : 0);
+        cp_async4(dst + k * 4, prm.k_scale + e, there);
+        cp_async4(dst + (KEYS + k) * 4, prm.v_scale + e, there);
+      }
+      cp_async_arrive(&mi.full[st]);
+    }
+    __syncwarp();
+  };
+
+  if (warp == C::WARPS) {
+    for (int i = 0; i < NS && i < nt; ++i) load(i);
+  } else {
+    // ---- the rows' queries as operands, in the order in which the threads hold their keys
+    for (int r = warp; r < N; r += C::WARPS) {
+      uint2 q = make_uint2(0, 0);
+      if (r < n_rows && lane < D / 4) q = __ldg(reinterpret_cast<const uint2*>(prm.q_rows + ((size_t)hkv * prm.total_rows + row0 + r) * D) + lane);
+      float qs = prm.scale_log2;
+      if constexpr (Q8) {
+        uint32_t m = __vmaxu2(q.x & 0x7FFF7FFFu, q.y & 0x7FFF7FFFu);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        const int e = (int)(max(m & 0xFFFFu, m >> 16) >> 7);             // exponent of the largest; 255: not finite
+        const int up = e == 255 || e < 27 ? 0 : 127 + 7 - e;             // largest in [2^7, 2^8)
+        const float f = __uint_as_float((uint32_t)(127 + up) << 23);
+        qs *= __uint_as_float((uint32_t)(127 - up) << 23);
+        const float a = __uint_as_float(q.x << 16), b = __uint_as_float(q.x & 0xFFFF0000u), c = __uint_as_float(q.y << 16),
+                    d = __uint_as_float(q.y & 0xFFFF0000u);
+        q = make_uint2(pack_p<FMT>(a * f, b * f), pack_p<FMT>(c * f, d * f));
+      }
+      if (lane < D / 4) {
+        const int d = 4 * lane, b = d / C::EPB, in = d % C::EPB, chunk = in / C::EPC, t = in % C::EPC / 4;
+        const int ks = (b * C::CPT + chunk % C::CPT) * C::KPC + t, a = chunk / C::CPT;
+        reinterpret_cast<uint2*>(smem + C::OFF_Q)[(ks * NT8 + r / 8) * 32 + (r % 8) * 4 + a] = q;
+      }
+      if (lane == 0) mi.qs[r] = r < n_rows ? qs : 0.0f;
+    }
+  }
+  __syncthreads();
+
+  if (warp == C::WARPS) {
+    int i = NS < nt ? NS : nt;
+    for (; i < nt && !*abort_flag; ++i) {
+      if (!mbar_wait(&mi.empty[i % NS], free_par(i / NS), abort_flag, prm.status, WF_EMPTY)) break;
+      load(i);
+    }
+    for (int k = i > NS ? i - NS : 0; k < i; ++k) mbar_wait_drain(&mi.full[k % NS], full_par(k / NS), abort_flag);   // every copy has landed before exit
+  } else {
+    // ================================================================ a warp: 16 keys at a time
+    const int g = lane >> 2, a = lane & 3;
+    constexpr bool Q_REGS = NT8 <= 2;
+    uint2 qf[Q_REGS ? C::KST : 1][Q_REGS ? NT8 : 1];
+    const uint32_t sq = smem_u32(smem + C::OFF_Q) + lane * 8;
+    if constexpr (Q_REGS) {
+#pragma unroll
+      for (int ks = 0; ks < C::KST; ++ks)
+#pragma unroll
+        for (int t = 0; t < NT8; ++t) qf[ks][t] = lds64(sq + (ks * NT8 + t) * 256);
+    }
+    // per row pair (2 a, 2 a + 1) of each 8 rows: reference maximum (log2 units), sum over this thread's keys, scale of the weights
+    float m[NT8][2], l[NT8][2], cw[NT8][2], qs[NT8][2], acc[C::MT][NT8][4];
+#pragma unroll
+    for (int t = 0; t < NT8; ++t)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        m[t][e] = -FLT_MAX; l[t][e] = 0.0f; cw[t][e] = 0x1p110f; qs[t][e] = mi.qs[8 * t + 2 * a + e];
+      }
+#pragma unroll
+    for (int j = 0; j < C::MT; ++j)
+#pragma unroll
+      for (int t = 0; t < NT8; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[j][t][e] = 0.0f;
+
+    for (int i = 0; i < nt; ++i) {
+      const int st = i % NS;
+      if (!mbar_wait(&mi.full[st], full_par(i / NS), abort_flag, prm.status, WF_FULL)) break;
+      const uint32_t stage = smem_u32(smem) + st * C::STAGE_BYTES;
+#pragma unroll 1
+      for (int step = 0; step < C::STEPS; ++step) {
+        const int r0 = (step * C::WARPS + warp) * 16, key0 = (j0 + i) * KEYS + r0;
+        if (key0 >= n) continue;
+        const bool tail = key0 + 16 > n;
+        // ---- S^T, two chains of products
+        float s[2][NT8][4];
+#pragma unroll
+        for (int t = 0; t < NT8; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[0][t][e] = s[1][t][e] = 0.0f;
+#pragma unroll
+        for (int b = 0; b < C::BOXES; ++b)
+#pragma unroll
+          for (int h = 0; h < C::CPT; ++h) {
+            uint4 kr[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              uint32_t off = (r0 + g + 8 * u) * C::BOXB + (a * C::CPT + h) * 16;
+              off ^= ((off >> 7) & C::SWZ) << 4;
+              kr[u] = lds128(stage + b * KEYS * C::BOXB + off);
+            }
+            const uint32_t x0[4] = {kr[0].x, kr[0].y, kr[0].z, kr[0].w}, x1[4] = {kr[1].x, kr[1].y, kr[1].z, kr[1].w};
+#pragma unroll
+            for (int t = 0; t < C::KPC; ++t) {
+              const int ks = (b * C::CPT + h) * C::KPC + t;
+              uint32_t a0, a1, a2, a3;
+              if constexpr (Q8) {
+                const uint32_t y0 = flip_signs<FMT>(x0[t]), y1 = flip_signs<FMT>(x1[t]);
+                a0 = codes_to_half2<FMT, 0>(y0); a2 = codes_to_half2<FMT, 1>(y0);
+                a1 = codes_to_half2<FMT, 0>(y1); a3 = codes_to_half2<FMT, 1>(y1);
+              } else {
+                a0 = x0[2 * t]; a2 = x0[2 * t + 1]; a1 = x1[2 * t]; a3 = x1[2 * t + 1];
+              }
+#pragma unroll
+              for (int c = 0; c < NT8; ++c) {
+                uint2 q;
+                if constexpr (Q_REGS) q = qf[ks][c]; else q = lds64(sq + (ks * NT8 + c) * 256);
+                mma16816<FMT>(s[ks & 1][c], a0, a1, a2, a3, q.x, q.y);
+              }
+            }
+          }
+        // ---- V of this thread: 4 keys (positions 2 a, 2 a + 1, 2 a + 8, 2 a + 9 of the 16)
+        uint32_t v[C::BOXES][4][C::BOXB / 32];
+#pragma unroll
+        for (int b = 0; b < C::BOXES; ++b)
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int k = 2 * a + (u & 1) + 8 * (u >> 1);
+            uint32_t off = (r0 + k) * C::BOXB + g * (C::BOXB / 8);
+            off ^= ((off >> 7) & C::SWZ) << 4;
+            const uint32_t from = stage + C::HALF_BYTES + b * KEYS * C::BOXB + off;
+            if constexpr (C::BOXB == 128) {
+              const uint4 y = lds128(from);
+              v[b][u][0] = y.x; v[b][u][1] = y.y; v[b][u][2] = y.z; v[b][u][3] = y.w;
+            } else {
+              const uint2 y = lds64(from);
+              v[b][u][0] = y.x; v[b][u][1] = y.y;
+            }
+            if (tail && key0 + k >= n) {                         // whatever stands behind the last entry, NaN included
+#pragma unroll
+              for (int z = 0; z < C::BOXB / 32; ++z) v[b][u][z] = 0;
+            }
+          }
+        float sk0 = 1.0f, sk1 = 1.0f, sv0 = 1.0f, sv1 = 1.0f;
+        if constexpr (Q8) {
+          const float* const sc = reinterpret_cast<const float*>(smem + C::OFF_SCALE) + st * 2 * KEYS + r0 + g;
+          sk0 = sc[0]; sk1 = sc[8]; sv0 = sc[KEYS]; sv1 = sc[KEYS + 8];
+        }
+        const bool out0 = tail && key0 + g >= n, out1 = tail && key0 + g + 8 >= n;
+        // ---- probabilities
+        uint32_t pb[NT8][2];
+#pragma unroll
+        for (int t = 0; t < NT8; ++t) {
+          float z[4], p[4], w[4];
+          bool raise = false;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            z[e] = (s[0][t][e] + s[1][t][e]) * ((e < 2 ? sk0 : sk1) * qs[t][e & 1]);
+            if (e < 2 ? out0 : out1) z[e] = -INFINITY;
+            p[e] = fast_exp2(z[e] - m[t][e & 1]);
+            raise |= z[e] > m[t][e & 1] + 8.0f;
+            w[e] = p[e];
+            if constexpr (Q8) {
+              w[e] = p[e] * ((e < 2 ? sv0 : sv1) * cw[t][e & 1]);
+              raise |= !(w[e] <= 32768.0f);
+            }
+          }
+          if (__any_sync(0xFFFFFFFFu, raise)) {                  // rare after the first keys
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float top = fmaxf(m[t][e], max_over_keys(fmaxf(z[e], z[2 + e])));
+              float f = fast_exp2(m[t][e] - top);
+              m[t][e] = top;
+              l[t][e] *= f;
+              p[e] = fast_exp2(z[e] - top);
+              p[2 + e] = fast_exp2(z[2 + e] - top);
+              w[e] = p[e]; w[2 + e] = p[2 + e];
+              if constexpr (Q8) {                                // cw = 1024 / (largest weight so far)
+                const float before = f * (1024.0f / cw[t][e]);
+                const float most = fmaxf(fmaxf(before, max_over_keys(fmaxf(p[e] * sv0, p[2 + e] * sv1))), 0x1p-100f);
+                cw[t][e] = 1024.0f / most;
+                f = before / most;
+                w[e] = p[e] * (sv0 * cw[t][e]);
+                w[2 + e] = p[2 + e] * (sv1 * cw[t][e]);
+              }
+#pragma unroll
+              for (int j = 0; j < C::MT; ++j) { acc[j][t][e] *= f; acc[j][t][2 + e] *= f; }
+            }
+          }
+          l[t][0] += p[0] + p[2];
+          l[t][1] += p[1] + p[3];
+          if (Q8 && tail) {                                      // scales behind the last entry may be anything
+            if (out0) w[0] = w[1] = 0.0f;
+            if (out1) w[2] = w[3] = 0.0f;
+          }
+          pb[t][0] = transpose8x8(pack_p<FMT>(w[0], w[1]));
+          pb[t][1] = transpose8x8(pack_p<FMT>(w[2], w[3]));
+        }
+        // ---- O^T
+#pragma unroll
+        for (int b = 0; b < C::BOXES; ++b)
+#pragma unroll
+          for (int z = 0; z < C::BOXB / 32; ++z) {
+            if constexpr (Q8) {
+              uint32_t h[4];                                     // bytes of keys 0 and 1: columns 0, 1 / 2, 3; of keys 2 and 3
+#pragma unroll
+              for (int u = 0; u < 2; ++u) {
+                h[2 * u] = flip_signs<FMT>(prmt(v[b][2 * u][z], v[b][2 * u + 1][z], 0x5140));
+                h[2 * u + 1] = flip_signs<FMT>(prmt(v[b][2 * u][z], v[b][2 * u + 1][z], 0x7362));
+              }
+#pragma unroll
+              for (int y = 0; y < 2; ++y) {
+                const int j = b * (C::MT / C::BOXES) + 2 * z + y;
+                const uint32_t a0 = codes_to_half2<FMT, 0>(h[y]), a1 = codes_to_half2<FMT, 1>(h[y]), a2 = codes_to_half2<FMT, 0>(h[2 + y]),
+                               a3 = codes_to_half2<FMT, 1>(h[2 + y]);
+#pragma unroll
+                for (int t = 0; t < NT8; ++t) mma16816<FMT>(acc[j][t], a0, a1, a2, a3, pb[t][0], pb[t][1]);
+              }
+            } else {
+              const int j = b * (C::MT / C::BOXES) + z;
+              const uint32_t a0 = prmt(v[b][0][z], v[b][1][z], 0x5410), a1 = prmt(v[b][0][z], v[b][1][z], 0x7632),
+                             a2 = prmt(v[b][2][z], v[b][3][z], 0x5410), a3 = prmt(v[b][2][z], v[b][3][z], 0x7632);
+#pragma unroll
+              for (int t = 0; t < NT8; ++t) mma16816<FMT>(acc[j][t], a0, a1, a2, a3, pb[t][0], pb[t][1]);
+            }
+          }
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&mi.empty[st]);
+    }
+    // ---- what this warp has: sums over its threads' keys, statistics; then, the ring being idle, O
+#pragma unroll
+    for (int t = 0; t < NT8; ++t)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l[t][e] += __shfl_xor_sync(0xFFFFFFFFu, l[t][e], o);
+        if (g == 0) mi.ml[warp][8 * t + 2 * a + e] = make_float2(m[t][e], l[t][e]);
+      }
+    named_barrier_sync(1, 32 * C::WARPS);                        // every warp has read its last stage
+    float* const part = reinterpret_cast<float*>(smem) + (size_t)warp * N * D;
+#pragma unroll
+    for (int t = 0; t < NT8; ++t)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float f = Q8 ? 1.0f / cw[t][e] : 1.0f;
+#pragma unroll
+        for (int j = 0; j < C::MT; ++j) {
+          constexpr int PER = C::MT / C::BOXES;
+          const int d = (j / PER) * C::EPB + g * (C::EPB / 8) + 2 * (j % PER);
+          *reinterpret_cast<float2*>(part + (8 * t + 2 * a + e) * D + d) = make_float2(acc[j][t][e] * f, acc[j][t][2 + e] * f);
+        }
+      }
+  }
+  __syncthreads();
+  // ---- the warps' results added up
+  for (int e = tid; e < n_rows * (D / 4); e += C::THREADS) {
+    const int r = e / (D / 4), c = e % (D / 4);
+    float top = -FLT_MAX, sum = 0.0f;
+#pragma unroll
+    for (int k = 0; k < C::WARPS; ++k) top = fmaxf(top, mi.ml[k][r].x);
+    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int k = 0; k < C::WARPS; ++k) {
+      const float2 ml = mi.ml[k][r];
+      const float f = fast_exp2(ml.x - top);
+      const float4 y = reinterpret_cast<const float4*>(smem)[(k * N + r) * (D / 4) + c];
+      sum = fmaf(f, ml.y, sum);
+      o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
+    }
+    const size_t at = part0 + (size_t)r * prm.n_slots;
+    reinterpret_cast<float4*>(prm.part_o + at * D)[c] = o;
+    if (c == 0) prm.part_ml[at] = sum == 0.0f ? make_float2(-INFINITY, 0.0f) : make_float2(top, sum);
+  }
+}
+
+namespace {
+
+template <int D, int FMT, int NT8>
+cudaError_t few_t(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, cudaStream_t st) {
+  using C = Few<D, FMT, NT8>;
+  constexpr int SMEM = C::OFF_MISC + (int)sizeof(FewMisc<C>);
+  static_assert(C::CTAS * (SMEM + 1024) <= 233472, "CTAs per SM");
+  if (cudaError_t e = cudaFuncSetAttribute(cache_few_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM); e != cudaSuccess) return e;
+  return launch_chained(cache_few_kernel<C>, dim3((unsigned)((long long)p.seqs * p.Hkv * p.n_rg * p.n_split)), dim3(C::THREADS), SMEM, st, 1, tm_k, tm_v, p);
+}
+template <int D, int FMT>
+cudaError_t few_n(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, cudaStream_t st) {
+  const int n = few_rows(p.rows);
+  return n == 8 ? few_t<D, FMT, 1>(tm_k, tm_v, p, st) : n == 16 ? few_t<D, FMT, 2>(tm_k, tm_v, p, st) : few_t<D, FMT, 4>(tm_k, tm_v, p, st);
+}
+template <int D>
+cudaError_t few_d(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, int format, cudaStream_t st) {
+  return format == FMT_INT8 ? few_n<D, FMT_INT8>(tm_k, tm_v, p, st) : format == FMT_E4M3 ? few_n<D, FMT_E4M3>(tm_k, tm_v, p, st) : few_n<D, FMT_BF16>(tm_k, tm_v, p, st);
+}
+template <int D, int FMT>
+int keys_t(int n) { return n == 8 ? Few<D, FMT, 1>::KEYS : n == 16 ? Few<D, FMT, 2>::KEYS : Few<D, FMT, 4>::KEYS; }
+
+}  // namespace
+
+int few_rows(int rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
+int few_ctas_per_sm(int rows) { return few_rows(rows) <= 16 ? 2 : 1; }
+int few_keys(int format, int d, int rows) {
+  const int n = few_rows(rows);
+  if (format == FMT_BF16) return d == 128 ? keys_t<128, FMT_BF16>(n) : keys_t<64, FMT_BF16>(n);
+  return d == 128 ? keys_t<128, FMT_INT8>(n) : keys_t<64, FMT_INT8>(n);
+}
+cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, int format, int d, cudaStream_t st) {
+  return d == 128 ? few_d<128>(tm_k, tm_v, p, format, st) : few_d<64>(tm_k, tm_v, p, format, st);
+}
+
+}  // namespace pc

@@ -9,6 +9,8 @@ namespace pc {
 // ---- pc_api.cu
 // Every kernel launch of the library is counted here (see pc_launch_count in pc.h).
 void note_launch();
+int wait_limit_kcycles();                        // limit of the device-side waits, units of 1024 cycles
+int sm100_count();                               // SMs of the current device, 0 if it is not an sm_100
 
 // Launches of one call, and of calls on one stream, follow each other closely: every kernel is launched with programmatic
 // stream serialisation, so that it is set up while its predecessor drains, and begins with chain() (kernels with a
