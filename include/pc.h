@@ -458,11 +458,13 @@ PC_API int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0
  *   - causally to the new tokens' own keys and values k_win, v_win [B,w,Hkv,d] (both NULL: not; a program that has written
  *     them to its cache already).
  * One softmax over all of them.  prefix and own may have different formats; entries behind those named are never used, whatever
- * they hold.  Keys are rotated already; token i of sequence b is rotated here at position q_pos0 + (q_pos ? q_pos[b] : 0) + i and
- * rounded to bf16, as in pc_parallel_attn; rope_theta = 0: queries come rotated.  q, k_win and v_win through element
+ * they hold.  Keys are rotated already; token i of sequence b is rotated here at position p = q_pos0 + (q_pos ? q_pos[b] : 0) + i
+ * and rounded to bf16: in fp32 (angles are the fp32 products p * theta^(-2t/d), as models compute them; from p = 2^15 on
+ * they are computed in fp64), where pc_parallel_attn rounds the fp64 rotation; rope_theta = 0: queries come rotated.  q, k_win and v_win through element
  * strides (sequence, token, head; 0,0,0 -> contiguous), multiples of 8.  A row that sees nothing gets zeros and lse -infinity.
  * out [B,w,Hq,d] bf16 and lse [B,Hq,w] fp32 (natural log; may be NULL) contiguous.
- * 1 <= w <= 128, d in {64, 128}, any Hq / Hkv.  Workspace: pc_cache_attn_workspace_bytes(args) (reads the sizes alone).
+ * 1 <= w <= 128, d in {64, 128}, any Hq / Hkv.  Workspace: pc_cache_attn_workspace_bytes(args) (reads the sizes and the caches'
+ * descriptors alone), aligned to 32 bytes.
  */
 typedef struct {
   int32_t B, w, Hq, Hkv, d;

@@ -34,14 +34,17 @@ struct KvRead {
 };
 cudaError_t launch_kv_dequantize(const KvRead& r, int format, int d, int sm_count, cudaStream_t st);
 
-// Queries of pc_cache_attn as rows: rows[hkv][(b * w + i) * G + g][d], rotated and rounded to bf16 (theta 0: as they are).
+// Queries of pc_cache_attn as rows: rows[hkv][(b * w + i) * G + g][d], rotated and rounded to bf16 (theta 0: as they are); halves
+// (or null): the same times a power of two of each row, as numbers of half precision, and its inverse times scale_log2 in half_scale.
 struct CacheRows {
   const void* q;
   long long stride[3];
   int B, w, Hq, Hkv, pos0;
   const int* pos;
-  double theta;
-  void* rows;
+  float theta, scale_log2;
+  void *rows, *halves;
+  float* half_scale;             // [Hkv,total_rows]
+  int* clear;                    // a word that is set to 0, or null
 };
 cudaError_t launch_cache_rows(const CacheRows& p, int d, cudaStream_t st);
 
@@ -66,6 +69,18 @@ int few_keys(int format, int d, int rows);       // keys of a stage
 int few_rows(int rows);                          // rows of a row group
 int few_ctas_per_sm(int rows);
 cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, int format, int d, cudaStream_t st);
+
+// The same phase for more than 32 rows of one sequence (pc_cache_wide.cu), blocks of 128 rows.
+struct WidePhase {
+  CachePhase c;                  // n_rg, n_split: of the blocks below
+  int alt;                       // 1: the two blocks of a CTA hold the same rows and take alternate key tiles; 0: different rows
+  int n_tiles;                   // 128-key tiles
+  const float* half_scale;       // [Hkv,total_rows] (8-bit formats)
+  const uint8_t *k8, *v8;        // 8-bit formats: the cache's codes
+  int* counter;                  // work queue, zeroed
+};
+// maps: rows of queries (box 64 x 128 rows; halves for 8-bit formats), and for bf16 keys (128, of a pair 64 entries) and values (128)
+cudaError_t launch_cache_wide(const CUtensorMap* maps, const WidePhase& p, int format, int d, bool pair, int sm_count, cudaStream_t st);
 
 // Joins the slots of a row and the new tokens' own keys.
 struct CacheMerge {

@@ -94,17 +94,18 @@ int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0, const
 // ------------------------------------------------------------------------------------ attention over shared and own caches
 namespace {
 
-struct PhasePlan { int n_rg, n_split; };
+struct PhasePlan { bool wide, pair; int alt, n_rg, n_split; };
 struct CachePlan {
   PhasePlan prefix, own;
   int n_slots;
   int64_t total_rows;
-  size_t off_rows, off_ml, off_o, total;
+  bool halves;                                   // the rows as halves as well (a wide phase over 8-bit codes)
+  size_t off_counter, off_rows, off_halves, off_scale, off_ml, off_o, total;
 };
 
 // Splits of the keys: rounds of the grid x (some tiles of fixed cost + tiles of a split) is least.
 PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count) {
-  PhasePlan p;
+  PhasePlan p = {};
   const int per = pc::few_rows((int)rows), keys = pc::few_keys(format, d, (int)rows);
   p.n_rg = (int)((rows + per - 1) / per);
   const int tiles = (n_keys + keys - 1) / keys;
@@ -118,6 +119,27 @@ PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n
   return p;
 }
 
+// Row groups and splits of the kernel for many rows: least time by a model in microseconds, as for the query windows - rounds
+// of the grid x (5 for an item + a tile), and the partial results through memory twice.
+PhasePlan wide_plan(int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count) {
+  PhasePlan p = {};
+  p.wide = true;
+  p.pair = format == PC_KV_BF16 && d == 128 && rows > 128 && sm_count >= 2;
+  const int64_t block = p.pair ? 256 : 128, blocks = (rows + block - 1) / block, units = p.pair ? sm_count / 2 : sm_count;
+  const int tiles = (n_keys + 127) / 128;
+  double least = -1.0;
+  for (int alt = blocks % 2 && blocks < 3 ? 1 : 0; alt <= 1; ++alt) {
+    const int64_t n_rg = alt ? blocks : (blocks + 1) / 2;
+    const double tile_us = alt ? 1.2 : 2.2;
+    for (int s = 1; s <= 64 && (s == 1 || 2 * s <= tiles + 1); ++s) {
+      const double rounds = std::ceil((double)(Hkv * n_rg * s) / (double)units);
+      const double cost = rounds * (5.0 + tile_us * std::ceil((double)tiles / s)) + (double)(rows * Hkv * s) * d * 8.0 / 4.0e6;
+      if (least < 0.0 || cost < least) { least = cost; p.alt = alt; p.n_rg = (int)n_rg; p.n_split = s; }
+    }
+  }
+  return p;
+}
+
 int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
   if (a->B < 1 || a->w < 1 || a->Hq < 1 || a->Hkv < 1 || a->Hq % a->Hkv != 0 || a->n_prefix < 0 || a->n_own < 0) return PC_ERR_INVALID_ARG;
   if (a->d != 64 && a->d != 128) return PC_ERR_UNSUPPORTED;
@@ -125,7 +147,8 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
   const int G = a->Hq / a->Hkv;
   p.total_rows = (int64_t)a->B * a->w * G;
   p.n_slots = 0;
-  p.prefix = p.own = {0, 0};
+  p.prefix = p.own = {};
+  p.halves = false;
   for (int own = 0; own <= 1; ++own) {
     const pc_kv_cache* const c = own ? a->own : a->prefix;
     const int n = own ? a->n_own : a->n_prefix;
@@ -133,11 +156,18 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     if (int32_t rc = check_cache(c, false); rc != PC_OK) return rc;
     if (c->B != (own ? a->B : 1) || c->Hkv != a->Hkv || c->d != a->d || n > c->capacity) return PC_ERR_INVALID_ARG;
     PhasePlan& ph = own ? p.own : p.prefix;
+    if (!own && p.total_rows > 32) {
+      ph = wide_plan(p.total_rows, a->Hkv, a->d, c->format, n, sm_count);
+      p.halves = c->format != PC_KV_BF16;
+    } else
     ph = few_plan(own ? a->B : 1, own ? (int64_t)a->w * G : p.total_rows, a->Hkv, a->d, c->format, n, sm_count);
     if ((own ? a->B : 1ll) * a->Hkv * ph.n_rg * ph.n_split > 0x7FFFFFFF) return PC_ERR_UNSUPPORTED;
     p.n_slots += ph.n_split;
   }
   size_t off = 0;
+  p.off_counter = off; off += ALIGN;
+  p.off_halves = off; off += p.halves ? align_up((size_t)p.total_rows * a->Hkv * a->d * 2) : 0;
+  p.off_scale = off; off += p.halves ? align_up((size_t)p.total_rows * a->Hkv * sizeof(float)) : 0;
   p.off_rows = off; off += align_up((size_t)p.total_rows * a->Hkv * a->d * 2);
   p.off_ml = off; off += align_up((size_t)p.total_rows * a->Hkv * p.n_slots * sizeof(float2));
   p.off_o = off; off += align_up((size_t)p.total_rows * a->Hkv * p.n_slots * a->d * sizeof(float));
@@ -174,7 +204,7 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
   const int sms = pc::sm100_count();
   if (int32_t rc = cache_plan(a, sms > 0 ? sms : 148, plan); rc != PC_OK) return rc;
   if (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16) || (a->k_win == nullptr) != (a->v_win == nullptr)) return PC_ERR_INVALID_ARG;
-  if (!aligned(a->k_win, 16) || !aligned(a->v_win, 16) || !aligned(a->workspace, 16)) return PC_ERR_INVALID_ARG;
+  if (!aligned(a->k_win, 16) || !aligned(a->v_win, 16) || !aligned(a->workspace, 32)) return PC_ERR_INVALID_ARG;
   if (plan.n_slots == 0 && a->k_win == nullptr) return PC_ERR_INVALID_ARG;              // nothing to attend to
   if ((a->q_pos == nullptr && a->q_pos0 < 0) || !(a->rope_theta >= 0.0f) || !(a->softmax_scale >= 0.0f)) return PC_ERR_INVALID_ARG;
   pc::CacheRows rows = {};
@@ -188,11 +218,12 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   uint8_t* const ws = static_cast<uint8_t*>(a->workspace);
   rows.q = a->q; rows.B = a->B; rows.w = a->w; rows.Hq = a->Hq; rows.Hkv = a->Hkv; rows.pos0 = a->q_pos0; rows.pos = a->q_pos;
-  rows.theta = (double)a->rope_theta; rows.rows = ws + plan.off_rows;
-  cudaError_t e = pc::launch_cache_rows(rows, a->d, st);
-
   const double scale = a->softmax_scale > 0.0f ? (double)a->softmax_scale : 1.0 / std::sqrt((double)a->d);
   const float scale_log2 = (float)(scale * 1.4426950408889634);
+  rows.theta = a->rope_theta; rows.scale_log2 = scale_log2; rows.rows = ws + plan.off_rows;
+  rows.clear = reinterpret_cast<int*>(ws + plan.off_counter);
+  if (plan.halves) { rows.halves = ws + plan.off_halves; rows.half_scale = reinterpret_cast<float*>(ws + plan.off_scale); }
+  cudaError_t e = pc::launch_cache_rows(rows, a->d, st);
   int slot = 0;
   for (int own = 0; own <= 1 && e == cudaSuccess; ++own) {
     const pc_kv_cache* const c = own ? a->own : a->prefix;
@@ -211,6 +242,23 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
     p.part_ml = reinterpret_cast<float2*>(ws + plan.off_ml);
     p.status = a->status_word;
     p.wait_kcycles = pc::wait_limit_kcycles();
+    if (ph.wide) {
+      pc::WidePhase wp = {};
+      wp.c = p; wp.alt = ph.alt; wp.n_tiles = (n + 127) / 128;
+      wp.half_scale = rows.half_scale;
+      wp.k8 = static_cast<const uint8_t*>(c->k); wp.v8 = static_cast<const uint8_t*>(c->v);
+      wp.counter = rows.clear;
+      const uint64_t d = (uint64_t)a->d, R = (uint64_t)plan.total_rows;
+      const uint64_t dims[4] = {d, R, (uint64_t)a->Hkv, 1}, str[3] = {d, R * d, R * d * (uint64_t)a->Hkv};
+      const uint32_t box[4] = {64, 128, 1, 1};
+      CUtensorMap maps[3] = {}, unused;
+      bool made = pc::make_tmap_bf16_4d(&maps[0], plan.halves ? rows.halves : rows.rows, dims, str, box);
+      if (c->format == PC_KV_BF16) made = made && cache_maps(c, n, ph.pair ? 64 : 128, &maps[1], &unused) && cache_maps(c, n, 128, &unused, &maps[2]);
+      if (!made) { launched(e); return PC_ERR_CUDA; }
+      e = pc::launch_cache_wide(maps, wp, c->format, a->d, ph.pair, sms, st);
+      slot += ph.n_split;
+      continue;
+    }
     CUtensorMap tm_k, tm_v;
     if (!cache_maps(c, n, pc::few_keys(c->format, c->d, p.rows), &tm_k, &tm_v)) { launched(e); return PC_ERR_CUDA; }
     e = pc::launch_cache_few(tm_k, tm_v, p, c->format, c->d, st);

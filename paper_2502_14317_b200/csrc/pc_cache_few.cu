@@ -172,10 +172,9 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
         uint32_t m = __vmaxu2(q.x & 0x7FFF7FFFu, q.y & 0x7FFF7FFFu);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        const int e = (int)(max(m & 0xFFFFu, m >> 16) >> 7);             // exponent of the largest; 255: not finite
-        const int up = e == 255 || e < 27 ? 0 : 127 + 7 - e;             // largest in [2^7, 2^8)
-        const float f = __uint_as_float((uint32_t)(127 + up) << 23);
-        qs *= __uint_as_float((uint32_t)(127 - up) << 23);
+        float inv;
+        const float f = row_factor(max(m & 0xFFFFu, m >> 16), inv);
+        qs *= inv;
         const float a = __uint_as_float(q.x << 16), b = __uint_as_float(q.x & 0xFFFF0000u), c = __uint_as_float(q.y << 16),
                     d = __uint_as_float(q.y & 0xFFFF0000u);
         q = make_uint2(pack_p<FMT>(a * f, b * f), pack_p<FMT>(c * f, d * f));

@@ -2,40 +2,74 @@
 // row's partial results with the new tokens' own keys.
 #include "pc_cache.h"
 #include "pc_kernels.h"
+#include "pc_kv8.cuh"
 #include "pc_sm100.cuh"
+#include <type_traits>
 
 namespace pc {
 
-// rows[hkv][(b * w + i) * G + g][:] = the fp64 rotation of q[b, i, hkv * G + g, :] rounded once to bf16, pairs (t, t + d/2).  A block
-// per token: its angles are computed once, ahead of the wait for the kernel before (as far as they do not depend on it).
+// rows[hkv][(b * w + i) * G + g][:] = q[b, i, hkv * G + g, :] rotated in fp32, pairs (t, t + d/2), and rounded to bf16.  A block per
+// token, a warp per head: a lane holds one pair (d = 64) or two adjacent ones, whose angles it computes once.
+// The angle is one fp32 product of the position and theta^(-2t/d), as models compute it: off by at most 2^-22 of itself, up to
+// position 8192, the longest chunk, by less than half a step of the bf16 result.  From position 2^15 on it is computed in fp64, where the
+// fp32 product would be off by whole steps; fp64 everywhere costs FP64_US.
 template <int D>
 __global__ void __launch_bounds__(256) cache_rows_kernel(const CacheRows p) {
-  constexpr int HALF = D / 2;
-  __shared__ double cs[HALF], sn[HALF];
-  const int b = blockIdx.x / p.w, i = blockIdx.x % p.w, G = p.Hq / p.Hkv;
-  const int tid = threadIdx.x;
-  const bool turn = p.theta > 0.0;
-  double freq = 0.0;
-  if (turn && tid < HALF) freq = pow(p.theta, -2.0 * (double)tid / (double)D);
+  constexpr int E = D / 64;                                   // pairs of a lane
+  using Word = typename std::conditional<E == 2, uint32_t, uint16_t>::type;
+  const int b = blockIdx.x / p.w, i = blockIdx.x % p.w, G = p.Hq / p.Hkv, lane = threadIdx.x & 31;
+  const bool turn = p.theta > 0.0f;
+  float freq[E], c[E], s[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) freq[e] = turn ? powf(p.theta, -2.0f * (float)(E * lane + e) / (float)D) : 0.0f;
   chain();
-  if (turn && tid < HALF) {
-    const long long pos = (long long)p.pos0 + (p.pos ? p.pos[b] : 0) + i;
-    sincos((double)pos * freq, &sn[tid], &cs[tid]);
-  }
-  __syncthreads();
-  const uint16_t* const q = static_cast<const uint16_t*>(p.q) + b * p.stride[0] + i * p.stride[1];
-  uint16_t* const rows = static_cast<uint16_t*>(p.rows);
-  for (int e = tid; e < p.Hq * HALF; e += 256) {
-    const int h = e / HALF, t = e % HALF, hkv = h / G, g = h % G;
-    uint16_t x = q[h * p.stride[2] + t], y = q[h * p.stride[2] + t + HALF];
-    if (turn) {
-      const double u = (double)__uint_as_float((uint32_t)x << 16), v = (double)__uint_as_float((uint32_t)y << 16);
-      x = f64_to_bf16_rne(u * cs[t] - v * sn[t]);
-      y = f64_to_bf16_rne(v * cs[t] + u * sn[t]);
+  if (p.clear != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *p.clear = 0;
+  const long long pos = (long long)p.pos0 + (p.pos ? p.pos[b] : 0) + i;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if (pos < (1 << 15)) {
+      const float a = __fmul_rn((float)pos, freq[e]);
+      c[e] = cosf(a); s[e] = sinf(a);
+    } else {
+      double cd, sd;
+      sincos((double)pos * pow((double)p.theta, -2.0 * (double)(E * lane + e) / (double)D), &sd, &cd);
+      c[e] = (float)cd; s[e] = (float)sd;
     }
-    uint16_t* const to = rows + (((size_t)hkv * p.B * p.w + blockIdx.x) * G + g) * D + t;
-    to[0] = x;
-    to[HALF] = y;
+  }
+  const uint16_t* const q = static_cast<const uint16_t*>(p.q) + b * p.stride[0] + i * p.stride[1];
+  for (int h = threadIdx.x >> 5; h < p.Hq; h += 8) {
+    const int hkv = h / G, g = h % G;
+    const size_t row = ((size_t)hkv * p.B * p.w + blockIdx.x) * G + g;
+    const Word xw = reinterpret_cast<const Word*>(q + h * p.stride[2])[lane], yw = reinterpret_cast<const Word*>(q + h * p.stride[2] + D / 2)[lane];
+    uint16_t u[E], v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      u[e] = (uint16_t)(xw >> (16 * e)); v[e] = (uint16_t)(yw >> (16 * e));
+      if (turn) {
+        const float x = __uint_as_float((uint32_t)u[e] << 16), y = __uint_as_float((uint32_t)v[e] << 16);
+        u[e] = __bfloat16_as_ushort(__float2bfloat16_rn(__fsub_rn(__fmul_rn(x, c[e]), __fmul_rn(y, s[e]))));
+        v[e] = __bfloat16_as_ushort(__float2bfloat16_rn(__fadd_rn(__fmul_rn(y, c[e]), __fmul_rn(x, s[e]))));
+      }
+    }
+    Word* const to = reinterpret_cast<Word*>(static_cast<uint16_t*>(p.rows) + row * D);
+    if constexpr (E == 2) { to[lane] = u[0] | (uint32_t)u[1] << 16; to[32 + lane] = v[0] | (uint32_t)v[1] << 16; }
+    else { to[lane] = u[0]; to[32 + lane] = v[0]; }
+    if (p.halves == nullptr) continue;
+    uint32_t m = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) m = max(m, (uint32_t)max(u[e] & 0x7FFF, v[e] & 0x7FFF));
+    m = __reduce_max_sync(0xFFFFFFFFu, m);
+    float inv;
+    const float f = row_factor(m, inv);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      u[e] = __half_as_ushort(__float2half_rn(__uint_as_float((uint32_t)u[e] << 16) * f));
+      v[e] = __half_as_ushort(__float2half_rn(__uint_as_float((uint32_t)v[e] << 16) * f));
+    }
+    Word* const th = reinterpret_cast<Word*>(static_cast<uint16_t*>(p.halves) + row * D);
+    if constexpr (E == 2) { th[lane] = u[0] | (uint32_t)u[1] << 16; th[32 + lane] = v[0] | (uint32_t)v[1] << 16; }
+    else { th[lane] = u[0]; th[32 + lane] = v[0]; }
+    if (lane == 0) p.half_scale[row] = p.scale_log2 * inv;
   }
 }
 

@@ -184,10 +184,10 @@ __device__ __forceinline__ void mbar_wait_cluster(uint64_t* bar, uint32_t parity
 }
 
 template <class C>
-__device__ __forceinline__ void init_barriers2(Misc2& mi, int wait_kcycles, bool leader) {
+__device__ __forceinline__ void init_barriers2(Misc2& mi, int wait_kcycles, bool leader, uint32_t kv_arrivals = 1) {
   constexpr int N = C::NCTA;
   for (int i = 0; i < C::NQ; ++i) { mbar_init(&mi.q_full[i], 1); mbar_init(&mi.q_free[i], 1); }
-  for (int i = 0; i < C::NS; ++i) { mbar_init(&mi.kv_full[i], 1); mbar_init(&mi.kv_free[i], 1); }
+  for (int i = 0; i < C::NS; ++i) { mbar_init(&mi.kv_full[i], kv_arrivals); mbar_init(&mi.kv_free[i], 1); }
   for (int b = 0; b < 2; ++b) {
     mbar_init(&mi.s_full[b], 1); mbar_init(&mi.o_full[b], 1); mbar_init(&mi.t_full[b], 1);
     mbar_init(&mi.p_half[b], 4 * N); mbar_init(&mi.p_full[b], 4 * N); // 4 softmax warps of the block in each CTA
@@ -422,6 +422,7 @@ struct Hooks {
       : cx(c), p_half(in_cta<C>(&c.mi->p_half[b], 0)), p_full(in_cta<C>(&c.mi->p_full[b], 0)),
         s_read(in_cta<C>(&c.mi->s_read[C::TWO_S ? b : 0], 0)), pv_done(&c.mi->pv_done[b]), tiles(0) {}
   __device__ __forceinline__ void on_read() const { warp_arrive_leader(s_read); }
+  __device__ __forceinline__ void scale_keys(uint32_t (&)[32], uint32_t (&)[32], uint32_t (&)[32], uint32_t (&)[32]) const {}
   __device__ __forceinline__ void before_p() const { WAIT2S(pv_done, free_par(tiles), W2_PV); tc_fence_after_sync(); }
   __device__ __forceinline__ void on_half() const { warp_arrive_leader(p_half); }
   __device__ __forceinline__ void on_full() const { warp_arrive_leader(p_full); }

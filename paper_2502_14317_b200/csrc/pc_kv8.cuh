@@ -56,6 +56,15 @@ __device__ __forceinline__ uint32_t values_to_codes(float a, float b, float c, f
     return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
   }
 }
+// The power of two that brings a row of queries, whose largest magnitude has the bf16 bits `bits`, into the range of half
+// precision (largest in [2^7, 2^8)), and its inverse; 1 where the row is not finite or next to nothing.  Elements 2^-22 below the
+// largest become subnormal and lose bits, 2^-32 below it they are gone.
+__device__ __forceinline__ float row_factor(uint32_t bits, float& inverse) {
+  const int e = (int)(bits >> 7), up = e == 255 || e < 27 ? 0 : 127 + 7 - e;
+  inverse = __uint_as_float((uint32_t)(127 - up) << 23);
+  return __uint_as_float((uint32_t)(127 + up) << 23);
+}
+
 template <int FMT>
 __device__ __forceinline__ constexpr float top_code() { return FMT == FMT_INT8 ? 127.0f : 448.0f; }
 

@@ -72,7 +72,7 @@ __device__ __forceinline__ void rescale_rows(uint32_t o_taddr, float alpha) {
 // 886 -> 874.  The second half by its sum as well, with a barrier for the first half's P V: 7842, 5283, 888.)
 // GEN: tiles with masked columns (columns >= vis; vis <= 0: all) and the first tile of a block; the tiles between
 // run straight-line code (the branches around the masks cost 300 of 1240 cycles).
-// Hooks: on_read() - all logits are in registers; before_p() - called before the accumulator is touched and before
+// Hooks: on_read() - all logits are in registers; scale_keys() - factors of their columns; before_p() - called before the accumulator is touched and before
 // probabilities are stored at p_taddr (64 columns); on_half(), on_full() - keys 0..63 / all keys of P are in TMEM.
 template <int D, bool GEN, class Hooks>
 __device__ __forceinline__ void softmax_tile(uint32_t s_taddr, uint32_t p_taddr, uint32_t o_taddr, int vis, bool first_tile,
@@ -87,6 +87,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_taddr, uint32_t p_taddr,
   tmem_wait_ld();
   loaded(c0); loaded(c1); loaded(c2); loaded(c3);
   hk.on_read();
+  hk.scale_keys(c0, c1, c2, c3);
   if (GEN) { mask32(c0, 0, vis); mask32(c1, 32, vis); mask32(c2, 64, vis); mask32(c3, 96, vis); }
   auto first_half = [&]() {
     const uint64_t negm2 = dup2(st.m == -INFINITY ? 0.0f : -st.m);  // nothing visible so far: exp2(-inf) = 0

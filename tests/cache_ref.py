@@ -38,13 +38,16 @@ def to_bf16(x):
 
 
 def rotate(q, pos, theta):
-    """q [B,w,H,d] float64 at positions pos [B,w] -> rounded to bf16"""
-    d = q.shape[-1]
+    """q [B,w,H,d] float64 at positions pos [B,w] < 2^15 -> rotated in fp32 with fp32 angles, rounded to bf16.  The operations are torch's own
+    on the GPU, whose pow, cos and sin of fp32 numbers are the ones that the definition means; test_rotation has it against 64 bits."""
     if theta == 0:
         return q
-    a = (pos[..., None] * theta ** (-2.0 * np.arange(d // 2) / d))[:, :, None]
-    x, y = q[..., :d // 2], q[..., d // 2:]
-    return to_bf16(np.concatenate([x * np.cos(a) - y * np.sin(a), y * np.cos(a) + x * np.sin(a)], -1)).astype(np.float64)
+    d, f32 = q.shape[-1], torch.float32
+    t = torch.arange(d // 2, device="cuda", dtype=f32)
+    a = torch.tensor(pos, device="cuda", dtype=f32).unsqueeze(-1) * torch.pow(torch.tensor(theta, device="cuda", dtype=f32), -2.0 * t / d)
+    c, s = torch.cos(a).unsqueeze(2), torch.sin(a).unsqueeze(2)
+    x, y = torch.from_numpy(q).to("cuda", f32).split(d // 2, -1)
+    return f64(torch.cat([x * c - y * s, y * c + x * s], -1).to(torch.bfloat16))
 
 
 def attention(q, pos, theta, scale, prefix, n_prefix, own, lens, kw, vw):

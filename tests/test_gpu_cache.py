@@ -258,6 +258,29 @@ def test_values_that_are_not_finite_reach_their_rows(fmt, B):
     assert np.isfinite(out[:, :, :2]).all() and np.isnan(out[:, :, 2:, 5]).all()
 
 
+@pytest.mark.parametrize("d,theta", [(64, 1.0e4), (128, 5.0e5)])
+@pytest.mark.parametrize("pos", [0, 1, 4095, 8191, 32766, 32767, 32768, 1000000, 2 ** 30])
+def test_rotation(d, theta, pos):
+    """The rotated queries themselves: sequence t sees a key that is the t-th unit vector (value 1) and a zero key, so that its lse is
+    log(1 + exp(q_t)).  Below 2^15 the fp32 angle is off by at most 2^-22 of itself, above by nothing; fp32 products and sums take 2^-21.  q_t is the
+    bf16 number nearest to something in that interval, and is read out of the lse, whose slope is sigmoid(q_t) >= 0.01, to 100 * 2^-20."""
+    q = _normal(75, 1, 2, 1, d)
+    k = torch.zeros(d, 1, 2, d, dtype=torch.bfloat16)
+    k[torch.arange(d), 0, 0, torch.arange(d)] = 1.0
+    cache = {"format": "bf16", "k": k.cuda(), "v": torch.zeros_like(k).cuda()}
+    lse = pc.cache_attn(q.cuda().expand(d, 2, 1, d), own=cache, q_pos0=5, q_pos=torch.full((d,), pos - 5, dtype=torch.int32, device="cuda"),
+                        rope_theta=theta, softmax_scale=1.0, want_lse=True)["lse"].cpu().numpy().astype(np.float64)
+    got = np.log(np.expm1(lse))[:, 0].T                                   # [w, d]
+    x, y = ref.f64(q)[0, :, 0, :d // 2], ref.f64(q)[0, :, 0, d // 2:]
+    a = (pos + np.arange(2))[:, None] * float(theta) ** (-2.0 * np.arange(d // 2) / d)
+    want = np.concatenate([x * np.cos(a) - y * np.sin(a), y * np.cos(a) + x * np.sin(a)], -1)
+    size = np.hypot(x, y)
+    size = np.concatenate([size, size], -1)
+    off = np.where(pos + np.arange(2) < 2 ** 15, 2.0 ** -22, 0.0)[:, None] * np.concatenate([a, a], -1)
+    low, high = (ref.to_bf16(want + sign * size * (off + 2.0 ** -21)) for sign in (-1, 1))
+    assert (got >= low - 100 * 2.0 ** -20).all() and (got <= high + 100 * 2.0 ** -20).all()
+
+
 def test_queries_of_any_size():
     """Queries become halves times a power of two of their row: very large and very small rows keep their bits."""
     for up in (2.0 ** -60, 1.0, 2.0 ** 30):
