@@ -468,7 +468,7 @@ PC_API int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0
  */
 typedef struct {
   int32_t B, w, Hq, Hkv, d;
-  int32_t n_prefix, n_own, q_pos0;
+  int32_t n_prefix, n_own, q_pos0, clear_status; /* clear_status: the status word is set to 0 first */
   float rope_theta, softmax_scale;               /* softmax_scale 0 -> 1/sqrt(d) */
   const void* q;
   int64_t q_stride[3];

@@ -119,20 +119,29 @@ def load_library():
     return lib
 
 
+def _host_module():
+    """csrc/pc_host.cpp as it was built for this torch and this Python."""
+    from .build import host_path
+    path = host_path(torch.__version__)
+    try:
+        spec = importlib.util.spec_from_file_location(__package__ + "._pc_host", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+    except ImportError as e:
+        raise PcError("%s cannot be loaded: build it with `python -m paper_2502_14317_b200.build` (%s)" % (path, e)) from e
+    return module
+
+
+def _address(f):
+    return ctypes.cast(f, c_void_p).value
+
+
 def _host_hot_path(lib):
     """hot_path of csrc/pc_host.cpp on this library's entry points."""
     call = getattr(lib, "_host_hot_path", None)
     if call is None:
-        from .build import host_path
-        path = host_path(torch.__version__)
-        try:
-            spec = importlib.util.spec_from_file_location(__package__ + "._pc_host", path)
-            module = importlib.util.module_from_spec(spec)
-            spec.loader.exec_module(module)
-        except ImportError as e:
-            raise PcError("%s cannot be loaded: build it with `python -m paper_2502_14317_b200.build` (%s)" % (path, e)) from e
-        address = lambda f: ctypes.cast(f, c_void_p).value
-        call = lib._host_hot_path = functools.partial(module.hot_path, address(lib.pc_hot_path_workspace_bytes), address(lib.pc_hot_path))
+        module = _host_module()
+        call = lib._host_hot_path = functools.partial(module.hot_path, _address(lib.pc_hot_path_workspace_bytes), _address(lib.pc_hot_path))
     return call
 
 
@@ -742,39 +751,34 @@ def hot_path_from_host(hq, hk, hv, *, w, rope_theta, m, k_keep, softmax_scale=0.
 
 
 # ------------------------------------------------------------------------------------ 8-bit caches, attention over shared and own caches
-class _KvCache(Structure):
+class _KvCache(Structure):                                 # pc_kv_cache for gather_kv_quantize; the calls beside it fill it in csrc/pc_host.cpp
     _fields_ = [("format", c_int32), ("B", c_int32), ("Hkv", c_int32), ("d", c_int32), ("capacity", c_int64), ("k", c_void_p), ("v", c_void_p),
                 ("k_scale", c_void_p), ("v_scale", c_void_p)]
 
 
-class _CacheAttnArgs(Structure):
-    _fields_ = [(n, c_int32) for n in ("B", "w", "Hq", "Hkv", "d", "n_prefix", "n_own", "q_pos0")] + \
-               [("rope_theta", c_float), ("softmax_scale", c_float), ("q", c_void_p), ("q_stride", c_int64 * 3), ("k_win", c_void_p),
-                ("v_win", c_void_p), ("k_win_stride", c_int64 * 3), ("v_win_stride", c_int64 * 3), ("q_pos", c_void_p), ("own_len", c_void_p),
-                ("prefix", POINTER(_KvCache)), ("own", POINTER(_KvCache)), ("out", c_void_p), ("lse", c_void_p), ("status_word", c_void_p),
-                ("workspace", c_void_p), ("workspace_bytes", c_size_t)]
-
-
+_ALL = -2 ** 63                                           # as many entries as a cache holds
 _FORMATS = {"bf16": (0, torch.bfloat16), "int8": (1, torch.int8), "e4m3": (2, torch.float8_e4m3fn)}
 
 
-def _cache_lib():
-    """The library with the argument types of the calls below."""
-    lib = load_library()
-    if not getattr(lib, "_cache_calls", False):
-        lib.pc_kv_quantize.restype = c_int32
-        lib.pc_kv_quantize.argtypes = [POINTER(_KvCache), c_void_p, POINTER(c_int64), c_void_p, POINTER(c_int64), c_int32, c_int32] + [c_void_p] * 3
-        lib.pc_gather_kv_quantize.restype = c_int32
-        lib.pc_gather_kv_quantize.argtypes = [c_void_p, c_void_p, POINTER(c_int64), c_void_p, c_void_p, c_int32, c_int32, POINTER(_KvCache),
-                                              c_void_p, c_void_p]
-        lib.pc_kv_dequantize.restype = c_int32
-        lib.pc_kv_dequantize.argtypes = [POINTER(_KvCache), c_int32, c_int32] + [c_void_p] * 4
-        lib.pc_cache_attn_workspace_bytes.restype = c_size_t
-        lib.pc_cache_attn_workspace_bytes.argtypes = [POINTER(_CacheAttnArgs)]
-        lib.pc_cache_attn.restype = c_int32
-        lib.pc_cache_attn.argtypes = [POINTER(_CacheAttnArgs), c_void_p]
-        lib._cache_calls = True
-    return lib
+class _CacheCalls:
+    """The calls below on a library's entry points, those that csrc/pc_host.cpp makes with their addresses."""
+
+    def __init__(self, lib):
+        host = _host_module()
+        self.quantize = functools.partial(host.kv_quantize, _address(lib.pc_kv_quantize))
+        self.dequantize = functools.partial(host.kv_dequantize, _address(lib.pc_kv_dequantize))
+        self.attn = functools.partial(host.cache_attn, _address(lib.pc_cache_attn_workspace_bytes), _address(lib.pc_cache_attn))
+        self.gather = lib.pc_gather_kv_quantize
+        self.gather.restype = c_int32
+        self.gather.argtypes = [c_void_p, c_void_p, POINTER(c_int64), c_void_p, c_void_p, c_int32, c_int32, POINTER(_KvCache), c_void_p, c_void_p]
+
+
+def _cache_calls():
+    lib = _LIB or load_library()
+    calls = getattr(lib, "_cache_calls", None)
+    if calls is None:
+        calls = lib._cache_calls = _CacheCalls(lib)
+    return calls
 
 
 def kv_cache(B, Hkv, capacity, d, format, device="cuda"):
@@ -787,95 +791,60 @@ def kv_cache(B, Hkv, capacity, d, format, device="cuda"):
     return {"format": format, "k": k, "v": v, "k_scale": ks, "v_scale": vs}
 
 
-def _kv_desc(cache, dev):
-    """pc_kv_cache of a cache's tensors."""
-    if cache["format"] not in _FORMATS:
-        raise PcError("format must be one of %s" % ", ".join(_FORMATS))
-    number, dtype = _FORMATS[cache["format"]]
-    k, v, ks, vs = cache["k"], cache["v"], cache.get("k_scale"), cache.get("v_scale")
-    if k.dim() != 4 or k.shape != v.shape or not (k.dtype is v.dtype is dtype) or not (k.is_contiguous() and v.is_contiguous()) or \
-            not (k.device == v.device == dev):
-        raise PcError("k and v of a cache must be contiguous [B, Hkv, capacity, d] of its format, on the device of the call's tensors")
-    if number and not all(t is not None and t.shape == k.shape[:3] and t.dtype is torch.float32 and t.is_contiguous() and t.device == dev
-                          for t in (ks, vs)):
-        raise PcError("k_scale and v_scale of a cache must be contiguous float32 [B, Hkv, capacity]")
-    B, Hkv, cap, d = k.shape
-    return _KvCache(number, B, Hkv, d, cap, k.data_ptr(), v.data_ptr(), ks.data_ptr() if number else None, vs.data_ptr() if number else None)
-
-
-def _per_sequence(t, B, dev, name):
-    if t is not None and (t.dtype is not torch.int32 or t.shape != (B,) or not t.is_contiguous() or t.device != dev):
-        raise PcError("%s must be a contiguous int32 tensor with one entry per sequence" % name)
-    return _ptr(t)
-
-
-def _source(t, shape, dev, name):
-    """Strides of bf16 rows [B,n,H,d] with a contiguous head dimension."""
-    s = t.stride()
-    if t.shape != shape or t.dtype is not torch.bfloat16 or t.device != dev or s[3] != 1:
-        raise PcError("%s must be bfloat16 %s with a contiguous head dimension" % (name, list(shape)))
-    return s[:3]
-
-
 def kv_quantize(cache, k, v, *, at=0, status=None):
     """pc_kv_quantize: writes k, v [B,n,Hkv,d] bf16 to entries at .. at + n - 1 of an 8-bit cache; at: an int, or an int32
     tensor [B] for sequences of different lengths (entries behind the capacity are then left out and ``status`` says so)."""
-    lib = _cache_lib()
-    _need_cuda(k, v)
-    desc = _kv_desc(cache, k.device)
-    B, n, Hkv, d = k.shape
-    if (B, Hkv, d) != (desc.B, desc.Hkv, desc.d):
-        raise PcError("k and v must be [B, n, Hkv, d] with the B, Hkv and d of the cache")
-    sk, sv = _Strides(*_source(k, k.shape, k.device, "k")), _Strides(*_source(v, k.shape, k.device, "v"))
-    first, each = (0, _per_sequence(at, B, k.device, "at")) if torch.is_tensor(at) else (int(at), None)
-    _check(lib.pc_kv_quantize(ctypes.byref(desc), k.data_ptr(), sk, v.data_ptr(), sv, n, first, each, _ptr(status), _stream()), "pc_kv_quantize")
+    rc = _cache_calls().quantize(_stream(), True, cache, k, v, at, status)
+    if rc != 0:
+        _refused(rc, "pc_kv_quantize")
     return cache
+
+
+def _refused(rc, what):
+    if isinstance(rc, str):
+        raise PcError(rc)
+    _check(rc, what)
 
 
 def gather_kv_quantize(k_src, v_src, kept, idx, cache=None, *, format="int8", pos_out=None, want_pos=False):
     """pc_gather_kv_quantize: as gather_kv, into an 8-bit cache of one sequence (made here if none is given).
 
     Returns (cache, pos [Hkv, m*k] or None)."""
-    lib = _cache_lib()
+    calls = _cache_calls()
     _need_cuda(k_src, v_src, kept, idx)
     C, L, Hkv, d = k_src.shape
     m, _, k = idx.shape
     dev = k_src.device
     if not _same_rows(k_src, v_src) or not (k_src.dtype is v_src.dtype is torch.bfloat16) or v_src.shape != k_src.shape or v_src.device != dev:
         raise PcError("k_src and v_src must be bfloat16 and share strides with a contiguous head dimension")
-    if idx.shape[1] != Hkv or kept.shape != (m,) or not (idx.dtype is kept.dtype is torch.int32 and idx.is_contiguous() and kept.is_contiguous()):
+    if idx.shape[1] != Hkv or kept.shape != (m,) or not (idx.dtype is kept.dtype is torch.int32 and idx.is_contiguous() and kept.is_contiguous()
+                                                         and idx.device == kept.device == dev):
         raise PcError("idx must be contiguous int32 [m, Hkv, k], kept contiguous int32 [m]")
     if cache is None:
         cache = kv_cache(1, Hkv, m * k, d, format, dev)
-    desc = _kv_desc(cache, dev)
-    if (desc.B, desc.Hkv, desc.d) != (1, Hkv, d) or desc.capacity < m * k:
-        raise PcError("the cache must hold m * k entries of one sequence, with the Hkv and d of k_src")
+    number, dtype = _FORMATS.get(cache["format"], (0, None))
+    kc, scales = cache["k"], (cache.get("k_scale"), cache.get("v_scale"))
+    if number == 0 or kc.dim() != 4 or kc.shape[:2] != (1, Hkv) or kc.shape[2] < m * k or kc.shape[3] != d or \
+            not all(t.shape == kc.shape and t.dtype is dtype and t.is_contiguous() and t.device == dev for t in (kc, cache["v"])) or \
+            not all(t is not None and t.shape == kc.shape[:3] and t.dtype is torch.float32 and t.is_contiguous() and t.device == dev for t in scales):
+        raise PcError("the cache must be an 8-bit one that holds m * k entries of one sequence, with the Hkv and d of k_src")
     if pos_out is None and want_pos:
         pos_out = torch.empty((Hkv, m * k), dtype=torch.int32, device=dev)
     if pos_out is not None and (pos_out.shape != (Hkv, m * k) or pos_out.dtype is not torch.int32 or not pos_out.is_contiguous() or
                                 pos_out.device != dev):
         raise PcError("pos_out must be contiguous int32 [Hkv, m*k]")
-    _check(lib.pc_gather_kv_quantize(k_src.data_ptr(), v_src.data_ptr(), _Strides(*k_src.stride()[:3]), kept.data_ptr(), idx.data_ptr(), m, k,
-                                     ctypes.byref(desc), _ptr(pos_out), _stream()), "pc_gather_kv_quantize")
+    desc = _KvCache(number, 1, Hkv, d, kc.shape[2], kc.data_ptr(), cache["v"].data_ptr(), scales[0].data_ptr(), scales[1].data_ptr())
+    _check(calls.gather(k_src.data_ptr(), v_src.data_ptr(), _Strides(*k_src.stride()[:3]), kept.data_ptr(), idx.data_ptr(), m, k,
+                        ctypes.byref(desc), _ptr(pos_out), _stream()), "pc_gather_kv_quantize")
     return cache, pos_out
 
 
 def kv_dequantize(cache, n=None, *, at=0, k_out=None, v_out=None):
     """pc_kv_dequantize: entries at .. at + n - 1 (n: the capacity) of an 8-bit cache as bf16 [B,Hkv,n,d]; at as in kv_quantize."""
-    lib = _cache_lib()
-    dev = cache["k"].device
-    _need_cuda(cache["k"])
-    desc = _kv_desc(cache, dev)
-    n = desc.capacity if n is None else int(n)
-    first, each = (0, _per_sequence(at, desc.B, dev, "at")) if torch.is_tensor(at) else (int(at), None)
-    shape = (desc.B, desc.Hkv, n, desc.d)
-    k_out = torch.empty(shape, dtype=torch.bfloat16, device=dev) if k_out is None else k_out
-    v_out = torch.empty(shape, dtype=torch.bfloat16, device=dev) if v_out is None else v_out
-    for t in (k_out, v_out):
-        if t.shape != shape or t.dtype is not torch.bfloat16 or not t.is_contiguous() or t.device != dev:
-            raise PcError("k_out and v_out must be contiguous bfloat16 [B, Hkv, n, d]")
-    _check(lib.pc_kv_dequantize(ctypes.byref(desc), n, first, each, k_out.data_ptr(), v_out.data_ptr(), _stream()), "pc_kv_dequantize")
-    return k_out, v_out
+    got = _cache_calls().dequantize(_stream(), True, cache, n, at, k_out, v_out)
+    if got[0] != 0:
+        _refused(got if isinstance(got, str) else got[0], "pc_kv_dequantize")
+    return got[1], got[2]
 
 
 def cache_attn(q, k_win=None, v_win=None, *, prefix=None, n_prefix=None, own=None, n_own=None, own_len=None, q_pos0=0, q_pos=None,
@@ -886,57 +855,8 @@ def cache_attn(q, k_win=None, v_win=None, *, prefix=None, n_prefix=None, own=Non
     n_prefix, n_own: valid entries (the capacities); own_len: int32 [B], entries of each sequence; positions of the queries:
     q_pos0 + q_pos[b] + i.  ``buffers`` (dict) keeps out, lse, status and workspace between calls.
     Returns dict(out, lse, status, workspace)."""
-    lib = _cache_lib()
-    _need_cuda(q)
-    dev = q.device
-    B, w, Hq, d = q.shape
-    b = {} if buffers is None else buffers
-    a = _CacheAttnArgs(B=B, w=w, Hq=Hq, d=d, q_pos0=int(q_pos0), rope_theta=float(rope_theta), softmax_scale=float(softmax_scale),
-                       q=q.data_ptr())
-    a.q_stride[:] = _source(q, q.shape, dev, "q")
-    Hkv = 0
-    for name, cache, n in (("prefix", prefix, n_prefix), ("own", own, n_own)):
-        if cache is None:
-            if n:
-                raise PcError("n_%s without a cache" % name)
-            continue
-        desc = _kv_desc(cache, dev)
-        Hkv = Hkv or desc.Hkv
-        setattr(a, name, ctypes.pointer(desc))
-        setattr(a, "n_" + name, desc.capacity if n is None else int(n))
-    if (k_win is None) != (v_win is None):
-        raise PcError("k_win and v_win go together")
-    if k_win is not None:
-        Hkv = Hkv or k_win.shape[2]
-        a.k_win, a.v_win = k_win.data_ptr(), v_win.data_ptr()
-        a.k_win_stride[:] = _source(k_win, (B, w, Hkv, d), dev, "k_win")
-        a.v_win_stride[:] = _source(v_win, (B, w, Hkv, d), dev, "v_win")
-    a.Hkv = Hkv
-    a.q_pos, a.own_len = _per_sequence(q_pos, B, dev, "q_pos"), _per_sequence(own_len, B, dev, "own_len")
-    f32, i32 = torch.float32, torch.int32
-    out = _kept(b, "out", (B, w, Hq, d), torch.bfloat16, dev) if out is None else out
-    out = torch.empty((B, w, Hq, d), dtype=torch.bfloat16, device=dev) if out is None else out
-    if lse_out is None and want_lse:
-        lse_out = _kept(b, "lse", (B, Hq, w), f32, dev)
-        lse_out = torch.empty((B, Hq, w), dtype=f32, device=dev) if lse_out is None else lse_out
-    if out.shape != (B, w, Hq, d) or out.dtype is not torch.bfloat16 or not out.is_contiguous() or out.device != dev:
-        raise PcError("out must be contiguous bfloat16 [B, w, Hq, d]")
-    if lse_out is not None and (lse_out.shape != (B, Hq, w) or lse_out.dtype is not f32 or not lse_out.is_contiguous() or lse_out.device != dev):
-        raise PcError("lse_out must be contiguous float32 [B, Hq, w]")
-    if status is None:
-        status = _kept(b, "status", (1,), i32, dev)
-        status = torch.zeros(1, dtype=i32, device=dev) if status is None else status
-    need = int(lib.pc_cache_attn_workspace_bytes(ctypes.byref(a)))
-    if workspace is None:
-        workspace = b.get("workspace")
-    if workspace is None or workspace.numel() < need or workspace.device != dev:
-        _let_go(workspace)
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
-    a.out, a.lse, a.status_word = out.data_ptr(), _ptr(lse_out), status.data_ptr()
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _check(lib.pc_cache_attn(ctypes.byref(a), _stream()), "pc_cache_attn")
-    if buffers is not None:
-        buffers.update(out=out, status=status, workspace=workspace)
-        if lse_out is not None:
-            buffers["lse"] = lse_out
-    return {"out": out, "lse": lse_out, "status": status, "workspace": workspace}
+    got = _cache_calls().attn(_stream(), True, q, k_win, v_win, prefix, own, own_len, q_pos, (out, lse_out, status, workspace), buffers,
+                              _ALL if n_prefix is None else n_prefix, _ALL if n_own is None else n_own, q_pos0, want_lse, rope_theta, softmax_scale)
+    if got[0] != 0:
+        _refused(got if isinstance(got, str) else got[0], "pc_cache_attn")
+    return got[1]

@@ -44,7 +44,7 @@ struct CacheRows {
   float theta, scale_log2;
   void *rows, *halves;
   float* half_scale;             // [Hkv,total_rows]
-  int* clear;                    // a word that is set to 0, or null
+  int *clear, *clear_too;        // words that are set to 0, or null
 };
 cudaError_t launch_cache_rows(const CacheRows& p, int d, cudaStream_t st);
 

@@ -222,6 +222,7 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
   const float scale_log2 = (float)(scale * 1.4426950408889634);
   rows.theta = a->rope_theta; rows.scale_log2 = scale_log2; rows.rows = ws + plan.off_rows;
   rows.clear = reinterpret_cast<int*>(ws + plan.off_counter);
+  rows.clear_too = a->clear_status ? a->status_word : nullptr;
   if (plan.halves) { rows.halves = ws + plan.off_halves; rows.half_scale = reinterpret_cast<float*>(ws + plan.off_scale); }
   cudaError_t e = pc::launch_cache_rows(rows, a->d, st);
   int slot = 0;

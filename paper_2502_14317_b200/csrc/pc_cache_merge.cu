@@ -23,7 +23,10 @@ __global__ void __launch_bounds__(256) cache_rows_kernel(const CacheRows p) {
 #pragma unroll
   for (int e = 0; e < E; ++e) freq[e] = turn ? powf(p.theta, -2.0f * (float)(E * lane + e) / (float)D) : 0.0f;
   chain();
-  if (p.clear != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *p.clear = 0;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (p.clear != nullptr) *p.clear = 0;
+    if (p.clear_too != nullptr) *p.clear_too = 0;
+  }
   const long long pos = (long long)p.pos0 + (p.pos ? p.pos[b] : 0) + i;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
