@@ -34,16 +34,18 @@ struct KvRead {
 };
 cudaError_t launch_kv_dequantize(const KvRead& r, int format, int d, int sm_count, cudaStream_t st);
 
-// Queries of pc_cache_attn as rows: rows[hkv][(b * w + i) * G + g][d], rotated and rounded to bf16 (theta 0: as they are); halves
-// (or null): the same times a power of two of each row, as numbers of half precision, and its inverse times scale_log2 in half_scale.
+// Queries of pc_cache_attn as rows of a kv-head: row (b * w + i) * G + g is q[b, i, hkv * G + g, :], rotated and rounded to bf16
+// (theta 0: as it is), in memory as rows[hkv][row][d].  The kernel for few rows makes them where it needs them and leaves them
+// there for those behind it; ahead of the one for many rows a launch of its own does, and, for 8-bit codes, leaves halves: the same times a power of
+// two of each row as numbers of half precision, whose inverse times scale_log2 is in half_scale.
 struct CacheRows {
   const void* q;
   long long stride[3];
   int B, w, Hq, Hkv, pos0;
   const int* pos;
   float theta, scale_log2;
-  void *rows, *halves;
-  float* half_scale;             // [Hkv,total_rows]
+  void *rows, *halves;           // halves: or null
+  float* half_scale;             // [Hkv,B*w*G]
   int *clear, *clear_too;        // words that are set to 0, or null
 };
 cudaError_t launch_cache_rows(const CacheRows& p, int d, cudaStream_t st);
@@ -57,8 +59,8 @@ struct CachePhase {
   const float *k_scale, *v_scale;                // [seqs,Hkv,capacity] (8-bit formats)
   long long capacity;
   int n_rg, n_split, slot0, n_slots, total_rows; // row groups of a sequence, key splits; total_rows = rows of a kv-head over all sequences
-  float scale_log2;
-  const __nv_bfloat16* q_rows;                   // [Hkv,total_rows,d]
+  CacheRows q;
+  int rows_made;                                 // 1: the rows are in memory; 0: this launch makes them
   float* part_o;                                 // [Hkv,total_rows,n_slots,d]
   float2* part_ml;                               // [Hkv,total_rows,n_slots]
   int* status;
@@ -84,13 +86,12 @@ cudaError_t launch_cache_wide(const CUtensorMap* maps, const WidePhase& p, int f
 
 // Joins the slots of a row and the new tokens' own keys.
 struct CacheMerge {
-  int B, w, Hq, Hkv, n_slots, total_rows;
+  int n_slots, total_rows;
   const float* part_o;
   const float2* part_ml;
-  const __nv_bfloat16* q_rows;
+  CacheRows q;                                   // (rows in memory)
   const void *k_win, *v_win;                     // or null
   long long k_stride[3], v_stride[3];
-  float scale_log2;
   __nv_bfloat16* out;
   float* lse;
 };

@@ -99,7 +99,7 @@ struct CachePlan {
   PhasePlan prefix, own;
   int n_slots;
   int64_t total_rows;
-  bool halves;                                   // the rows as halves as well (a wide phase over 8-bit codes)
+  bool rows, halves;                             // a launch for the rows (for a wide phase, or no phase at all), as halves as well (over 8-bit codes)
   size_t off_counter, off_rows, off_halves, off_scale, off_ml, off_o, total;
 };
 
@@ -148,7 +148,7 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
   p.total_rows = (int64_t)a->B * a->w * G;
   p.n_slots = 0;
   p.prefix = p.own = {};
-  p.halves = false;
+  p.rows = p.halves = false;
   for (int own = 0; own <= 1; ++own) {
     const pc_kv_cache* const c = own ? a->own : a->prefix;
     const int n = own ? a->n_own : a->n_prefix;
@@ -158,12 +158,14 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     PhasePlan& ph = own ? p.own : p.prefix;
     if (!own && p.total_rows > 32) {
       ph = wide_plan(p.total_rows, a->Hkv, a->d, c->format, n, sm_count);
+      p.rows = true;
       p.halves = c->format != PC_KV_BF16;
     } else
     ph = few_plan(own ? a->B : 1, own ? (int64_t)a->w * G : p.total_rows, a->Hkv, a->d, c->format, n, sm_count);
     if ((own ? a->B : 1ll) * a->Hkv * ph.n_rg * ph.n_split > 0x7FFFFFFF) return PC_ERR_UNSUPPORTED;
     p.n_slots += ph.n_split;
   }
+  if (p.n_slots == 0) p.rows = true;
   size_t off = 0;
   p.off_counter = off; off += ALIGN;
   p.off_halves = off; off += p.halves ? align_up((size_t)p.total_rows * a->Hkv * a->d * 2) : 0;
@@ -220,11 +222,17 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
   rows.q = a->q; rows.B = a->B; rows.w = a->w; rows.Hq = a->Hq; rows.Hkv = a->Hkv; rows.pos0 = a->q_pos0; rows.pos = a->q_pos;
   const double scale = a->softmax_scale > 0.0f ? (double)a->softmax_scale : 1.0 / std::sqrt((double)a->d);
   const float scale_log2 = (float)(scale * 1.4426950408889634);
-  rows.theta = a->rope_theta; rows.scale_log2 = scale_log2; rows.rows = ws + plan.off_rows;
-  rows.clear = reinterpret_cast<int*>(ws + plan.off_counter);
-  rows.clear_too = a->clear_status ? a->status_word : nullptr;
-  if (plan.halves) { rows.halves = ws + plan.off_halves; rows.half_scale = reinterpret_cast<float*>(ws + plan.off_scale); }
-  cudaError_t e = pc::launch_cache_rows(rows, a->d, st);
+  rows.theta = a->rope_theta; rows.scale_log2 = scale_log2;
+  cudaError_t e = cudaSuccess;
+  rows.rows = ws + plan.off_rows;
+  if (plan.rows) {
+    rows.clear = reinterpret_cast<int*>(ws + plan.off_counter);
+    rows.clear_too = a->clear_status ? a->status_word : nullptr;
+    if (plan.halves) { rows.halves = ws + plan.off_halves; rows.half_scale = reinterpret_cast<float*>(ws + plan.off_scale); }
+    e = pc::launch_cache_rows(rows, a->d, st);
+  } else if (a->clear_status && a->status_word) {
+    e = cudaMemsetAsync(a->status_word, 0, sizeof(int), st);
+  }
   int slot = 0;
   for (int own = 0; own <= 1 && e == cudaSuccess; ++own) {
     const pc_kv_cache* const c = own ? a->own : a->prefix;
@@ -237,8 +245,8 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
     p.Hkv = a->Hkv; p.n_keys = n; p.len = own ? a->own_len : nullptr;
     p.k_scale = c->k_scale; p.v_scale = c->v_scale; p.capacity = c->capacity;
     p.n_rg = ph.n_rg; p.n_split = ph.n_split; p.slot0 = slot; p.n_slots = plan.n_slots; p.total_rows = (int)plan.total_rows;
-    p.scale_log2 = scale_log2;
-    p.q_rows = reinterpret_cast<const __nv_bfloat16*>(ws + plan.off_rows);
+    p.q = rows;
+    p.rows_made = plan.rows || slot > 0;
     p.part_o = reinterpret_cast<float*>(ws + plan.off_o);
     p.part_ml = reinterpret_cast<float2*>(ws + plan.off_ml);
     p.status = a->status_word;
@@ -266,11 +274,11 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
     slot += ph.n_split;
   }
   if (e != cudaSuccess) return launched(e);
-  merge.B = a->B; merge.w = a->w; merge.Hq = a->Hq; merge.Hkv = a->Hkv; merge.n_slots = plan.n_slots; merge.total_rows = (int)plan.total_rows;
+  merge.n_slots = plan.n_slots; merge.total_rows = (int)plan.total_rows;
   merge.part_o = reinterpret_cast<const float*>(ws + plan.off_o);
   merge.part_ml = reinterpret_cast<const float2*>(ws + plan.off_ml);
-  merge.q_rows = reinterpret_cast<const __nv_bfloat16*>(ws + plan.off_rows);
-  merge.k_win = a->k_win; merge.v_win = a->v_win; merge.scale_log2 = scale_log2;
+  merge.q = rows;
+  merge.k_win = a->k_win; merge.v_win = a->v_win;
   merge.out = static_cast<__nv_bfloat16*>(a->out); merge.lse = a->lse;
   return launched(pc::launch_cache_merge(merge, a->d, st));
 }

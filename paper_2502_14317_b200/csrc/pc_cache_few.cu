@@ -14,7 +14,7 @@
 // Bound by reading the cache.  A warp takes 16 keys at a time on its own, with its own maximum, sum and accumulators, and waits for
 // nobody but the copies; a producer warp keeps the ring full.  The maximum is looked at with one vote per 8 rows and raised
 // only where a logit exceeds it by 2^8.  The warps' results are added in shared memory, the splits' by the merge kernel.
-#include "pc_cache.h"
+#include "pc_cache_rows.cuh"
 #include "pc_kernels.h"
 #include "pc_kv8.cuh"
 #include "pc_sm100.cuh"
@@ -121,6 +121,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
   }
+  RowTurner<D> turner(prm.rows_made ? 0.0f : prm.q.theta, lane);
   __syncthreads();
   chain();
   int n = prm.n_keys;                                            // entries of this sequence
@@ -129,11 +130,6 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   const int j0 = (int)((long long)n_all * split / prm.n_split), nt = (int)((long long)n_all * (split + 1) / prm.n_split) - j0;
   const int row0 = seq * prm.rows + rg * N, n_rows = prm.rows - rg * N < N ? prm.rows - rg * N : N;      // rows of the kv-head
   const size_t part0 = ((size_t)hkv * prm.total_rows + row0) * prm.n_slots + prm.slot0 + split;
-
-  if (nt == 0) {                                                 // nothing for this split: the merge leaves it out
-    if (tid < n_rows) prm.part_ml[part0 + (size_t)tid * prm.n_slots] = make_float2(-INFINITY, 0.0f);
-    return;
-  }
 
   // copies of tile i into its stage; the whole producer warp calls
   auto load = [&](int i) {
@@ -162,30 +158,38 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 
   if (warp == C::WARPS) {
     for (int i = 0; i < NS && i < nt; ++i) load(i);
-  } else {
+  } else if (nt > 0 || (split == 0 && !prm.rows_made)) {
     // ---- the rows' queries as operands, in the order in which the threads hold their keys
     for (int r = warp; r < N; r += C::WARPS) {
-      uint2 q = make_uint2(0, 0);
-      if (r < n_rows && lane < D / 4) q = __ldg(reinterpret_cast<const uint2*>(prm.q_rows + ((size_t)hkv * prm.total_rows + row0 + r) * D) + lane);
-      float qs = prm.scale_log2;
-      if constexpr (Q8) {
-        uint32_t m = __vmaxu2(q.x & 0x7FFF7FFFu, q.y & 0x7FFF7FFFu);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) m = __vmaxu2(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
-        float inv;
-        const float f = row_factor(max(m & 0xFFFFu, m >> 16), inv);
-        qs *= inv;
-        const float a = __uint_as_float(q.x << 16), b = __uint_as_float(q.x & 0xFFFF0000u), c = __uint_as_float(q.y << 16),
-                    d = __uint_as_float(q.y & 0xFFFF0000u);
-        q = make_uint2(pack_p<FMT>(a * f, b * f), pack_p<FMT>(c * f, d * f));
+      constexpr int E = D / 32;
+      uint32_t q[E / 2] = {};
+      if (r < n_rows) {
+        turner.row(prm.q, prm.rows_made != 0, hkv, row0 + r, lane, q);
+        if (split == 0 && !prm.rows_made) RowTurner<D>::store(prm.q.rows, (size_t)hkv * prm.total_rows + row0 + r, lane, q);
       }
-      if (lane < D / 4) {
-        const int d = 4 * lane, b = d / C::EPB, in = d % C::EPB, chunk = in / C::EPC, t = in % C::EPC / 4;
+      float qs = prm.q.scale_log2;
+      if constexpr (Q8) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) m = __vmaxu2(m, q[i] & 0x7FFF7FFFu);
+        float inv;
+        const float f = row_factor(__reduce_max_sync(0xFFFFFFFFu, max(m & 0xFFFFu, m >> 16)), inv);
+        qs *= inv;
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) q[i] = pack_p<FMT>(__uint_as_float(q[i] << 16) * f, __uint_as_float(q[i] & 0xFFFF0000u) * f);
+      }
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) {
+        const int d = E * lane + 2 * i, b = d / C::EPB, in = d % C::EPB, chunk = in / C::EPC, t = in % C::EPC / 4;
         const int ks = (b * C::CPT + chunk % C::CPT) * C::KPC + t, a = chunk / C::CPT;
-        reinterpret_cast<uint2*>(smem + C::OFF_Q)[(ks * NT8 + r / 8) * 32 + (r % 8) * 4 + a] = q;
+        reinterpret_cast<uint32_t*>(smem + C::OFF_Q)[2 * ((ks * NT8 + r / 8) * 32 + (r % 8) * 4 + a) + (d % 4) / 2] = q[i];
       }
       if (lane == 0) mi.qs[r] = r < n_rows ? qs : 0.0f;
     }
+  }
+  if (nt == 0) {                                                 // nothing for this split: the merge leaves it out
+    if (tid < n_rows) prm.part_ml[part0 + (size_t)tid * prm.n_slots] = make_float2(-INFINITY, 0.0f);
+    return;
   }
   __syncthreads();
 

@@ -105,18 +105,22 @@ struct Converter {
   const WidePhase& prm;
   Extra8& ex;
   uint32_t raw;                                            // this lane's first slot
+  // Row and 16-byte piece of a row of this lane: of the eight lanes that store together at head size 128, four are in the next
+  // row, whose swizzle puts their chunks into the other banks.
+  int lane_row, piece;
   int warp, lane, slot = 0;                                // slot: raw slot of the next half that is converted
   uint32_t k = 0, v = 0, tile = 0;                         // stages used so far; tiles of earlier items
   __device__ __forceinline__ Converter(const Ctx2& c, const WidePhase& p, Extra8& e, uint8_t* raw_smem, int w, int l)
-      : cx(c), prm(p), ex(e), raw(smem_u32(raw_smem) + (w * PIECES * 32 + l) * 16), warp(w), lane(l) {}
+      : cx(c), prm(p), ex(e), raw(smem_u32(raw_smem) + (w * PIECES * 32 + l) * 16), lane_row(D == 128 ? (l >> 4) * 2 + ((l >> 2) & 1) : l / 4),
+        piece(D == 128 ? (l & 3) | ((l >> 1) & 4) : l & 3), warp(w), lane(l) {}
 
   __device__ __forceinline__ void fetch(bool values, int j, int hkv, int s) {
     const uint8_t* const src = (values ? prm.v8 : prm.k8) + ((size_t)hkv * prm.c.capacity + (size_t)j * TILE + warp * 32) * D;
     const int left = prm.c.n_keys - j * TILE - warp * 32;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-      const int row = i * (32 / LPR) + lane / LPR;
-      cp_async16(raw + s * C::RAW_BYTES + i * 512, row < left ? src + (size_t)row * D + (lane % LPR) * 16 : (const void*)(values ? prm.v8 : prm.k8), row < left);
+      const int row = i * (32 / LPR) + lane_row;
+      cp_async16(raw + s * C::RAW_BYTES + i * 512, row < left ? src + (size_t)row * D + piece * 16 : (const void*)(values ? prm.v8 : prm.k8), row < left);
     }
     const float* const sc = (values ? prm.c.v_scale : prm.c.k_scale) + (size_t)hkv * prm.c.capacity;
     cp_async4(smem_u32(&ex.raw_scale[s][warp * 32 + lane]), lane < left ? sc + (size_t)j * TILE + warp * 32 + lane : sc, lane < left);
@@ -140,7 +144,7 @@ struct Converter {
     const uint32_t to = smem_u32(cx.ring) + st * C::STAGE_BYTES;
 #pragma unroll 2
     for (int i = 0; i < PIECES; ++i) {
-      const int row = warp * 32 + i * (32 / LPR) + lane / LPR, c = lane % LPR;      // elements 16 c .. 16 c + 15 of the row
+      const int row = warp * 32 + i * (32 / LPR) + lane_row, c = piece;      // elements 16 c .. 16 c + 15 of the row
       const uint4 x = lds128(raw + slot * C::RAW_BYTES + i * 512);
       uint4 a, b;
       if constexpr (VALUES) {
@@ -464,7 +468,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       if (d.kind == KIND_DONE) break;
       const int n = b ? d.n[1] : d.n[0];
       if (n > 0) {
-        float scale_log2 = prm.c.scale_log2;
+        float scale_log2 = prm.c.q.scale_log2;
         if constexpr (Q8) {
           const int row = first_row(d.h[0], b, 0) + r;
           if (row < rows) scale_log2 = __ldg(prm.half_scale + (size_t)d.hkv * prm.c.total_rows + row);
