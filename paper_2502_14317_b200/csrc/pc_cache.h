@@ -78,10 +78,9 @@ struct WidePhase {
   int alt;                       // 1: the two blocks of a CTA hold the same rows and take alternate key tiles; 0: different rows
   int n_tiles;                   // 128-key tiles
   const float* half_scale;       // [Hkv,total_rows] (8-bit formats)
-  const uint8_t *k8, *v8;        // 8-bit formats: the cache's codes
   int* counter;                  // work queue, zeroed
 };
-// maps: rows of queries (box 64 x 128 rows; halves for 8-bit formats), and for bf16 keys (128, of a pair 64 entries) and values (128)
+// maps: rows of queries (box 64 x 128 rows; halves for 8-bit formats), keys (128, of a pair 64 entries) and values (128)
 cudaError_t launch_cache_wide(const CUtensorMap* maps, const WidePhase& p, int format, int d, bool pair, int sm_count, cudaStream_t st);
 
 // Joins the slots of a row and the new tokens' own keys.

@@ -255,14 +255,13 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
       pc::WidePhase wp = {};
       wp.c = p; wp.alt = ph.alt; wp.n_tiles = (n + 127) / 128;
       wp.half_scale = rows.half_scale;
-      wp.k8 = static_cast<const uint8_t*>(c->k); wp.v8 = static_cast<const uint8_t*>(c->v);
       wp.counter = rows.clear;
       const uint64_t d = (uint64_t)a->d, R = (uint64_t)plan.total_rows;
       const uint64_t dims[4] = {d, R, (uint64_t)a->Hkv, 1}, str[3] = {d, R * d, R * d * (uint64_t)a->Hkv};
       const uint32_t box[4] = {64, 128, 1, 1};
       CUtensorMap maps[3] = {}, unused;
       bool made = pc::make_tmap_bf16_4d(&maps[0], plan.halves ? rows.halves : rows.rows, dims, str, box);
-      if (c->format == PC_KV_BF16) made = made && cache_maps(c, n, ph.pair ? 64 : 128, &maps[1], &unused) && cache_maps(c, n, 128, &unused, &maps[2]);
+      made = made && cache_maps(c, n, ph.pair ? 64 : 128, &maps[1], &unused) && cache_maps(c, n, 128, &unused, &maps[2]);
       if (!made) { launched(e); return PC_ERR_CUDA; }
       e = pc::launch_cache_wide(maps, wp, c->format, a->d, ph.pair, sms, st);
       slot += ph.n_split;

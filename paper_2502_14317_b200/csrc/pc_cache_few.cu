@@ -57,10 +57,10 @@ __device__ __forceinline__ uint32_t free_par(uint32_t n) { return (n & 1u) ^ 1u;
 template <int FMT>
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if constexpr (FMT == FMT_BF16)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
   else
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
@@ -79,16 +79,6 @@ __device__ __forceinline__ float max_over_keys(float x) {
 #pragma unroll
   for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, o));
   return x;
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-  uint2 v;
-  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
-  return v;
 }
 __device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, bool there) {      // zero where there is no entry
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
@@ -205,12 +195,12 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     const int g = lane >> 2, a = lane & 3;
     constexpr bool Q_REGS = NT8 <= 2;
     uint2 qf[Q_REGS ? C::KST : 1][Q_REGS ? NT8 : 1];
-    const uint32_t sq = smem_u32(smem + C::OFF_Q) + lane * 8;
+    const uint2* const sq = reinterpret_cast<const uint2*>(smem + C::OFF_Q) + lane;
     if constexpr (Q_REGS) {
 #pragma unroll
       for (int ks = 0; ks < C::KST; ++ks)
 #pragma unroll
-        for (int t = 0; t < NT8; ++t) qf[ks][t] = lds64(sq + (ks * NT8 + t) * 256);
+        for (int t = 0; t < NT8; ++t) qf[ks][t] = sq[(ks * NT8 + t) * 32];
     }
     // per row pair (2 a, 2 a + 1) of each 8 rows: reference maximum (log2 units), sum over this thread's keys, scale of the weights
     float m[NT8][2], l[NT8][2], cw[NT8][2], qs[NT8][2], acc[C::MT][NT8][4];
@@ -230,7 +220,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     for (int i = 0; i < nt; ++i) {
       const int st = i % NS;
       if (!mbar_wait(&mi.full[st], full_par(i / NS), abort_flag, prm.status, WF_FULL)) break;
-      const uint32_t stage = smem_u32(smem) + st * C::STAGE_BYTES;
+      const uint8_t* const stage = smem + st * C::STAGE_BYTES;
 #pragma unroll 1
       for (int step = 0; step < C::STEPS; ++step) {
         const int r0 = (step * C::WARPS + warp) * 16, key0 = (j0 + i) * KEYS + r0;
@@ -251,7 +241,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             for (int u = 0; u < 2; ++u) {
               uint32_t off = (r0 + g + 8 * u) * C::BOXB + (a * C::CPT + h) * 16;
               off ^= ((off >> 7) & C::SWZ) << 4;
-              kr[u] = lds128(stage + b * KEYS * C::BOXB + off);
+              kr[u] = *reinterpret_cast<const uint4*>(stage + b * KEYS * C::BOXB + off);
             }
             const uint32_t x0[4] = {kr[0].x, kr[0].y, kr[0].z, kr[0].w}, x1[4] = {kr[1].x, kr[1].y, kr[1].z, kr[1].w};
 #pragma unroll
@@ -268,7 +258,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 #pragma unroll
               for (int c = 0; c < NT8; ++c) {
                 uint2 q;
-                if constexpr (Q_REGS) q = qf[ks][c]; else q = lds64(sq + (ks * NT8 + c) * 256);
+                if constexpr (Q_REGS) q = qf[ks][c]; else q = sq[(ks * NT8 + c) * 32];
                 mma16816<FMT>(s[ks & 1][c], a0, a1, a2, a3, q.x, q.y);
               }
             }
@@ -282,12 +272,12 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             const int k = 2 * a + (u & 1) + 8 * (u >> 1);
             uint32_t off = (r0 + k) * C::BOXB + g * (C::BOXB / 8);
             off ^= ((off >> 7) & C::SWZ) << 4;
-            const uint32_t from = stage + C::HALF_BYTES + b * KEYS * C::BOXB + off;
+            const uint8_t* const from = stage + C::HALF_BYTES + b * KEYS * C::BOXB + off;
             if constexpr (C::BOXB == 128) {
-              const uint4 y = lds128(from);
+              const uint4 y = *reinterpret_cast<const uint4*>(from);
               v[b][u][0] = y.x; v[b][u][1] = y.y; v[b][u][2] = y.z; v[b][u][3] = y.w;
             } else {
-              const uint2 y = lds64(from);
+              const uint2 y = *reinterpret_cast<const uint2*>(from);
               v[b][u][0] = y.x; v[b][u][1] = y.y;
             }
             if (tail && key0 + k >= n) {                         // whatever stands behind the last entry, NaN included

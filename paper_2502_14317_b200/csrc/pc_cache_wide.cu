@@ -5,9 +5,8 @@
 // 128).  alt = 1: both blocks hold the same rows and take alternate key tiles.  Every item (kv-head, row group, key split) leaves
 // partial results, which the merge kernel joins with the sequences' own.
 //
-// 8-bit caches: the epilogue's warps, which have nothing to do while an item's tiles go through, make operands of the codes.  A
-// thread copies 16 codes at a time into slots of its own (cp.async, three tiles deep, so that no barrier is needed), and
-// writes them into the ring's stages as halves (keys, exactly; the scale of a key multiplies its column of S in the softmax
+// 8-bit caches: the epilogue's warps, which have nothing to do while an item's tiles go through, make operands of the codes.  These
+// arrive in three slots of half a tile (keys or values), and go into the ring's stages as halves (keys, exactly; the scale of a key multiplies its column of S in the softmax
 // warps, the power of two of a query row is part of the row's softmax scale) or as bf16 (values, code * scale rounded once, as they are read back:
 // the probabilities beside them are rounded to bf16 too).
 #include "pc_cache.h"
@@ -36,8 +35,7 @@ struct Off8 {
 // key_scale: a tile's scales stay until its softmax has read them.  The converter is at most NK + 2 tiles ahead of that: a key stage is
 // free once the products of its tile have run, and those wait for the softmax to have read the logits before theirs.
 struct __align__(16) Extra8 {
-  uint64_t sc_full[8];
-  float raw_scale[3][TILE];
+  uint64_t sc_full[8], raw_full[3], raw_free[3];
   float key_scale[8][TILE];
 };
 static_assert(Off8<Cfg8<128, 1>>::EXTRA + sizeof(Extra8) <= 232448, "shared memory of a CTA");
@@ -54,23 +52,6 @@ __device__ __forceinline__ Item decode_item(const WidePhase& p, int item) {
   return it;
 }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool there) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-  return v;
-}
-__device__ __forceinline__ void sts128(uint32_t a, uint4 v) {
-  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
-}
 // f16 operands, fp32 accumulation
 __host__ __device__ constexpr uint32_t make_idesc_f16_f32(int M, int N) {
   return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
@@ -97,108 +78,110 @@ struct ScaledHooks : Hooks<C> {
   }
 };
 
-// Codes of the epilogue's warps on their way into the ring.  A half is the keys or the values of a tile; a warp has 32 of its rows.
+// Halves (keys or values of a tile) of an item's n tiles in the order in which the issuers want them: K of the first `lag` tiles, then
+// V of tile t, K of tile t + lag.
+__device__ __forceinline__ void half_of(int h, int n, int lag, bool& values, int& t) {
+  if (lag > n) lag = n;
+  if (h < lag) { values = false; t = h; return; }
+  h -= lag;
+  const int both = n - lag;                                // tiles whose V is followed by a K
+  if (h < 2 * both) { values = (h & 1) == 0; t = (h >> 1) + (values ? 0 : lag); }
+  else { values = true; t = both + (h - 2 * both); }
+}
+
+// The epilogue's warps between the raw slots and the ring; a warp has 32 rows of a half.
 template <class C, int FMT>
 struct Converter {
-  static constexpr int D = C::D, LPR = D / 16, PIECES = 32 * LPR / 32;      // lanes of a row, 16-byte pieces of a lane
+  static constexpr int D = C::D, LPR = D / 16, PIECES = LPR;                // 16-byte pieces of a row; pieces of a lane
   const Ctx2& cx;
   const WidePhase& prm;
   Extra8& ex;
-  uint32_t raw;                                            // this lane's first slot
-  // Row and 16-byte piece of a row of this lane: of the eight lanes that store together at head size 128, four are in the next
-  // row, whose swizzle puts their chunks into the other banks.
+  const uint8_t* raw;
+  // Row and piece of this lane in a step of 32 / LPR rows: of the eight lanes that store together at head size 128, four are in the
+  // next row, whose swizzle puts their chunks into the other banks.
   int lane_row, piece;
-  int warp, lane, slot = 0;                                // slot: raw slot of the next half that is converted
-  uint32_t k = 0, v = 0, tile = 0;                         // stages used so far; tiles of earlier items
-  __device__ __forceinline__ Converter(const Ctx2& c, const WidePhase& p, Extra8& e, uint8_t* raw_smem, int w, int l)
-      : cx(c), prm(p), ex(e), raw(smem_u32(raw_smem) + (w * PIECES * 32 + l) * 16), lane_row(D == 128 ? (l >> 4) * 2 + ((l >> 2) & 1) : l / 4),
+  int warp, lane;
+  uint32_t k = 0, v = 0, raws = 0, tile = 0;               // uses of the stages and of the slots; tiles of earlier items
+  __device__ __forceinline__ Converter(const Ctx2& c, const WidePhase& p, Extra8& e, const uint8_t* raw_smem, int w, int l)
+      : cx(c), prm(p), ex(e), raw(raw_smem), lane_row(D == 128 ? (l >> 4) * 2 + ((l >> 2) & 1) : l / 4),
         piece(D == 128 ? (l & 3) | ((l >> 1) & 4) : l & 3), warp(w), lane(l) {}
 
-  __device__ __forceinline__ void fetch(bool values, int j, int hkv, int s) {
-    const uint8_t* const src = (values ? prm.v8 : prm.k8) + ((size_t)hkv * prm.c.capacity + (size_t)j * TILE + warp * 32) * D;
-    const int left = prm.c.n_keys - j * TILE - warp * 32;
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int row = i * (32 / LPR) + lane_row;
-      cp_async16(raw + s * C::RAW_BYTES + i * 512, row < left ? src + (size_t)row * D + piece * 16 : (const void*)(values ? prm.v8 : prm.k8), row < left);
-    }
-    const float* const sc = (values ? prm.c.v_scale : prm.c.k_scale) + (size_t)hkv * prm.c.capacity;
-    cp_async4(smem_u32(&ex.raw_scale[s][warp * 32 + lane]), lane < left ? sc + (size_t)j * TILE + warp * 32 + lane : sc, lane < left);
-  }
-  // the n-th half of an item in the order in which the issuers want them: K of the first `lag` tiles, then V of tile t, K of tile t + lag
-  __device__ __forceinline__ void half_of(int h, int n, int lag, bool& values, int& t) const {
-    if (lag > n) lag = n;
-    if (h < lag) { values = false; t = h; return; }
-    h -= lag;
-    const int both = n - lag;                              // tiles whose V is followed by a K
-    if (h < 2 * both) { values = (h & 1) == 0; t = (h >> 1) + (values ? 0 : lag); }
-    else { values = true; t = both + (h - 2 * both); }
+  // scale of this lane's row (row `lane` of the warp's 32), 0 behind the last entry
+  __device__ __forceinline__ float scale_of(const Item& it, int h, int lag) const {
+    bool values;
+    int t;
+    half_of(h, it.n, lag, values, t);
+    const int key = (it.j0 + t) * TILE + warp * 32 + lane;
+    return key < prm.c.n_keys ? __ldg((values ? prm.c.v_scale : prm.c.k_scale) + (size_t)it.hkv * prm.c.capacity + key) : 0.0f;
   }
   template <bool VALUES>
-  __device__ __forceinline__ bool convert(int t) {
+  __device__ __forceinline__ bool convert(int t, float scale) {
     Misc2& mi = *cx.mi;
     uint32_t& n = VALUES ? v : k;
     constexpr int FIRST = VALUES ? C::NK : 0, STAGES = VALUES ? C::NV : C::NK;
-    const int st = FIRST + n % STAGES;
-    if (!WAIT2S(&mi.kv_free[st], free_par(n / STAGES), W2_KVFREE)) return false;
-    const uint32_t to = smem_u32(cx.ring) + st * C::STAGE_BYTES;
-#pragma unroll 2
-    for (int i = 0; i < PIECES; ++i) {
-      const int row = warp * 32 + i * (32 / LPR) + lane_row, c = piece;      // elements 16 c .. 16 c + 15 of the row
-      const uint4 x = lds128(raw + slot * C::RAW_BYTES + i * 512);
-      uint4 a, b;
-      if constexpr (VALUES) {
-        const float s = ex.raw_scale[slot][row];
-        const uint2 y0 = codes_to_bf16x4<FMT>(x.x, s), y1 = codes_to_bf16x4<FMT>(x.y, s), y2 = codes_to_bf16x4<FMT>(x.z, s), y3 = codes_to_bf16x4<FMT>(x.w, s);
-        a = make_uint4(y0.x, y0.y, y1.x, y1.y);
-        b = make_uint4(y2.x, y2.y, y3.x, y3.y);
-      } else {
-        const uint32_t z0 = flip_signs<FMT>(x.x), z1 = flip_signs<FMT>(x.y), z2 = flip_signs<FMT>(x.z), z3 = flip_signs<FMT>(x.w);
-        a = make_uint4(codes_to_half2<FMT, 0>(z0), codes_to_half2<FMT, 1>(z0), codes_to_half2<FMT, 0>(z1), codes_to_half2<FMT, 1>(z1));
-        b = make_uint4(codes_to_half2<FMT, 0>(z2), codes_to_half2<FMT, 1>(z2), codes_to_half2<FMT, 0>(z3), codes_to_half2<FMT, 1>(z3));
+    const int st = FIRST + n % STAGES, slot = raws % C::RAW;
+    if (!WAIT2S(&mi.kv_free[st], free_par(n / STAGES), W2_KVFREE) || !WAIT2S(&ex.raw_full[slot], full_par(raws / C::RAW), W2_KVFULL)) return false;
+    uint8_t* const to = cx.ring + st * C::STAGE_BYTES;
+    const uint8_t* const from = raw + slot * C::RAW_BYTES;
+#pragma unroll
+    for (int i0 = 0; i0 < PIECES; i0 += 4) {               // four pieces at a time, their latencies side by side
+      uint4 in[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        uint32_t off = (warp * 32 + (i0 + u) * (32 / LPR) + lane_row) * D + piece * 16;
+        off ^= ((off >> 7) & (D == 128 ? 7 : 3)) << 4;
+        in[u] = *reinterpret_cast<const uint4*>(from + off);
       }
-      const uint32_t base = to + (c / 4) * 16384;
-      sts128(base + sw128_offset(row, (2 * c) % 8), a);
-      sts128(base + sw128_offset(row, (2 * c + 1) % 8), b);
+      if (i0 + 4 == PIECES) warp_arrive(&ex.raw_free[slot]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int local = (i0 + u) * (32 / LPR) + lane_row, row = warp * 32 + local;
+        const uint4 x = in[u];
+        uint4 a, b;
+        if constexpr (VALUES) {
+          const float s = __shfl_sync(0xFFFFFFFFu, scale, local);
+          const uint2 y0 = codes_to_bf16x4<FMT>(x.x, s), y1 = codes_to_bf16x4<FMT>(x.y, s), y2 = codes_to_bf16x4<FMT>(x.z, s), y3 = codes_to_bf16x4<FMT>(x.w, s);
+          a = make_uint4(y0.x, y0.y, y1.x, y1.y);
+          b = make_uint4(y2.x, y2.y, y3.x, y3.y);
+        } else {
+          const uint32_t z0 = flip_signs<FMT>(x.x), z1 = flip_signs<FMT>(x.y), z2 = flip_signs<FMT>(x.z), z3 = flip_signs<FMT>(x.w);
+          a = make_uint4(codes_to_half2<FMT, 0>(z0), codes_to_half2<FMT, 1>(z0), codes_to_half2<FMT, 0>(z1), codes_to_half2<FMT, 1>(z1));
+          b = make_uint4(codes_to_half2<FMT, 0>(z2), codes_to_half2<FMT, 1>(z2), codes_to_half2<FMT, 0>(z3), codes_to_half2<FMT, 1>(z3));
+        }
+        uint8_t* const base = to + (piece / 4) * 16384;    // elements 16 piece .. 16 piece + 15 of the row
+        *reinterpret_cast<uint4*>(base + sw128_offset(row, (2 * piece) % 8)) = a;
+        *reinterpret_cast<uint4*>(base + sw128_offset(row, (2 * piece + 1) % 8)) = b;
+      }
     }
     if constexpr (!VALUES) {
       const uint32_t at = tile + t;
-      ex.key_scale[at % 8][warp * 32 + lane] = ex.raw_scale[slot][warp * 32 + lane];
+      ex.key_scale[at % 8][warp * 32 + lane] = scale;
       warp_arrive(&ex.sc_full[at % 8]);
     }
     fence_proxy_async_smem();
     warp_arrive(&mi.kv_full[st]);
     ++n;
+    ++raws;
     return true;
   }
   __device__ __forceinline__ void item(const Item& it, int lag) {
-    const int halves = 2 * it.n;
-    bool values;
-    int t;
-    for (int h = 0; h < C::RAW; ++h) {
-      if (h < halves) { half_of(h, it.n, lag, values, t); fetch(values, it.j0 + t, it.hkv, h); }
-      cp_async_commit();
-    }
-    slot = 0;
-    for (int h = 0; h < halves; ++h) {
-      cp_async_wait<C::RAW - 1>();
-      __syncwarp();                                        // scales come through the warp's other lanes
+    float next = scale_of(it, 0, lag);
+    for (int h = 0; h < 2 * it.n; ++h) {
+      const float scale = next;
+      if (h + 1 < 2 * it.n) next = scale_of(it, h + 1, lag);
+      bool values;
+      int t;
       half_of(h, it.n, lag, values, t);
-      if (!(values ? convert<true>(t) : convert<false>(t))) break;
-      __syncwarp();
-      if (h + C::RAW < halves) { half_of(h + C::RAW, it.n, lag, values, t); fetch(values, it.j0 + t, it.hkv, slot); }
-      cp_async_commit();
-      slot = slot + 1 == C::RAW ? 0 : slot + 1;
+      if (!(values ? convert<true>(t, scale) : convert<false>(t, scale))) break;
     }
-    cp_async_wait<0>();
-    __syncwarp();
     tile += it.n;
   }
 };
 
 }  // namespace
 
-// tensor maps (boxes of 64 d): tm_q (rows of a kv-head, 128), bf16: tm_k (64 entries of a pair or 128), tm_v (128).  Rows behind the end
+// tensor maps: tm_q (rows of a kv-head, 64 x 128); bf16 (boxes of 64 d): tm_k (64 entries of a pair or 128), tm_v (128); 8 bits: codes of 128
+// entries.  Rows behind the end
 // of a tensor read as zeros; the softmax masks the entries behind the last.
 template <int D, int FMT, bool PAIR>
 __global__ void __launch_bounds__(NT2, 1)
@@ -215,7 +198,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   const int block_rows = TILE * NCTA, group_rows = block_rows * (alt ? 1 : 2), rows = prm.c.rows;
   // first row of block b of CTA `r` in row group rg
   auto first_row = [&](int rg, int b, int r) { return rg * group_rows + (alt ? 0 : b * block_rows) + r * TILE; };
-  if (tid == WARP_PRODUCER * 32) { tma_prefetch_desc(&tm_q); if (!Q8) { tma_prefetch_desc(&tm_k); tma_prefetch_desc(&tm_v); } }
+  if (tid == WARP_PRODUCER * 32) { tma_prefetch_desc(&tm_q); tma_prefetch_desc(&tm_k); tma_prefetch_desc(&tm_v); }
   Ctx2 cx;
   cx.mi = reinterpret_cast<Misc2*>(smem + O::MISC);
   cx.sQ = smem + O::Q;
@@ -228,6 +211,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     init_barriers2<C>(mi, prm.c.wait_kcycles, leader, Q8 ? 4 : 1);       // four converting warps in the place of one copy
     if constexpr (Q8) {
       for (int i = 0; i < 8; ++i) mbar_init(&ex.sc_full[i], 4);
+      for (int i = 0; i < 3; ++i) { mbar_init(&ex.raw_full[i], 1); mbar_init(&ex.raw_free[i], 4); }
       fence_mbar_init();
     }
   }
@@ -246,6 +230,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       if (elect_one()) {
         const int n_items = prm.c.Hkv * prm.c.n_rg * prm.c.n_split;
         Prod p;
+        [[maybe_unused]] uint32_t raws = 0;                // uses of the raw slots
         while (!*cx.abort_flag) {
           const int item = next_item<C>(cx, p, leader, prm.counter, n_items);
           if (item >= n_items) break;
@@ -268,7 +253,17 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               load_box<C>(cx.sQ + qs * C::Q_BYTES + a * 16384, &tm_q, bar, a * 64, first_row(it.rg, b, rank), it.hkv, 0);
             ++p.q;
           }
-          if constexpr (!Q8) {
+          if constexpr (Q8) {
+            for (int h = 0; h < 2 * it.n; ++h, ++raws) {
+              bool values;
+              int t;
+              half_of(h, it.n, alt ? 2 : 1, values, t);
+              const int slot = raws % C::RAW;
+              if (!WAIT2(&ex.raw_free[slot], free_par(raws / C::RAW), W2_KVFREE)) break;
+              mbar_arrive_expect_tx(&ex.raw_full[slot], C::RAW_BYTES);
+              tma_load_4d(smem + O::RAW + slot * C::RAW_BYTES, values ? &tm_v : &tm_k, &ex.raw_full[slot], 0, (it.j0 + t) * TILE, it.hkv, 0);
+            }
+          } else {
             uint8_t* dst;
             auto load_k = [&](int t) {
               const uint32_t bar = ring_stage<C, false>(cx, p, leader, &dst);
@@ -291,8 +286,10 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         d.kind = KIND_DONE; d.c = d.hkv = d.len = 0;
         publish<C>(cx, p, d);
         if constexpr (!Q8) drain_copies<C>(cx, p, leader);
-        else if (*cx.abort_flag)                            // only queries were copied here
+        else if (*cx.abort_flag) {                          // every copy issued has landed before the exit
           for (uint32_t i = (p.q > NQ ? p.q - NQ : 0); i < p.q; ++i) mbar_wait_drain(&mi.q_full[i % NQ], full_par(i / NQ), cx.abort_flag);
+          for (uint32_t i = (raws > C::RAW ? raws - C::RAW : 0); i < raws; ++i) mbar_wait_drain(&ex.raw_full[i % C::RAW], full_par(i / C::RAW), cx.abort_flag);
+        }
       }
       __syncwarp();
     } else if (warp == WARP_QK && leader) {

@@ -3,6 +3,7 @@
 #include <cstdint>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
+#include "pc_sm100.cuh"
 
 namespace pc {
 
@@ -34,11 +35,24 @@ __device__ __forceinline__ uint32_t flip_signs(uint32_t x) { return FMT == FMT_I
 // Four codes times their scale, rounded once to bf16
 template <int FMT>
 __device__ __forceinline__ uint2 codes_to_bf16x4(uint32_t x, float scale) {
-  x = flip_signs<FMT>(x);
-  const uint32_t h0 = codes_to_half2<FMT, 0>(x), h1 = codes_to_half2<FMT, 1>(x);
-  const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h0)), b = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-  const __nv_bfloat162 p = __floats2bfloat162_rn(a.x * scale, a.y * scale), q = __floats2bfloat162_rn(b.x * scale, b.y * scale);
-  return make_uint2(*reinterpret_cast<const uint32_t*>(&p), *reinterpret_cast<const uint32_t*>(&q));
+  const uint64_t s2 = pack_f32x2(scale, scale);
+  uint64_t lo, hi;
+  if constexpr (FMT == FMT_INT8) {                         // a byte u behind 0x4B0000 reads as 2^23 + u
+    x = flip_signs<FMT>(x);
+    const uint64_t bias = pack_f32x2(-8388736.0f, -8388736.0f);          // 2^23 + 128
+    auto f = [&](uint32_t sel) { return __uint_as_float(prmt(x, 0x4B000000u, sel)); };
+    lo = add_f32x2(pack_f32x2(f(0x7440), f(0x7441)), bias);
+    hi = add_f32x2(pack_f32x2(f(0x7442), f(0x7443)), bias);
+  } else {
+    const uint32_t h0 = codes_to_half2<FMT, 0>(x), h1 = codes_to_half2<FMT, 1>(x);
+    const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h0)), b = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+    lo = pack_f32x2(a.x, a.y);
+    hi = pack_f32x2(b.x, b.y);
+  }
+  float a, b, c, d;
+  unpack_f32x2(mul_f32x2(lo, s2), a, b);
+  unpack_f32x2(mul_f32x2(hi, s2), c, d);
+  return make_uint2(pack_bf16x2(a, b), pack_bf16x2(c, d));
 }
 
 // Four values (already multiplied by Q / a) -> codes
