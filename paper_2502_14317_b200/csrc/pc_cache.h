@@ -50,6 +50,17 @@ struct CacheRows {
 };
 cudaError_t launch_cache_rows(const CacheRows& p, int d, cudaStream_t st);
 
+// What a row's result is joined from beside the caches' results that a kernel has itself: slots in memory and the new tokens' own keys.
+struct CacheMerge {
+  int n_slots, total_rows;
+  const float* part_o;
+  const float2* part_ml;
+  CacheRows q;                                   // (rows in memory)
+  const void *k_win, *v_win;                     // or null
+  long long k_stride[3], v_stride[3];
+  __nv_bfloat16* out;
+  float* lse;
+};
 // One phase of pc_cache_attn: the rows of each of `seqs` sequences (prefix: one, all rows; own caches: B, w * G rows) over a cache.
 // A split's result of a row goes to slot slot0 + split of its n_slots: the unnormalised output, and (maximum in log2 units,
 // sum); a split without keys leaves (-inf, 0) and no output.
@@ -66,11 +77,16 @@ struct CachePhase {
   int* status;
   int wait_kcycles;
 };
+// Few rows (pc_cache_few.cu), groups of 8 or 16.  finish null: every split leaves its slot.  Else the splits of a (sequence, kv-head, row
+// group) are the CTAs of a cluster, and the kernel finishes its rows: its splits' results, finish's slots and the new tokens' keys.
+// deep: one CTA per SM with twice the stages and warps, else two.
 // maps of the cache's keys and values: boxes of few_keys() entries
-int few_keys(int format, int d, int rows);       // keys of a stage
+int few_keys(int format, int d);                 // keys of a stage
 int few_rows(int rows);                          // rows of a row group
-int few_ctas_per_sm(int rows);
-cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, int format, int d, cudaStream_t st);
+int few_warps(int rows, bool deep);              // warps that take keys, 16 at a time
+int few_clusters(int n_split, bool deep);        // clusters of n_split CTAs that the current device runs at a time
+cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool deep, int format,
+                             int d, cudaStream_t st);
 
 // The same phase for more than 32 rows of one sequence (pc_cache_wide.cu), blocks of 128 rows.
 struct WidePhase {
@@ -84,16 +100,6 @@ struct WidePhase {
 cudaError_t launch_cache_wide(const CUtensorMap* maps, const WidePhase& p, int format, int d, bool pair, int sm_count, cudaStream_t st);
 
 // Joins the slots of a row and the new tokens' own keys.
-struct CacheMerge {
-  int n_slots, total_rows;
-  const float* part_o;
-  const float2* part_ml;
-  CacheRows q;                                   // (rows in memory)
-  const void *k_win, *v_win;                     // or null
-  long long k_stride[3], v_stride[3];
-  __nv_bfloat16* out;
-  float* lse;
-};
 cudaError_t launch_cache_merge(const CacheMerge& p, int d, cudaStream_t st);
 
 }  // namespace pc

@@ -4,6 +4,7 @@
 #include "pc_kernels.h"
 #include "pc_tmap.h"
 
+#include <atomic>
 #include <cmath>
 
 namespace {
@@ -94,28 +95,49 @@ int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0, const
 // ------------------------------------------------------------------------------------ attention over shared and own caches
 namespace {
 
-struct PhasePlan { bool wide, pair; int alt, n_rg, n_split; };
+struct PhasePlan { bool wide, pair, deep, finish; int alt, n_rg, n_split; };
 struct CachePlan {
   PhasePlan prefix, own;
-  int n_slots;
+  int n_slots;                                   // results of a row in memory
+  bool finished;                                 // the last phase finishes the rows: no merge
   int64_t total_rows;
   bool rows, halves;                             // a launch for the rows (for a wide phase, or no phase at all), as halves as well (over 8-bit codes)
   size_t off_counter, off_rows, off_halves, off_scale, off_ml, off_o, total;
 };
 
-// Splits of the keys: rounds of the grid x (some tiles of fixed cost + tiles of a split) is least.
-PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count) {
+// Clusters of n CTAs of the kernel for few rows that the current device runs at a time (asked once per device).
+int few_fit(int n, bool deep) {
+  static std::atomic<int> known[64][2][17];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  std::atomic<int>& k = known[dev][deep][n];
+  int v = k.load(std::memory_order_relaxed);
+  if (v == 0) k.store(v = pc::few_clusters(n, deep) + 1, std::memory_order_relaxed);
+  return v - 1;
+}
+
+// Splits of the keys, and whether the kernel finishes its rows itself (the last phase; up to 16 splits, the CTAs of a cluster)
+// or leaves slots for the merge.  Least time by a model in microseconds: rounds of the grid x (5 for the queries, the first unit and
+// the join + its units, 0.65 each for a warp, or their bytes at the CTA's share of the memory's rate), and 4 for the merge's launch.
+PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, bool last, int sm_count) {
   PhasePlan p = {};
-  const int per = pc::few_rows((int)rows), keys = pc::few_keys(format, d, (int)rows);
+  const int per = pc::few_rows((int)rows), keys = pc::few_keys(format, d);
   p.n_rg = (int)((rows + per - 1) / per);
   const int tiles = (n_keys + keys - 1) / keys;
-  const int64_t items = seqs * Hkv * p.n_rg, units = (int64_t)sm_count * pc::few_ctas_per_sm((int)rows);
-  int64_t least = -1;
+  const double items = (double)seqs * Hkv * p.n_rg, tile_us = 2.0 * keys * d * (format == PC_KV_BF16 ? 2 : 1) / 6.5e6;
+  double least = -1.0;
   p.n_split = 1;
-  for (int s = 1; s <= 64 && s <= tiles; ++s) {
-    const int64_t rounds = (items * s + units - 1) / units, cost = rounds * (4 + (tiles + s - 1) / s) * 64 + s;
-    if (least < 0 || cost < least) { least = cost; p.n_split = s; }
-  }
+  for (int finish = last ? 1 : 0; finish >= 0; --finish)
+    for (int deep = 0; deep <= 1; ++deep) {
+      const double alone = 0.65 * (keys / 16) / pc::few_warps((int)rows, deep != 0);
+      for (int s = 1; s <= (finish ? 16 : 64) && s <= tiles; ++s) {
+        const double fit = finish && s > 1 ? few_fit(s, deep != 0) : (double)(deep ? 1 : 2) * sm_count / s;
+        if (fit < 1.0) continue;
+        const double rounds = std::ceil(items / fit), active = (items < fit ? items : fit) * s;
+        const double cost = rounds * (5.0 + (tile_us * active > alone ? tile_us * active : alone) * std::ceil((double)tiles / s)) + (finish ? 0.0 : 4.0);
+        if (least < 0.0 || cost < least) { least = cost; p.n_split = s; p.deep = deep != 0; p.finish = finish != 0; }
+      }
+    }
   return p;
 }
 
@@ -143,12 +165,12 @@ PhasePlan wide_plan(int64_t rows, int Hkv, int d, int format, int n_keys, int sm
 int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
   if (a->B < 1 || a->w < 1 || a->Hq < 1 || a->Hkv < 1 || a->Hq % a->Hkv != 0 || a->n_prefix < 0 || a->n_own < 0) return PC_ERR_INVALID_ARG;
   if (a->d != 64 && a->d != 128) return PC_ERR_UNSUPPORTED;
-  if (a->w > 128 || (int64_t)a->B * a->w * a->Hq > (1 << 24)) return PC_ERR_UNSUPPORTED;
+  if (a->w > 128 || a->Hq > (1 << 18) || (int64_t)a->B * a->w * a->Hq > (1 << 24)) return PC_ERR_UNSUPPORTED;
   const int G = a->Hq / a->Hkv;
   p.total_rows = (int64_t)a->B * a->w * G;
   p.n_slots = 0;
   p.prefix = p.own = {};
-  p.rows = p.halves = false;
+  p.rows = p.halves = p.finished = false;
   for (int own = 0; own <= 1; ++own) {
     const pc_kv_cache* const c = own ? a->own : a->prefix;
     const int n = own ? a->n_own : a->n_prefix;
@@ -161,11 +183,12 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
       p.rows = true;
       p.halves = c->format != PC_KV_BF16;
     } else
-    ph = few_plan(own ? a->B : 1, own ? (int64_t)a->w * G : p.total_rows, a->Hkv, a->d, c->format, n, sm_count);
+    ph = few_plan(own ? a->B : 1, own ? (int64_t)a->w * G : p.total_rows, a->Hkv, a->d, c->format, n, own || a->n_own == 0, sm_count);
     if ((own ? a->B : 1ll) * a->Hkv * ph.n_rg * ph.n_split > 0x7FFFFFFF) return PC_ERR_UNSUPPORTED;
-    p.n_slots += ph.n_split;
+    if (!ph.finish) p.n_slots += ph.n_split;
+    p.finished |= ph.finish;
   }
-  if (p.n_slots == 0) p.rows = true;
+  if (p.n_slots == 0 && !p.finished) p.rows = true;
   size_t off = 0;
   p.off_counter = off; off += ALIGN;
   p.off_halves = off; off += p.halves ? align_up((size_t)p.total_rows * a->Hkv * a->d * 2) : 0;
@@ -207,7 +230,7 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
   if (int32_t rc = cache_plan(a, sms > 0 ? sms : 148, plan); rc != PC_OK) return rc;
   if (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16) || (a->k_win == nullptr) != (a->v_win == nullptr)) return PC_ERR_INVALID_ARG;
   if (!aligned(a->k_win, 16) || !aligned(a->v_win, 16) || !aligned(a->workspace, 32)) return PC_ERR_INVALID_ARG;
-  if (plan.n_slots == 0 && a->k_win == nullptr) return PC_ERR_INVALID_ARG;              // nothing to attend to
+  if (a->n_prefix == 0 && a->n_own == 0 && a->k_win == nullptr) return PC_ERR_INVALID_ARG;              // nothing to attend to
   if ((a->q_pos == nullptr && a->q_pos0 < 0) || !(a->rope_theta >= 0.0f) || !(a->softmax_scale >= 0.0f)) return PC_ERR_INVALID_ARG;
   pc::CacheRows rows = {};
   pc::CacheMerge merge = {};
@@ -233,6 +256,12 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
   } else if (a->clear_status && a->status_word) {
     e = cudaMemsetAsync(a->status_word, 0, sizeof(int), st);
   }
+  merge.n_slots = plan.n_slots; merge.total_rows = (int)plan.total_rows;
+  merge.part_o = reinterpret_cast<const float*>(ws + plan.off_o);
+  merge.part_ml = reinterpret_cast<const float2*>(ws + plan.off_ml);
+  merge.q = rows;
+  merge.k_win = a->k_win; merge.v_win = a->v_win;
+  merge.out = static_cast<__nv_bfloat16*>(a->out); merge.lse = a->lse;
   int slot = 0;
   for (int own = 0; own <= 1 && e == cudaSuccess; ++own) {
     const pc_kv_cache* const c = own ? a->own : a->prefix;
@@ -268,17 +297,11 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
       continue;
     }
     CUtensorMap tm_k, tm_v;
-    if (!cache_maps(c, n, pc::few_keys(c->format, c->d, p.rows), &tm_k, &tm_v)) { launched(e); return PC_ERR_CUDA; }
-    e = pc::launch_cache_few(tm_k, tm_v, p, c->format, c->d, st);
+    if (!cache_maps(c, n, pc::few_keys(c->format, c->d), &tm_k, &tm_v)) { launched(e); return PC_ERR_CUDA; }
+    e = pc::launch_cache_few(tm_k, tm_v, p, ph.finish ? &merge : nullptr, ph.deep, c->format, c->d, st);
     slot += ph.n_split;
   }
-  if (e != cudaSuccess) return launched(e);
-  merge.n_slots = plan.n_slots; merge.total_rows = (int)plan.total_rows;
-  merge.part_o = reinterpret_cast<const float*>(ws + plan.off_o);
-  merge.part_ml = reinterpret_cast<const float2*>(ws + plan.off_ml);
-  merge.q = rows;
-  merge.k_win = a->k_win; merge.v_win = a->v_win;
-  merge.out = static_cast<__nv_bfloat16*>(a->out); merge.lse = a->lse;
+  if (e != cudaSuccess || plan.finished) return launched(e);
   return launched(pc::launch_cache_merge(merge, a->d, st));
 }
 

@@ -1,43 +1,46 @@
-// Attention of few query rows over a cache in bf16 or 8 bits (pc_cache_attn): up to 32 rows of a kv-head at a time.
+// Attention of few query rows over a cache in bf16 or 8 bits (pc_cache_attn): up to 16 rows of a kv-head at a time.
 //
 // With keys, then head-dim columns, as the 16 rows of a product and the query rows as its 8 columns,
 //     S^T [16 keys x 8 rows] = K Q^T,      O^T [16 of d x 8 rows] += V^T P^T,
-// a step computes what its rows need (8, 16 or 32 of them) and no more, and the codes of a cache go from shared memory into
+// a step computes what its rows need (8 or 16 of them) and no more, and the codes of a cache go from shared memory into
 // the operands' registers on their way: the operand layout asks a thread for 4 consecutive elements of a key at a time (for V: of
 // 4 keys at a time, so that bytes of two keys are interleaved), and which elements of d they are is free as long as Q has
 // them in the same order.  int8 and e4m3 become half precision exactly; the scale of a key multiplies its row of S^T, the scale
 // of a value its probability, so nothing that a cache holds is rounded.  Queries are bf16 numbers; times a power of two of their row
 // they are halves too (elements 2^-22 below the row's largest lose bits).  Probabilities are rounded to half precision (11 bits,
 // bf16 caches: bf16, 8 bits) beside sums and accumulators in fp32; half precision has a short range, so they are held relative to the
-// largest product of probability and scale of their row (c below), raised together with the reference maximum.
+// largest product of probability and scale of their row (cw below), raised together with the reference maximum.
 //
-// Bound by reading the cache.  A warp takes 16 keys at a time on its own, with its own maximum, sum and accumulators, and waits for
-// nobody but the copies; a producer warp keeps the ring full.  The maximum is looked at with one vote per 8 rows and raised
-// only where a logit exceeds it by 2^8.  The warps' results are added in shared memory, the splits' by the merge kernel.
+// Bound by reading the cache, and, with 16 rows of 8-bit codes, by the instructions that make operands of them.  A warp takes 16 keys (a
+// unit) at a time on its own, with its own maximum, sum and accumulators, and waits for nobody but the copies; a producer warp keeps
+// the ring full.  The maximum is looked at with one vote per 8 rows and raised only where a logit exceeds it by 2^8.  The warps'
+// results are added in shared memory, the splits' through distributed shared memory or by the merge kernel.
+#include "pc_cache_finish.cuh"
 #include "pc_cache_rows.cuh"
 #include "pc_kernels.h"
 #include "pc_kv8.cuh"
-#include "pc_sm100.cuh"
 #include <cfloat>
 
 namespace pc {
 
 namespace {
 
-template <int D_, int FMT_, int NT8_>
+template <int D_, int FMT_, int NT8_, bool DEEP_>
 struct Few {
   static constexpr int D = D_, FMT = FMT_, NT8 = NT8_;
   static constexpr int EB = FMT == FMT_BF16 ? 2 : 1;            // bytes of an element
   static constexpr int ROWB = D * EB, BOXES = ROWB > 128 ? 2 : 1, BOXB = ROWB / BOXES, EPB = BOXB / EB;
-  static constexpr int SWZ = BOXB == 128 ? 7 : 3;
-  static constexpr int WARPS = NT8 <= 2 ? 4 : 8;                // consumer warps
-  static constexpr int CTAS = NT8 <= 2 ? 2 : 1;                 // CTAs of an SM
-  static constexpr int STEPS = NT8 <= 2 && ROWB <= 128 ? 2 : 1;
-  static constexpr int KEYS = 16 * WARPS * STEPS, HALF_BYTES = KEYS * ROWB, STAGE_BYTES = 2 * HALF_BYTES;
-  static constexpr int NS_ = 98304 * (CTAS == 1 ? 2 : 1) / STAGE_BYTES, NS = NS_ > 8 ? 8 : NS_;
+  // Consumer warps: with the producers 16 warps an SM, 128 registers a thread, or 12 and 168.
+  static constexpr int CTAS = DEEP_ ? 1 : 2, WARPS = (NT8 == 1 ? 16 : 12) / CTAS - 1;
+  static constexpr int UNITS = ROWB == 256 ? 4 : 8;             // of a stage
+  static constexpr int KEYS = 16 * UNITS, HALF_BYTES = KEYS * ROWB, STAGE_BYTES = 2 * HALF_BYTES;
+  static constexpr int NS = 196608 / CTAS / STAGE_BYTES;
+  // a warp that waits for its next unit's stage is less than a lap of the ring ahead of the copies
+  static_assert((WARPS + UNITS - 1) / UNITS < NS, "parity of a stage");
   static constexpr int N = 8 * NT8, KST = D / 16, MT = D / 16;
   static constexpr int THREADS = 32 * (WARPS + 1);
-  static constexpr int OFF_SCALE = NS * STAGE_BYTES, OFF_Q = OFF_SCALE + (EB == 1 ? NS * 2 * KEYS * 4 : 0), OFF_MISC = OFF_Q + KST * NT8 * 256;
+  static constexpr int OFF_SCALE = NS * STAGE_BYTES, OFF_Q = OFF_SCALE + (EB == 1 ? NS * 2 * KEYS * 4 : 0), OFF_ROWS = OFF_Q + KST * NT8 * 256,
+                       OFF_MISC = OFF_ROWS + N * D * 2;
   static constexpr int CPT = BOXB / 64, EPC = 16 / EB, KPC = EPC / 4;      // 16-byte chunks of a thread in a box row, their elements and k-steps
   static_assert(WARPS * N * D * 4 <= OFF_SCALE, "partial results of the warps go into the ring");
 };
@@ -47,7 +50,7 @@ struct __align__(16) FewMisc {
   int abort_flag;                                               // these two words stay adjacent (bounded waits)
   int wait_kcycles;
   float qs[C::N];                                               // scale of a row's logits, in log2 units
-  float2 ml[C::WARPS][C::N];
+  float2 ml[C::WARPS][C::N], all[C::N];                         // maximum and sum of a row: of a warp, of the CTA
 };
 enum { WF_FULL = 411, WF_EMPTY };
 
@@ -58,10 +61,10 @@ template <int FMT>
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if constexpr (FMT == FMT_BF16)
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
   else
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
   uint32_t r;
@@ -86,25 +89,33 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, bool t
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {                             // once this thread's copies have landed
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
+template <int E>
+__device__ __forceinline__ void ld_cluster(uint32_t addr, float (&x)[E]) {
+  if constexpr (E == 4)
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]) : "r"(addr) : "memory");
+  else
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "r"(addr) : "memory");
+}
 
 }  // namespace
 
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, C::CTAS)
-cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CachePhase prm) {
-  constexpr int D = C::D, FMT = C::FMT, NT8 = C::NT8, N = C::N, KEYS = C::KEYS, NS = C::NS;
+cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CachePhase prm,
+                 const __grid_constant__ CacheMerge fin, const int finish) {
+  constexpr int D = C::D, FMT = C::FMT, NT8 = C::NT8, N = C::N, KEYS = C::KEYS, NS = C::NS, E = D / 32;
   constexpr bool Q8 = FMT != FMT_BF16;
   extern __shared__ __align__(1024) uint8_t smem[];
   FewMisc<C>& mi = *reinterpret_cast<FewMisc<C>*>(smem + C::OFF_MISC);
   volatile int* const abort_flag = &mi.abort_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   int x = blockIdx.x;
-  const int split = x % prm.n_split; x /= prm.n_split;
+  const int split = x % prm.n_split; x /= prm.n_split;          // (finish: the rank in the cluster)
   const int rg = x % prm.n_rg; x /= prm.n_rg;
   const int hkv = x % prm.Hkv, seq = x / prm.Hkv;
 
-  if (tid == 0) {
-    for (int i = 0; i < NS; ++i) { mbar_init(&mi.full[i], Q8 ? 33 : 1); mbar_init(&mi.empty[i], C::WARPS); }
+  if (tid == C::WARPS * 32) {
+    for (int i = 0; i < NS; ++i) { mbar_init(&mi.full[i], Q8 ? 33 : 1); mbar_init(&mi.empty[i], C::UNITS); }
     mi.abort_flag = 0;
     mi.wait_kcycles = prm.wait_kcycles;
     fence_mbar_init();
@@ -114,13 +125,17 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   RowTurner<D> turner(prm.rows_made ? 0.0f : prm.q.theta, lane);
   __syncthreads();
   chain();
-  int n = prm.n_keys;                                            // entries of this sequence
-  if (prm.len != nullptr) { n = prm.len[seq]; n = n < 0 ? 0 : n > prm.n_keys ? prm.n_keys : n; }
-  const int n_all = (n + KEYS - 1) / KEYS;
-  const int j0 = (int)((long long)n_all * split / prm.n_split), nt = (int)((long long)n_all * (split + 1) / prm.n_split) - j0;
+  const int entries = prm.len != nullptr ? __ldg(prm.len + seq) : prm.n_keys;
   const int row0 = seq * prm.rows + rg * N, n_rows = prm.rows - rg * N < N ? prm.rows - rg * N : N;      // rows of the kv-head
   const size_t part0 = ((size_t)hkv * prm.total_rows + row0) * prm.n_slots + prm.slot0 + split;
 
+  int n, j0, nt;                                                 // entries of this sequence; tiles j0 .. j0 + nt - 1 of this split
+  auto share = [&]() {
+    n = entries < 0 ? 0 : entries > prm.n_keys ? prm.n_keys : entries;
+    const int n_all = (n + KEYS - 1) / KEYS;
+    j0 = (int)((long long)n_all * split / prm.n_split);
+    nt = (int)((long long)n_all * (split + 1) / prm.n_split) - j0;
+  };
   // copies of tile i into its stage; the whole producer warp calls
   auto load = [&](int i) {
     const int st = i % NS, key = (j0 + i) * KEYS;
@@ -146,16 +161,18 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     __syncwarp();
   };
 
+
   if (warp == C::WARPS) {
+    share();
     for (int i = 0; i < NS && i < nt; ++i) load(i);
-  } else if (nt > 0 || (split == 0 && !prm.rows_made)) {
-    // ---- the rows' queries as operands, in the order in which the threads hold their keys
+  } else {
+    // ---- the rows' queries: as they are, and as operands in the order in which the threads hold their keys
     for (int r = warp; r < N; r += C::WARPS) {
-      constexpr int E = D / 32;
       uint32_t q[E / 2] = {};
       if (r < n_rows) {
         turner.row(prm.q, prm.rows_made != 0, hkv, row0 + r, lane, q);
-        if (split == 0 && !prm.rows_made) RowTurner<D>::store(prm.q.rows, (size_t)hkv * prm.total_rows + row0 + r, lane, q);
+        if (finish) RowTurner<D>::store(smem + C::OFF_ROWS, r, lane, q);
+        else if (split == 0 && !prm.rows_made) RowTurner<D>::store(prm.q.rows, (size_t)hkv * prm.total_rows + row0 + r, lane, q);
       }
       float qs = prm.q.scale_log2;
       if constexpr (Q8) {
@@ -176,11 +193,15 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
       if (lane == 0) mi.qs[r] = r < n_rows ? qs : 0.0f;
     }
+    share();
   }
-  if (nt == 0) {                                                 // nothing for this split: the merge leaves it out
-    if (tid < n_rows) prm.part_ml[part0 + (size_t)tid * prm.n_slots] = make_float2(-INFINITY, 0.0f);
-    return;
-  }
+  if (nt == 0) {                                                 // nothing for this split
+    if (!finish) {
+      if (tid < n_rows) prm.part_ml[part0 + (size_t)tid * prm.n_slots] = make_float2(-INFINITY, 0.0f);
+      return;
+    }
+    if (tid < N) mi.all[tid] = make_float2(-INFINITY, 0.0f);
+  } else {
   __syncthreads();
 
   if (warp == C::WARPS) {
@@ -193,15 +214,11 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   } else {
     // ================================================================ a warp: 16 keys at a time
     const int g = lane >> 2, a = lane & 3;
-    constexpr bool Q_REGS = NT8 <= 2;
-    uint2 qf[Q_REGS ? C::KST : 1][Q_REGS ? NT8 : 1];
-    const uint2* const sq = reinterpret_cast<const uint2*>(smem + C::OFF_Q) + lane;
-    if constexpr (Q_REGS) {
+    uint2 qf[C::KST][NT8];
 #pragma unroll
-      for (int ks = 0; ks < C::KST; ++ks)
+    for (int ks = 0; ks < C::KST; ++ks)
 #pragma unroll
-        for (int t = 0; t < NT8; ++t) qf[ks][t] = sq[(ks * NT8 + t) * 32];
-    }
+      for (int t = 0; t < NT8; ++t) qf[ks][t] = reinterpret_cast<const uint2*>(smem + C::OFF_Q)[(ks * NT8 + t) * 32 + lane];
     // per row pair (2 a, 2 a + 1) of each 8 rows: reference maximum (log2 units), sum over this thread's keys, scale of the weights
     float m[NT8][2], l[NT8][2], cw[NT8][2], qs[NT8][2], acc[C::MT][NT8][4];
 #pragma unroll
@@ -216,51 +233,56 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       for (int t = 0; t < NT8; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[j][t][e] = 0.0f;
+    // Places of this thread's chunks in a unit, whose rows begin at a multiple of 16: the swizzle of a row goes by its last bits.
+    // K: chunk a CPT + h of keys g and g + 8;  V: chunk g of keys 2 a + e and 2 a + e + 8.
+    uint32_t k_at[C::CPT], v_at[2];
+#pragma unroll
+    for (int h = 0; h < C::CPT; ++h) k_at[h] = g * C::BOXB + (((a * C::CPT + h) * 16) ^ ((C::BOXB == 128 ? g : (g >> 1) & 3) << 4));
+#pragma unroll
+    for (int e = 0; e < 2; ++e) v_at[e] = C::HALF_BYTES + (2 * a + e) * C::BOXB + ((g * (C::BOXB / 8)) ^ ((C::BOXB == 128 ? 2 * a + e : a) << 4));
 
-    for (int i = 0; i < nt; ++i) {
-      const int st = i % NS;
-      if (!mbar_wait(&mi.full[st], full_par(i / NS), abort_flag, prm.status, WF_FULL)) break;
-      const uint8_t* const stage = smem + st * C::STAGE_BYTES;
-#pragma unroll 1
-      for (int step = 0; step < C::STEPS; ++step) {
-        const int r0 = (step * C::WARPS + warp) * 16, key0 = (j0 + i) * KEYS + r0;
-        if (key0 >= n) continue;
-        const bool tail = key0 + 16 > n;
-        // ---- S^T, two chains of products
-        float s[2][NT8][4];
+    int st = warp / C::UNITS;                                    // stage and lap of the unit
+    uint32_t lap = 0;
+    for (int u = warp; u < nt * C::UNITS; u += C::WARPS) {
+      const int r0 = u % C::UNITS * 16, key0 = (j0 + u / C::UNITS) * KEYS + r0;
+      if (!mbar_wait(&mi.full[st], lap & 1u, abort_flag, prm.status, WF_FULL)) break;
+      if (key0 < n) {
+        const uint8_t* const unit = smem + st * C::STAGE_BYTES + r0 * C::BOXB;
+        const int left = n - key0;                               // entries of the unit, 16 or more: all
+        float sk0 = 1.0f, sk1 = 1.0f, sv0 = 1.0f, sv1 = 1.0f;
+        if constexpr (Q8) {
+          const float* const sc = reinterpret_cast<const float*>(smem + C::OFF_SCALE) + st * 2 * KEYS + r0 + g;
+          sk0 = sc[0]; sk1 = sc[8]; sv0 = sc[KEYS]; sv1 = sc[KEYS + 8];
+        }
+        // ---- S^T, in two chains of products
+        constexpr int CH = NT8 == 1 ? 2 : 1;
+        float s[CH][NT8][4];
 #pragma unroll
-        for (int t = 0; t < NT8; ++t)
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[0][t][e] = s[1][t][e] = 0.0f;
+          for (int t = 0; t < NT8; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[c][t][e] = 0.0f;
 #pragma unroll
         for (int b = 0; b < C::BOXES; ++b)
 #pragma unroll
           for (int h = 0; h < C::CPT; ++h) {
-            uint4 kr[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              uint32_t off = (r0 + g + 8 * u) * C::BOXB + (a * C::CPT + h) * 16;
-              off ^= ((off >> 7) & C::SWZ) << 4;
-              kr[u] = *reinterpret_cast<const uint4*>(stage + b * KEYS * C::BOXB + off);
-            }
-            const uint32_t x0[4] = {kr[0].x, kr[0].y, kr[0].z, kr[0].w}, x1[4] = {kr[1].x, kr[1].y, kr[1].z, kr[1].w};
+            const uint4 y0 = *reinterpret_cast<const uint4*>(unit + b * KEYS * C::BOXB + k_at[h]),
+                        y1 = *reinterpret_cast<const uint4*>(unit + b * KEYS * C::BOXB + k_at[h] + 8 * C::BOXB);
+            const uint32_t x0[4] = {y0.x, y0.y, y0.z, y0.w}, x1[4] = {y1.x, y1.y, y1.z, y1.w};
 #pragma unroll
             for (int t = 0; t < C::KPC; ++t) {
               const int ks = (b * C::CPT + h) * C::KPC + t;
               uint32_t a0, a1, a2, a3;
               if constexpr (Q8) {
-                const uint32_t y0 = flip_signs<FMT>(x0[t]), y1 = flip_signs<FMT>(x1[t]);
-                a0 = codes_to_half2<FMT, 0>(y0); a2 = codes_to_half2<FMT, 1>(y0);
-                a1 = codes_to_half2<FMT, 0>(y1); a3 = codes_to_half2<FMT, 1>(y1);
+                const uint32_t z0 = flip_signs<FMT>(x0[t]), z1 = flip_signs<FMT>(x1[t]);
+                a0 = codes_to_half2<FMT, 0>(z0); a2 = codes_to_half2<FMT, 1>(z0);
+                a1 = codes_to_half2<FMT, 0>(z1); a3 = codes_to_half2<FMT, 1>(z1);
               } else {
                 a0 = x0[2 * t]; a2 = x0[2 * t + 1]; a1 = x1[2 * t]; a3 = x1[2 * t + 1];
               }
 #pragma unroll
-              for (int c = 0; c < NT8; ++c) {
-                uint2 q;
-                if constexpr (Q_REGS) q = qf[ks][c]; else q = sq[(ks * NT8 + c) * 32];
-                mma16816<FMT>(s[ks & 1][c], a0, a1, a2, a3, q.x, q.y);
-              }
+              for (int c = 0; c < NT8; ++c) mma16816<FMT>(s[ks % CH][c], a0, a1, a2, a3, qf[ks][c].x, qf[ks][c].y);
             }
           }
         // ---- V of this thread: 4 keys (positions 2 a, 2 a + 1, 2 a + 8, 2 a + 9 of the 16)
@@ -268,56 +290,63 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 #pragma unroll
         for (int b = 0; b < C::BOXES; ++b)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int k = 2 * a + (u & 1) + 8 * (u >> 1);
-            uint32_t off = (r0 + k) * C::BOXB + g * (C::BOXB / 8);
-            off ^= ((off >> 7) & C::SWZ) << 4;
-            const uint8_t* const from = stage + C::HALF_BYTES + b * KEYS * C::BOXB + off;
+          for (int k = 0; k < 4; ++k) {
+            const uint8_t* const from = unit + b * KEYS * C::BOXB + v_at[k & 1] + (k >> 1) * 8 * C::BOXB;
             if constexpr (C::BOXB == 128) {
               const uint4 y = *reinterpret_cast<const uint4*>(from);
-              v[b][u][0] = y.x; v[b][u][1] = y.y; v[b][u][2] = y.z; v[b][u][3] = y.w;
+              v[b][k][0] = y.x; v[b][k][1] = y.y; v[b][k][2] = y.z; v[b][k][3] = y.w;
             } else {
               const uint2 y = *reinterpret_cast<const uint2*>(from);
-              v[b][u][0] = y.x; v[b][u][1] = y.y;
-            }
-            if (tail && key0 + k >= n) {                         // whatever stands behind the last entry, NaN included
-#pragma unroll
-              for (int z = 0; z < C::BOXB / 32; ++z) v[b][u][z] = 0;
+              v[b][k][0] = y.x; v[b][k][1] = y.y;
             }
           }
-        float sk0 = 1.0f, sk1 = 1.0f, sv0 = 1.0f, sv1 = 1.0f;
-        if constexpr (Q8) {
-          const float* const sc = reinterpret_cast<const float*>(smem + C::OFF_SCALE) + st * 2 * KEYS + r0 + g;
-          sk0 = sc[0]; sk1 = sc[8]; sv0 = sc[KEYS]; sv1 = sc[KEYS + 8];
+        // ---- logits; the last unit ends before its 16th key: whatever stands behind it, NaN included, must not count
+        float z[NT8][4];
+#pragma unroll
+        for (int t = 0; t < NT8; ++t)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[t][e] = (CH == 2 ? s[0][t][e] + s[CH - 1][t][e] : s[0][t][e]) * ((e < 2 ? sk0 : sk1) * qs[t][e & 1]);
+        if (left < 16) {
+#pragma unroll
+          for (int t = 0; t < NT8; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (g + (e < 2 ? 0 : 8) >= left) z[t][e] = -INFINITY;
+          if (g >= left) sv0 = 0.0f;
+          if (g + 8 >= left) sv1 = 0.0f;
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (2 * a + (k & 1) + 8 * (k >> 1) >= left)
+#pragma unroll
+              for (int b = 0; b < C::BOXES; ++b)
+#pragma unroll
+                for (int y = 0; y < C::BOXB / 32; ++y) v[b][k][y] = 0;
         }
-        const bool out0 = tail && key0 + g >= n, out1 = tail && key0 + g + 8 >= n;
         // ---- probabilities
         uint32_t pb[NT8][2];
 #pragma unroll
         for (int t = 0; t < NT8; ++t) {
-          float z[4], p[4], w[4];
-          bool raise = false;
+          float p[4], w[4], over = -INFINITY, heavy = 0.0f;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            z[e] = (s[0][t][e] + s[1][t][e]) * ((e < 2 ? sk0 : sk1) * qs[t][e & 1]);
-            if (e < 2 ? out0 : out1) z[e] = -INFINITY;
-            p[e] = fast_exp2(z[e] - m[t][e & 1]);
-            raise |= z[e] > m[t][e & 1] + 8.0f;
+            const float above = z[t][e] - m[t][e & 1];
+            over = fmaxf(over, above);
+            p[e] = fast_exp2(above);
             w[e] = p[e];
             if constexpr (Q8) {
               w[e] = p[e] * ((e < 2 ? sv0 : sv1) * cw[t][e & 1]);
-              raise |= !(w[e] <= 32768.0f);
+              heavy = fmaxf(heavy, w[e]);
             }
           }
-          if (__any_sync(0xFFFFFFFFu, raise)) {                  // rare after the first keys
+          if (__any_sync(0xFFFFFFFFu, over > 8.0f || heavy > 32768.0f)) {          // rare after the first keys
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float top = fmaxf(m[t][e], max_over_keys(fmaxf(z[e], z[2 + e])));
+              const float top = fmaxf(m[t][e], max_over_keys(fmaxf(z[t][e], z[t][2 + e])));
               float f = fast_exp2(m[t][e] - top);
               m[t][e] = top;
               l[t][e] *= f;
-              p[e] = fast_exp2(z[e] - top);
-              p[2 + e] = fast_exp2(z[2 + e] - top);
+              p[e] = fast_exp2(z[t][e] - top);
+              p[2 + e] = fast_exp2(z[t][2 + e] - top);
               w[e] = p[e]; w[2 + e] = p[2 + e];
               if constexpr (Q8) {                                // cw = 1024 / (largest weight so far)
                 const float before = f * (1024.0f / cw[t][e]);
@@ -333,10 +362,6 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
           }
           l[t][0] += p[0] + p[2];
           l[t][1] += p[1] + p[3];
-          if (Q8 && tail) {                                      // scales behind the last entry may be anything
-            if (out0) w[0] = w[1] = 0.0f;
-            if (out1) w[2] = w[3] = 0.0f;
-          }
           pb[t][0] = transpose8x8(pack_p<FMT>(w[0], w[1]));
           pb[t][1] = transpose8x8(pack_p<FMT>(w[2], w[3]));
         }
@@ -371,6 +396,8 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&mi.empty[st]);
+      st += (u + C::WARPS) / C::UNITS - u / C::UNITS;
+      if (st >= NS) { st -= NS; ++lap; }
     }
     // ---- what this warp has: sums over its threads' keys, statistics; then, the ring being idle, O
 #pragma unroll
@@ -397,7 +424,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
   }
   __syncthreads();
-  // ---- the warps' results added up
+  // ---- the warps' results added up, into the first warp's place or the slot
   for (int e = tid; e < n_rows * (D / 4); e += C::THREADS) {
     const int r = e / (D / 4), c = e % (D / 4);
     float top = -FLT_MAX, sum = 0.0f;
@@ -413,44 +440,108 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
     }
     const size_t at = part0 + (size_t)r * prm.n_slots;
-    reinterpret_cast<float4*>(prm.part_o + at * D)[c] = o;
-    if (c == 0) prm.part_ml[at] = sum == 0.0f ? make_float2(-INFINITY, 0.0f) : make_float2(top, sum);
+    const float2 ml = sum == 0.0f ? make_float2(-INFINITY, 0.0f) : make_float2(top, sum);
+    if (finish) {
+      reinterpret_cast<float4*>(smem)[r * (D / 4) + c] = o;
+      if (c == 0) mi.all[r] = ml;
+    } else {
+      reinterpret_cast<float4*>(prm.part_o + at * D)[c] = o;
+      if (c == 0) prm.part_ml[at] = ml;
+    }
   }
+  }
+  if (!finish) return;
+
+  // ---- the splits' results, the slots in memory and the new tokens' keys: a warp per row, the rows dealt out over the cluster
+  if (prm.n_split > 1) cluster_sync_all(); else __syncthreads();
+  const int G = prm.q.Hq / prm.q.Hkv;
+  for (int r = split + prm.n_split * warp; r < n_rows; r += prm.n_split * (C::WARPS + 1)) {
+    const int row = row0 + r, bi = row / G, i = bi % prm.q.w;
+    RowSum<D> sum;
+    float2 mine = make_float2(-INFINITY, 0.0f);
+    if (lane < prm.n_split) {
+      float y[2];
+      ld_cluster<2>(map_to_cta(&mi.all[r], lane), y);
+      mine = make_float2(y[0], y[1]);
+    }
+    sum.join(mine, prm.n_split, [&](int s, float (&y)[E]) { ld_cluster<E>(map_to_cta(reinterpret_cast<const float*>(smem) + r * D + lane * E, s), y); });
+    const size_t slots = ((size_t)hkv * prm.total_rows + row) * fin.n_slots;
+    sum.join_slots(fin.part_ml + slots, fin.part_o + slots * D, fin.n_slots, 0, 1, lane);
+    if (fin.k_win != nullptr) {
+      uint32_t y[E / 2];
+      float q[E];
+#pragma unroll
+      for (int e = 0; e < E / 2; ++e) y[e] = reinterpret_cast<const uint32_t*>(smem + C::OFF_ROWS)[r * (D / 2) + lane * (E / 2) + e];
+      RowSum<D>::unpack(y, q);
+      sum.join_window(fin, q, hkv, bi / prm.q.w, i, 0, 1, lane);
+    }
+    sum.store(fin, hkv * G + row % G, bi, lane);
+  }
+  if (prm.n_split > 1) cluster_sync_all();                       // no CTA exits while another may read its shared memory
 }
 
 namespace {
 
-template <int D, int FMT, int NT8>
-cudaError_t few_t(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, cudaStream_t st) {
-  using C = Few<D, FMT, NT8>;
+template <class C>
+cudaError_t prepare(int cluster) {
   constexpr int SMEM = C::OFF_MISC + (int)sizeof(FewMisc<C>);
   static_assert(C::CTAS * (SMEM + 1024) <= 233472, "CTAs per SM");
   if (cudaError_t e = cudaFuncSetAttribute(cache_few_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM); e != cudaSuccess) return e;
-  return launch_chained(cache_few_kernel<C>, dim3((unsigned)((long long)p.seqs * p.Hkv * p.n_rg * p.n_split)), dim3(C::THREADS), SMEM, st, 1, tm_k, tm_v, p);
+  return cluster > 8 ? cudaFuncSetAttribute(cache_few_kernel<C>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : cudaSuccess;
+}
+template <class C>
+cudaError_t few_t(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, cudaStream_t st) {
+  const int cluster = finish ? p.n_split : 1;
+  if (cudaError_t e = prepare<C>(cluster); e != cudaSuccess) return e;
+  return launch_chained(cache_few_kernel<C>, dim3((unsigned)((long long)p.seqs * p.Hkv * p.n_rg * p.n_split)), dim3(C::THREADS),
+                        C::OFF_MISC + sizeof(FewMisc<C>), st, cluster, tm_k, tm_v, p, finish ? *finish : CacheMerge{}, finish != nullptr ? 1 : 0);
 }
 template <int D, int FMT>
-cudaError_t few_n(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, cudaStream_t st) {
-  const int n = few_rows(p.rows);
-  return n == 8 ? few_t<D, FMT, 1>(tm_k, tm_v, p, st) : n == 16 ? few_t<D, FMT, 2>(tm_k, tm_v, p, st) : few_t<D, FMT, 4>(tm_k, tm_v, p, st);
+cudaError_t few_n(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool deep, cudaStream_t st) {
+  if (few_rows(p.rows) == 8)
+    return deep ? few_t<Few<D, FMT, 1, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT, 1, false>>(tm_k, tm_v, p, finish, st);
+  return deep ? few_t<Few<D, FMT, 2, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT, 2, false>>(tm_k, tm_v, p, finish, st);
 }
 template <int D>
-cudaError_t few_d(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, int format, cudaStream_t st) {
-  return format == FMT_INT8 ? few_n<D, FMT_INT8>(tm_k, tm_v, p, st) : format == FMT_E4M3 ? few_n<D, FMT_E4M3>(tm_k, tm_v, p, st) : few_n<D, FMT_BF16>(tm_k, tm_v, p, st);
+cudaError_t few_d(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool deep, int format, cudaStream_t st) {
+  return format == FMT_INT8   ? few_n<D, FMT_INT8>(tm_k, tm_v, p, finish, deep, st)
+         : format == FMT_E4M3 ? few_n<D, FMT_E4M3>(tm_k, tm_v, p, finish, deep, st)
+                              : few_n<D, FMT_BF16>(tm_k, tm_v, p, finish, deep, st);
 }
-template <int D, int FMT>
-int keys_t(int n) { return n == 8 ? Few<D, FMT, 1>::KEYS : n == 16 ? Few<D, FMT, 2>::KEYS : Few<D, FMT, 4>::KEYS; }
+template <class C>
+int clusters_t(int n_split) {
+  if (prepare<C>(n_split) != cudaSuccess) { cudaGetLastError(); return 0; }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)n_split);
+  cfg.blockDim = dim3(C::THREADS);
+  cfg.dynamicSmemBytes = C::OFF_MISC + sizeof(FewMisc<C>);
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {(unsigned)n_split, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  if (cudaOccupancyMaxActiveClusters(&n, cache_few_kernel<C>, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
+  return n;
+}
 
 }  // namespace
 
-int few_rows(int rows) { return rows <= 8 ? 8 : rows <= 16 ? 16 : 32; }
-int few_ctas_per_sm(int rows) { return few_rows(rows) <= 16 ? 2 : 1; }
-int few_keys(int format, int d, int rows) {
-  const int n = few_rows(rows);
-  if (format == FMT_BF16) return d == 128 ? keys_t<128, FMT_BF16>(n) : keys_t<64, FMT_BF16>(n);
-  return d == 128 ? keys_t<128, FMT_INT8>(n) : keys_t<64, FMT_INT8>(n);
+int few_rows(int rows) { return rows <= 8 ? 8 : 16; }
+int few_warps(int rows, bool deep) {
+  if (few_rows(rows) == 8) return deep ? Few<128, FMT_INT8, 1, true>::WARPS : Few<128, FMT_INT8, 1, false>::WARPS;
+  return deep ? Few<128, FMT_INT8, 2, true>::WARPS : Few<128, FMT_INT8, 2, false>::WARPS;
 }
-cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, int format, int d, cudaStream_t st) {
-  return d == 128 ? few_d<128>(tm_k, tm_v, p, format, st) : few_d<64>(tm_k, tm_v, p, format, st);
+int few_clusters(int n_split, bool deep) {          // all builds take an SM's shared memory in one or two parts
+  return deep ? clusters_t<Few<128, FMT_INT8, 2, true>>(n_split) : clusters_t<Few<128, FMT_INT8, 2, false>>(n_split);
+}
+int few_keys(int format, int d) {
+  if (format == FMT_BF16) return d == 128 ? Few<128, FMT_BF16, 1, false>::KEYS : Few<64, FMT_BF16, 1, false>::KEYS;
+  return d == 128 ? Few<128, FMT_INT8, 1, false>::KEYS : Few<64, FMT_INT8, 1, false>::KEYS;
+}
+cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool deep, int format,
+                             int d, cudaStream_t st) {
+  return d == 128 ? few_d<128>(tm_k, tm_v, p, finish, deep, format, st) : few_d<64>(tm_k, tm_v, p, finish, deep, format, st);
 }
 
 }  // namespace pc

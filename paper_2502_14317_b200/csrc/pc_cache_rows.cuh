@@ -9,16 +9,17 @@
 
 namespace pc {
 
-// Out of line: the arithmetic is long, and cold code costs a short kernel more than the calls do.
+// Out of line: cold code costs a short kernel more than the calls do.
 static __device__ __noinline__ float row_freq(float theta, float exponent) { return powf(theta, exponent); }
-static __device__ __noinline__ float2 row_angle(float freq, long long pos, float theta, float exponent) {
-  if (pos < (1 << 15)) {
-    const float a = __fmul_rn((float)pos, freq);
-    return make_float2(cosf(a), sinf(a));
-  }
+static __device__ __noinline__ float2 row_angle_far(long long pos, float theta, float exponent) {
   double c, s;
   sincos((double)pos * pow((double)theta, (double)exponent), &s, &c);
   return make_float2((float)c, (float)s);
+}
+static __device__ __noinline__ float2 row_angle(float freq, long long pos, float theta, float exponent) {
+  if (pos >= (1 << 15) || pos < 0) return row_angle_far(pos, theta, exponent);
+  const float a = __fmul_rn((float)pos, freq);
+  return make_float2(cosf(a), sinf(a));
 }
 
 // Angles of a token's pairs: lanes l and l + 16 hold elements of the same E pairs and compute half of them each.
