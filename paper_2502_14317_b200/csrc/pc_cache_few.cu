@@ -35,8 +35,6 @@ struct Few {
   static constexpr int UNITS = ROWB == 256 ? 4 : 8;             // of a stage
   static constexpr int KEYS = 16 * UNITS, HALF_BYTES = KEYS * ROWB, STAGE_BYTES = 2 * HALF_BYTES;
   static constexpr int NS = 196608 / CTAS / STAGE_BYTES;
-  // a warp that waits for its next unit's stage is less than a lap of the ring ahead of the copies
-  static_assert((WARPS + UNITS - 1) / UNITS < NS, "parity of a stage");
   static constexpr int N = 8 * NT8, KST = D / 16, MT = D / 16;
   static constexpr int THREADS = 32 * (WARPS + 1);
   static constexpr int OFF_SCALE = NS * STAGE_BYTES, OFF_Q = OFF_SCALE + (EB == 1 ? NS * 2 * KEYS * 4 : 0), OFF_ROWS = OFF_Q + KST * NT8 * 256,
@@ -115,7 +113,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   const int hkv = x % prm.Hkv, seq = x / prm.Hkv;
 
   if (tid == C::WARPS * 32) {
-    for (int i = 0; i < NS; ++i) { mbar_init(&mi.full[i], Q8 ? 33 : 1); mbar_init(&mi.empty[i], C::UNITS); }
+    for (int i = 0; i < NS; ++i) { mbar_init(&mi.full[i], Q8 ? 33 : 1); mbar_init(&mi.empty[i], C::WARPS); }
     mi.abort_flag = 0;
     mi.wait_kcycles = prm.wait_kcycles;
     fence_mbar_init();
@@ -241,12 +239,15 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 #pragma unroll
     for (int e = 0; e < 2; ++e) v_at[e] = C::HALF_BYTES + (2 * a + e) * C::BOXB + ((g * (C::BOXB / 8)) ^ ((C::BOXB == 128 ? 2 * a + e : a) << 4));
 
-    int st = warp / C::UNITS;                                    // stage and lap of the unit
+    // The units go round among the warps.  A warp waits for every tile and leaves every tile, with a unit of its own there or not: copies may
+    // land out of order, and the parity of a barrier tells a lap of the ring only from the one before it.
+    int st = 0, u = warp;
     uint32_t lap = 0;
-    for (int u = warp; u < nt * C::UNITS; u += C::WARPS) {
-      const int r0 = u % C::UNITS * 16, key0 = (j0 + u / C::UNITS) * KEYS + r0;
+    for (int i = 0; i < nt; ++i) {
       if (!mbar_wait(&mi.full[st], lap & 1u, abort_flag, prm.status, WF_FULL)) break;
-      if (key0 < n) {
+      for (; u < (i + 1) * C::UNITS; u += C::WARPS) {
+        const int r0 = (u - i * C::UNITS) * 16, key0 = (j0 + i) * KEYS + r0;
+        if (key0 >= n) continue;
         const uint8_t* const unit = smem + st * C::STAGE_BYTES + r0 * C::BOXB;
         const int left = n - key0;                               // entries of the unit, 16 or more: all
         float sk0 = 1.0f, sk1 = 1.0f, sv0 = 1.0f, sv1 = 1.0f;
@@ -396,8 +397,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&mi.empty[st]);
-      st += (u + C::WARPS) / C::UNITS - u / C::UNITS;
-      if (st >= NS) { st -= NS; ++lap; }
+      if (++st == NS) { st = 0; ++lap; }
     }
     // ---- what this warp has: sums over its threads' keys, statistics; then, the ring being idle, O
 #pragma unroll
