@@ -22,7 +22,7 @@ struct KvWrite {
   int* pos_out;                                  // gather: [Hkv,n] or null
   int* status;
 };
-cudaError_t launch_kv_quantize(const KvWrite& w, int format, int d, bool gather, int sm_count, cudaStream_t st);
+cudaError_t launch_kv_quantize(const KvWrite& w, int format, int d, bool gather, cudaStream_t st);
 
 struct KvRead {
   const uint8_t *k, *v;
@@ -31,8 +31,9 @@ struct KvRead {
   int B, Hkv, n, at0;
   const int* at;
   void *k_out, *v_out;
+  bool sectors;                                  // both aligned to 32 bytes
 };
-cudaError_t launch_kv_dequantize(const KvRead& r, int format, int d, int sm_count, cudaStream_t st);
+cudaError_t launch_kv_dequantize(const KvRead& r, int format, int d, cudaStream_t st);
 
 // Queries of pc_cache_attn as rows of a kv-head: row (b * w + i) * G + g is q[b, i, hkv * G + g, :], rotated and rounded to bf16
 // (theta 0: as it is), in memory as rows[hkv][row][d].  The kernel for few rows makes them where it needs them and leaves them
@@ -79,13 +80,11 @@ struct CachePhase {
 };
 // Few rows (pc_cache_few.cu), groups of 8 or 16.  finish null: every split leaves its slot.  Else the splits of a (sequence, kv-head, row
 // group) are the CTAs of a cluster, and the kernel finishes its rows: its splits' results, finish's slots and the new tokens' keys.
-// deep: one CTA per SM with twice the stages and warps, else two.
+// brief: the build for many sequences with few entries.
 // maps of the cache's keys and values: boxes of few_keys() entries
-int few_keys(int format, int d);                 // keys of a stage
+int few_keys(int format, int d, bool brief);     // keys of a stage
 int few_rows(int rows);                          // rows of a row group
-int few_warps(int rows, bool deep);              // warps that take keys, 16 at a time
-int few_clusters(int n_split, bool deep);        // clusters of n_split CTAs that the current device runs at a time
-cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool deep, int format,
+cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool brief, int format,
                              int d, cudaStream_t st);
 
 // The same phase for more than 32 rows of one sequence (pc_cache_wide.cu), blocks of 128 rows.

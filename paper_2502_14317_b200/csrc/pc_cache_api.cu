@@ -4,7 +4,6 @@
 #include "pc_kernels.h"
 #include "pc_tmap.h"
 
-#include <atomic>
 #include <cmath>
 
 namespace {
@@ -49,14 +48,13 @@ int32_t pc_kv_quantize(const pc_kv_cache* cache, const void* k_src, const int64_
   if (at == nullptr && (at0 < 0 || (int64_t)at0 + n > cache->capacity)) return PC_ERR_INVALID_ARG;
   pc::KvWrite w = {};
   if (!strides(k_stride, n, cache->Hkv, cache->d, w.k_stride) || !strides(v_stride, n, cache->Hkv, cache->d, w.v_stride)) return PC_ERR_INVALID_ARG;
-  const int sms = pc::sm100_count();
-  if (sms == 0) return PC_ERR_UNSUPPORTED;
+  if (pc::sm100_count() == 0) return PC_ERR_UNSUPPORTED;
   w.k_src = k_src; w.v_src = v_src;
   w.k = static_cast<uint8_t*>(cache->k); w.v = static_cast<uint8_t*>(cache->v);
   w.k_scale = cache->k_scale; w.v_scale = cache->v_scale;
   w.capacity = cache->capacity;
   w.B = cache->B; w.Hkv = cache->Hkv; w.n = n; w.at0 = at0; w.at = at; w.status = status_word;
-  return launched(pc::launch_kv_quantize(w, cache->format, cache->d, false, sms, static_cast<cudaStream_t>(stream)));
+  return launched(pc::launch_kv_quantize(w, cache->format, cache->d, false, static_cast<cudaStream_t>(stream)));
 }
 
 int32_t pc_gather_kv_quantize(const void* k_src, const void* v_src, const int64_t* kv_stride, const int32_t* kept, const int32_t* idx,
@@ -69,25 +67,23 @@ int32_t pc_gather_kv_quantize(const void* k_src, const void* v_src, const int64_
     if (kv_stride[i] <= 0 || kv_stride[i] % 8 != 0) return PC_ERR_INVALID_ARG;
     w.k_stride[i] = w.v_stride[i] = kv_stride[i];
   }
-  const int sms = pc::sm100_count();
-  if (sms == 0) return PC_ERR_UNSUPPORTED;
+  if (pc::sm100_count() == 0) return PC_ERR_UNSUPPORTED;
   w.k_src = k_src; w.v_src = v_src;
   w.k = static_cast<uint8_t*>(cache->k); w.v = static_cast<uint8_t*>(cache->v);
   w.k_scale = cache->k_scale; w.v_scale = cache->v_scale;
   w.capacity = cache->capacity;
   w.B = 1; w.Hkv = cache->Hkv; w.n = m * k;
   w.kept = kept; w.idx = idx; w.per_chunk = k; w.pos_out = pos_out;
-  return launched(pc::launch_kv_quantize(w, cache->format, cache->d, true, sms, static_cast<cudaStream_t>(stream)));
+  return launched(pc::launch_kv_quantize(w, cache->format, cache->d, true, static_cast<cudaStream_t>(stream)));
 }
 
 int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0, const int32_t* at, void* k_out, void* v_out, void* stream) {
   if (int32_t rc = check_cache(cache, true); rc != PC_OK) return rc;
   if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16) || n < 1) return PC_ERR_INVALID_ARG;
-  const int sms = pc::sm100_count();
-  if (sms == 0) return PC_ERR_UNSUPPORTED;
+  if (pc::sm100_count() == 0) return PC_ERR_UNSUPPORTED;
   const pc::KvRead r = {static_cast<const uint8_t*>(cache->k), static_cast<const uint8_t*>(cache->v), cache->k_scale, cache->v_scale,
-                        cache->capacity, cache->B, cache->Hkv, n, at0, at, k_out, v_out};
-  return launched(pc::launch_kv_dequantize(r, cache->format, cache->d, sms, static_cast<cudaStream_t>(stream)));
+                        cache->capacity, cache->B, cache->Hkv, n, at0, at, k_out, v_out, aligned(k_out, 32) && aligned(v_out, 32)};
+  return launched(pc::launch_kv_dequantize(r, cache->format, cache->d, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"
@@ -95,7 +91,7 @@ int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0, const
 // ------------------------------------------------------------------------------------ attention over shared and own caches
 namespace {
 
-struct PhasePlan { bool wide, pair, deep, finish; int alt, n_rg, n_split; };
+struct PhasePlan { bool wide, pair, brief, finish; int alt, n_rg, n_split; };
 struct CachePlan {
   PhasePlan prefix, own;
   int n_slots;                                   // results of a row in memory
@@ -105,39 +101,30 @@ struct CachePlan {
   size_t off_counter, off_rows, off_halves, off_scale, off_ml, off_o, total;
 };
 
-// Clusters of n CTAs of the kernel for few rows that the current device runs at a time (asked once per device).
-int few_fit(int n, bool deep) {
-  static std::atomic<int> known[64][2][17];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-  std::atomic<int>& k = known[dev][deep][n];
-  int v = k.load(std::memory_order_relaxed);
-  if (v == 0) k.store(v = pc::few_clusters(n, deep) + 1, std::memory_order_relaxed);
-  return v - 1;
-}
-
-// Splits of the keys, and whether the kernel finishes its rows itself (the last phase; up to 16 splits, the CTAs of a cluster)
-// or leaves slots for the merge.  Least time by a model in microseconds: rounds of the grid x (5 for the queries, the first unit and
-// the join + its units, 0.65 each for a warp, or their bytes at the CTA's share of the memory's rate), and 4 for the merge's launch.
+// Splits of the keys, and whether the kernel finishes its rows itself (the last phase; up to 8 splits, the CTAs of a cluster)
+// or leaves slots for the merge.  Least time by a model in microseconds: rounds of the grid, two CTAs per SM, x (7 for the queries, the
+// first unit and the join + its tiles, at a unit in 0.9 (8 rows) or 1.15 for a warp, or at the CTA's share of the memory's rate), and for
+// slots 1 + 0.1 a split for writing and merging them.
 PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, bool last, int sm_count) {
   PhasePlan p = {};
-  const int per = pc::few_rows((int)rows), keys = pc::few_keys(format, d);
+  const int per = pc::few_rows((int)rows);
   p.n_rg = (int)((rows + per - 1) / per);
-  const int tiles = (n_keys + keys - 1) / keys;
-  const double items = (double)seqs * Hkv * p.n_rg, tile_us = 2.0 * keys * d * (format == PC_KV_BF16 ? 2 : 1) / 6.5e6;
-  double least = -1.0;
+  const double items = (double)seqs * Hkv * p.n_rg;
+  p.brief = items > 2.0 * sm_count && n_keys <= 512;
+  const int keys = pc::few_keys(format, d, p.brief), tiles = (n_keys + keys - 1) / keys;
   p.n_split = 1;
-  for (int finish = last ? 1 : 0; finish >= 0; --finish)
-    for (int deep = 0; deep <= 1; ++deep) {
-      const double alone = 0.65 * (keys / 16) / pc::few_warps((int)rows, deep != 0);
-      for (int s = 1; s <= (finish ? 16 : 64) && s <= tiles; ++s) {
-        const double fit = finish && s > 1 ? few_fit(s, deep != 0) : (double)(deep ? 1 : 2) * sm_count / s;
-        if (fit < 1.0) continue;
-        const double rounds = std::ceil(items / fit), active = (items < fit ? items : fit) * s;
-        const double cost = rounds * (5.0 + (tile_us * active > alone ? tile_us * active : alone) * std::ceil((double)tiles / s)) + (finish ? 0.0 : 4.0);
-        if (least < 0.0 || cost < least) { least = cost; p.n_split = s; p.deep = deep != 0; p.finish = finish != 0; }
-      }
-    }
+  p.finish = last;
+  if (p.brief) return p;
+  const double tile_us = 2.0 * keys * d * (format == PC_KV_BF16 ? 2 : 1) / 6.5e6, alone = keys / 16 * (per == 8 ? 0.9 / 7 : 1.15 / 5);
+  double least = -1.0;
+  for (int s = 1; s <= 64 && s <= tiles; ++s) {
+    const bool finish = last && s <= 8;
+    const double fit = std::floor(2.0 * sm_count / s);
+    const double rounds = std::ceil(items / fit), active = (items < fit ? items : fit) * s;
+    const double cost = rounds * (7.0 + (tile_us * active > alone ? tile_us * active : alone) * std::ceil((double)tiles / s)) +
+                        (finish ? 0.0 : 1.0 + 0.1 * s);
+    if (least < 0.0 || cost < least) { least = cost; p.n_split = s; p.finish = finish; }
+  }
   return p;
 }
 
@@ -187,6 +174,8 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     if ((own ? a->B : 1ll) * a->Hkv * ph.n_rg * ph.n_split > 0x7FFFFFFF) return PC_ERR_UNSUPPORTED;
     if (!ph.finish) p.n_slots += ph.n_split;
     p.finished |= ph.finish;
+    // more than a round of CTAs: cheaper than each of them rotating its own
+    if (!ph.wide && (own ? a->B : 1.0) * a->Hkv * ph.n_rg * ph.n_split > 2.0 * sm_count) p.rows = true;
   }
   if (p.n_slots == 0 && !p.finished) p.rows = true;
   size_t off = 0;
@@ -297,8 +286,8 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
       continue;
     }
     CUtensorMap tm_k, tm_v;
-    if (!cache_maps(c, n, pc::few_keys(c->format, c->d), &tm_k, &tm_v)) { launched(e); return PC_ERR_CUDA; }
-    e = pc::launch_cache_few(tm_k, tm_v, p, ph.finish ? &merge : nullptr, ph.deep, c->format, c->d, st);
+    if (!cache_maps(c, n, pc::few_keys(c->format, c->d, ph.brief), &tm_k, &tm_v)) { launched(e); return PC_ERR_CUDA; }
+    e = pc::launch_cache_few(tm_k, tm_v, p, ph.finish ? &merge : nullptr, ph.brief, c->format, c->d, st);
     slot += ph.n_split;
   }
   if (e != cudaSuccess || plan.finished) return launched(e);

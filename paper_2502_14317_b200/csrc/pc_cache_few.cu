@@ -25,16 +25,17 @@ namespace pc {
 
 namespace {
 
-template <int D_, int FMT_, int NT8_, bool DEEP_>
+// SHORT: four CTAs per SM (16 rows: three) of three consumer warps and stages of half the size, for many sequences with few entries
+template <int D_, int FMT_, int NT8_, bool SHORT_>
 struct Few {
   static constexpr int D = D_, FMT = FMT_, NT8 = NT8_;
   static constexpr int EB = FMT == FMT_BF16 ? 2 : 1;            // bytes of an element
   static constexpr int ROWB = D * EB, BOXES = ROWB > 128 ? 2 : 1, BOXB = ROWB / BOXES, EPB = BOXB / EB;
   // Consumer warps: with the producers 16 warps an SM, 128 registers a thread, or 12 and 168.
-  static constexpr int CTAS = DEEP_ ? 1 : 2, WARPS = (NT8 == 1 ? 16 : 12) / CTAS - 1;
-  static constexpr int UNITS = ROWB == 256 ? 4 : 8;             // of a stage
+  static constexpr int CTAS = SHORT_ ? (NT8 == 1 ? 4 : 3) : 2, WARPS = (NT8 == 1 ? 16 : 12) / CTAS - 1;
+  static constexpr int UNITS = (ROWB == 256 ? 4 : 8) / (SHORT_ && ROWB != 64 ? 2 : 1);             // of a stage
   static constexpr int KEYS = 16 * UNITS, HALF_BYTES = KEYS * ROWB, STAGE_BYTES = 2 * HALF_BYTES;
-  static constexpr int NS = 196608 / CTAS / STAGE_BYTES;
+  static constexpr int NS = (SHORT_ ? 49152 : 98304) / STAGE_BYTES;
   static constexpr int N = 8 * NT8, KST = D / 16, MT = D / 16;
   static constexpr int THREADS = 32 * (WARPS + 1);
   static constexpr int OFF_SCALE = NS * STAGE_BYTES, OFF_Q = OFF_SCALE + (EB == 1 ? NS * 2 * KEYS * 4 : 0), OFF_ROWS = OFF_Q + KST * NT8 * 256,
@@ -483,65 +484,38 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
 namespace {
 
 template <class C>
-cudaError_t prepare(int cluster) {
+cudaError_t few_t(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, cudaStream_t st) {
   constexpr int SMEM = C::OFF_MISC + (int)sizeof(FewMisc<C>);
   static_assert(C::CTAS * (SMEM + 1024) <= 233472, "CTAs per SM");
   if (cudaError_t e = cudaFuncSetAttribute(cache_few_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM); e != cudaSuccess) return e;
-  return cluster > 8 ? cudaFuncSetAttribute(cache_few_kernel<C>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : cudaSuccess;
-}
-template <class C>
-cudaError_t few_t(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, cudaStream_t st) {
-  const int cluster = finish ? p.n_split : 1;
-  if (cudaError_t e = prepare<C>(cluster); e != cudaSuccess) return e;
-  return launch_chained(cache_few_kernel<C>, dim3((unsigned)((long long)p.seqs * p.Hkv * p.n_rg * p.n_split)), dim3(C::THREADS),
-                        C::OFF_MISC + sizeof(FewMisc<C>), st, cluster, tm_k, tm_v, p, finish ? *finish : CacheMerge{}, finish != nullptr ? 1 : 0);
+  return launch_chained(cache_few_kernel<C>, dim3((unsigned)((long long)p.seqs * p.Hkv * p.n_rg * p.n_split)), dim3(C::THREADS), SMEM, st,
+                        finish ? p.n_split : 1, tm_k, tm_v, p, finish ? *finish : CacheMerge{}, finish != nullptr ? 1 : 0);
 }
 template <int D, int FMT>
-cudaError_t few_n(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool deep, cudaStream_t st) {
+cudaError_t few_n(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool brief, cudaStream_t st) {
   if (few_rows(p.rows) == 8)
-    return deep ? few_t<Few<D, FMT, 1, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT, 1, false>>(tm_k, tm_v, p, finish, st);
-  return deep ? few_t<Few<D, FMT, 2, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT, 2, false>>(tm_k, tm_v, p, finish, st);
+    return brief ? few_t<Few<D, FMT, 1, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT, 1, false>>(tm_k, tm_v, p, finish, st);
+  return brief ? few_t<Few<D, FMT, 2, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT, 2, false>>(tm_k, tm_v, p, finish, st);
 }
 template <int D>
-cudaError_t few_d(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool deep, int format, cudaStream_t st) {
-  return format == FMT_INT8   ? few_n<D, FMT_INT8>(tm_k, tm_v, p, finish, deep, st)
-         : format == FMT_E4M3 ? few_n<D, FMT_E4M3>(tm_k, tm_v, p, finish, deep, st)
-                              : few_n<D, FMT_BF16>(tm_k, tm_v, p, finish, deep, st);
+cudaError_t few_d(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool brief, int format, cudaStream_t st) {
+  return format == FMT_INT8   ? few_n<D, FMT_INT8>(tm_k, tm_v, p, finish, brief, st)
+         : format == FMT_E4M3 ? few_n<D, FMT_E4M3>(tm_k, tm_v, p, finish, brief, st)
+                              : few_n<D, FMT_BF16>(tm_k, tm_v, p, finish, brief, st);
 }
-template <class C>
-int clusters_t(int n_split) {
-  if (prepare<C>(n_split) != cudaSuccess) { cudaGetLastError(); return 0; }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)n_split);
-  cfg.blockDim = dim3(C::THREADS);
-  cfg.dynamicSmemBytes = C::OFF_MISC + sizeof(FewMisc<C>);
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim = {(unsigned)n_split, 1, 1};
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  int n = 0;
-  if (cudaOccupancyMaxActiveClusters(&n, cache_few_kernel<C>, &cfg) != cudaSuccess) { cudaGetLastError(); return 0; }
-  return n;
+template <bool SHORT>
+int keys_t(int format, int d) {
+  if (format == FMT_BF16) return d == 128 ? Few<128, FMT_BF16, 1, SHORT>::KEYS : Few<64, FMT_BF16, 1, SHORT>::KEYS;
+  return d == 128 ? Few<128, FMT_INT8, 1, SHORT>::KEYS : Few<64, FMT_INT8, 1, SHORT>::KEYS;
 }
 
 }  // namespace
 
 int few_rows(int rows) { return rows <= 8 ? 8 : 16; }
-int few_warps(int rows, bool deep) {
-  if (few_rows(rows) == 8) return deep ? Few<128, FMT_INT8, 1, true>::WARPS : Few<128, FMT_INT8, 1, false>::WARPS;
-  return deep ? Few<128, FMT_INT8, 2, true>::WARPS : Few<128, FMT_INT8, 2, false>::WARPS;
-}
-int few_clusters(int n_split, bool deep) {          // all builds take an SM's shared memory in one or two parts
-  return deep ? clusters_t<Few<128, FMT_INT8, 2, true>>(n_split) : clusters_t<Few<128, FMT_INT8, 2, false>>(n_split);
-}
-int few_keys(int format, int d) {
-  if (format == FMT_BF16) return d == 128 ? Few<128, FMT_BF16, 1, false>::KEYS : Few<64, FMT_BF16, 1, false>::KEYS;
-  return d == 128 ? Few<128, FMT_INT8, 1, false>::KEYS : Few<64, FMT_INT8, 1, false>::KEYS;
-}
-cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool deep, int format,
+int few_keys(int format, int d, bool brief) { return brief ? keys_t<true>(format, d) : keys_t<false>(format, d); }
+cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool brief, int format,
                              int d, cudaStream_t st) {
-  return d == 128 ? few_d<128>(tm_k, tm_v, p, finish, deep, format, st) : few_d<64>(tm_k, tm_v, p, finish, deep, format, st);
+  return d == 128 ? few_d<128>(tm_k, tm_v, p, finish, brief, format, st) : few_d<64>(tm_k, tm_v, p, finish, brief, format, st);
 }
 
 }  // namespace pc

@@ -6,6 +6,7 @@
 #include "pc_cache.h"
 #include "pc_kernels.h"
 #include "pc_kv8.cuh"
+#include "pc_sm100.cuh"
 
 namespace pc {
 
@@ -35,113 +36,153 @@ __device__ __forceinline__ uint2 quantise(uint4 x, float& scale) {
                     values_to_codes<FMT>(__fmul_rn(lo16(x.z), r), __fmul_rn(hi16(x.z), r), __fmul_rn(lo16(x.w), r), __fmul_rn(hi16(x.w), r)));
 }
 
+// Work is dealt out in pieces of ROWS entries of one (sequence, kv-head); a group of lanes has U of them at a time, so that their loads
+// (for a gather: their positions, then their rows) are in flight together.
+constexpr int U = 4;
+template <int LANES>
+struct Piece {
+  static constexpr int GROUPS = NT / LANES, ROWS = GROUPS * U;
+  int per, bh, i;                                            // pieces of a head; this one's (sequence, kv-head) and the lanes' first entry
+  __device__ __forceinline__ Piece(long long piece, int n) : per((n + ROWS - 1) / ROWS), bh((int)(piece / per)) {
+    i = (int)(piece - (long long)bh * per) * ROWS + threadIdx.x / LANES;
+  }
+  static long long count(long long heads, int n) { return heads * ((n + ROWS - 1) / ROWS); }
+};
+
 }  // namespace
 
 template <int D, int FMT, bool GATHER>
-__global__ void __launch_bounds__(NT) kv_quantize_kernel(const KvWrite p) {
+__global__ void __launch_bounds__(NT) kv_quantize_kernel(const KvWrite p, const long long pieces) {
   chain();
-  constexpr int LANES = D / 8;
+  constexpr int LANES = D / 8, GROUPS = Piece<LANES>::GROUPS;
   const int lane = threadIdx.x % LANES;
-  const long long n_rows = (long long)p.B * p.n * p.Hkv, step = (long long)gridDim.x * (NT / LANES);
   // every lane of a warp goes through the same number of turns: the exchanges of row_max_bits are the whole warp's
-  for (long long row0 = (long long)blockIdx.x * (NT / LANES); row0 < n_rows; row0 += step) {
-    const long long row = row0 + threadIdx.x / LANES;
-    bool there = row < n_rows;
-    uint4 xk = make_uint4(0, 0, 0, 0), xv = xk;
-    long long to = 0;                                        // entry of the cache
-    if (there) {
-      if constexpr (GATHER) {                                // row = (kv-head, entry)
-        const int h = (int)(row / p.n), e = (int)(row % p.n), r = e / p.per_chunk, t = e % p.per_chunk;
-        const int pos = p.idx[((long long)r * p.Hkv + h) * p.per_chunk + t];
-        if (pos >= 0) {
-          const long long chunk = p.kept[r];
-          xk = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.k_src) + chunk * p.k_stride[0] + pos * p.k_stride[1] + h * p.k_stride[2]) + lane);
-          xv = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.v_src) + chunk * p.v_stride[0] + pos * p.v_stride[1] + h * p.v_stride[2]) + lane);
-        }
-        to = (long long)h * p.capacity + e;
-        if (p.pos_out != nullptr && lane == 0) p.pos_out[row] = pos < 0 ? -1 : pos;
-      } else {                                               // row = (sequence, token, kv-head)
-        const int h = (int)(row % p.Hkv);
-        const long long x = row / p.Hkv;
-        const int i = (int)(x % p.n), b = (int)(x / p.n);
-        const long long at = (long long)p.at0 + (p.at ? p.at[b] : 0) + i;
-        if (at < 0 || at >= p.capacity) {
-          if (lane == 0 && p.status) atomicCAS(p.status, 0, 401);
-          there = false;
-        } else {
-          xk = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.k_src) + b * p.k_stride[0] + i * p.k_stride[1] + h * p.k_stride[2]) + lane);
-          xv = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.v_src) + b * p.v_stride[0] + i * p.v_stride[1] + h * p.v_stride[2]) + lane);
-        }
-        to = ((long long)b * p.Hkv + h) * p.capacity + at;
+  for (long long piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+    const Piece<LANES> w(piece, p.n);
+    const int b = w.bh / p.Hkv, h = w.bh - b * p.Hkv;
+    long long to[U];                                         // entry of the cache, or -1
+    const uint16_t *k_at[U], *v_at[U];                       // null: zeros
+    if constexpr (GATHER) {
+      int pos[U], chunk[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int e = w.i + u * GROUPS, r = e / p.per_chunk;
+        to[u] = e < p.n ? (long long)h * p.capacity + e : -1;
+        pos[u] = e < p.n ? __ldg(p.idx + ((long long)r * p.Hkv + h) * p.per_chunk + (e - r * p.per_chunk)) : -1;
+        chunk[u] = e < p.n ? __ldg(p.kept + r) : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool there = pos[u] >= 0;
+        k_at[u] = there ? static_cast<const uint16_t*>(p.k_src) + chunk[u] * p.k_stride[0] + pos[u] * p.k_stride[1] + h * p.k_stride[2] : nullptr;
+        v_at[u] = there ? static_cast<const uint16_t*>(p.v_src) + chunk[u] * p.v_stride[0] + pos[u] * p.v_stride[1] + h * p.v_stride[2] : nullptr;
+        if (p.pos_out != nullptr && lane == 0 && to[u] >= 0) p.pos_out[(long long)h * p.n + w.i + u * GROUPS] = there ? pos[u] : -1;
+      }
+    } else {
+      const long long at0 = (long long)p.at0 + (p.at ? p.at[b] : 0);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = w.i + u * GROUPS;
+        const long long at = at0 + i;
+        const bool there = i < p.n && at >= 0 && at < p.capacity;
+        if (i < p.n && !there && lane == 0 && p.status) atomicCAS(p.status, 0, 401);
+        to[u] = there ? (long long)w.bh * p.capacity + at : -1;
+        k_at[u] = there ? static_cast<const uint16_t*>(p.k_src) + b * p.k_stride[0] + i * p.k_stride[1] + h * p.k_stride[2] : nullptr;
+        v_at[u] = there ? static_cast<const uint16_t*>(p.v_src) + b * p.v_stride[0] + i * p.v_stride[1] + h * p.v_stride[2] : nullptr;
       }
     }
-    float sk, sv;
-    const uint2 ck = quantise<FMT, LANES>(xk, sk), cv = quantise<FMT, LANES>(xv, sv);
-    if (there) {
-      reinterpret_cast<uint2*>(p.k + to * D)[lane] = ck;
-      reinterpret_cast<uint2*>(p.v + to * D)[lane] = cv;
-      if (lane == 0) { p.k_scale[to] = sk; p.v_scale[to] = sv; }
+    uint4 xk[U], xv[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      xk[u] = xv[u] = make_uint4(0, 0, 0, 0);
+      if (k_at[u] != nullptr) {
+        xk[u] = __ldg(reinterpret_cast<const uint4*>(k_at[u]) + lane);
+        xv[u] = __ldg(reinterpret_cast<const uint4*>(v_at[u]) + lane);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float sk, sv;
+      const uint2 ck = quantise<FMT, LANES>(xk[u], sk), cv = quantise<FMT, LANES>(xv[u], sv);
+      if (to[u] >= 0) {
+        reinterpret_cast<uint2*>(p.k + to[u] * D)[lane] = ck;
+        reinterpret_cast<uint2*>(p.v + to[u] * D)[lane] = cv;
+        if (lane == 0) { p.k_scale[to[u]] = sk; p.v_scale[to[u]] = sv; }
+      }
     }
   }
 }
 
 template <int D, int FMT>
-__global__ void __launch_bounds__(NT) kv_dequantize_kernel(const KvRead p) {
+__global__ void __launch_bounds__(NT) kv_dequantize_kernel(const KvRead p, const long long pieces) {
   chain();
-  constexpr int LANES = D / 16;                              // 16 codes a lane
+  constexpr int LANES = D / 16, GROUPS = Piece<LANES>::GROUPS;                // 16 codes a lane
   const int lane = threadIdx.x % LANES;
-  const long long n_rows = (long long)p.B * p.Hkv * p.n;
-  for (long long row = (long long)blockIdx.x * (NT / LANES) + threadIdx.x / LANES; row < n_rows; row += (long long)gridDim.x * (NT / LANES)) {
-    const int i = (int)(row % p.n);
-    const long long bh = row / p.n;
-    const long long at = (long long)p.at0 + (p.at ? p.at[bh / p.Hkv] : 0) + i;
-    uint4 k0 = make_uint4(0, 0, 0, 0), k1 = k0, v0 = k0, v1 = k0;
-    if (at >= 0 && at < p.capacity) {
-      const long long from = bh * p.capacity + at;
-      const uint4 k = __ldg(reinterpret_cast<const uint4*>(p.k + from * D) + lane), v = __ldg(reinterpret_cast<const uint4*>(p.v + from * D) + lane);
-      const float sk = __ldg(p.k_scale + from), sv = __ldg(p.v_scale + from);
-      uint2 a = codes_to_bf16x4<FMT>(k.x, sk), b = codes_to_bf16x4<FMT>(k.y, sk);
-      k0 = make_uint4(a.x, a.y, b.x, b.y);
-      a = codes_to_bf16x4<FMT>(k.z, sk); b = codes_to_bf16x4<FMT>(k.w, sk);
-      k1 = make_uint4(a.x, a.y, b.x, b.y);
-      a = codes_to_bf16x4<FMT>(v.x, sv); b = codes_to_bf16x4<FMT>(v.y, sv);
-      v0 = make_uint4(a.x, a.y, b.x, b.y);
-      a = codes_to_bf16x4<FMT>(v.z, sv); b = codes_to_bf16x4<FMT>(v.w, sv);
-      v1 = make_uint4(a.x, a.y, b.x, b.y);
+  for (long long piece = blockIdx.x; piece < pieces; piece += gridDim.x) {
+    const Piece<LANES> w(piece, p.n);
+    const long long at0 = (long long)p.at0 + (p.at ? p.at[w.bh / p.Hkv] : 0);
+    uint4 k[U], v[U];
+    float sk[U], sv[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = w.i + u * GROUPS;
+      const long long at = at0 + i;
+      k[u] = v[u] = make_uint4(0, 0, 0, 0);
+      sk[u] = sv[u] = 0.0f;
+      if (i < p.n && at >= 0 && at < p.capacity) {
+        const long long from = w.bh * p.capacity + at;
+        k[u] = __ldg(reinterpret_cast<const uint4*>(p.k + from * D) + lane);
+        v[u] = __ldg(reinterpret_cast<const uint4*>(p.v + from * D) + lane);
+        sk[u] = __ldg(p.k_scale + from);
+        sv[u] = __ldg(p.v_scale + from);
+      }
     }
-    uint4* const ko = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.k_out) + row * D) + 2 * lane;
-    uint4* const vo = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.v_out) + row * D) + 2 * lane;
-    ko[0] = k0; ko[1] = k1;
-    vo[0] = v0; vo[1] = v1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = w.i + u * GROUPS;
+      if (i >= p.n) break;
+      auto store = [&](void* to, const uint4& x, float s) {                  // 32 bytes, a whole sector, in one store
+        const uint2 a = codes_to_bf16x4<FMT>(x.x, s), b = codes_to_bf16x4<FMT>(x.y, s), c = codes_to_bf16x4<FMT>(x.z, s), d = codes_to_bf16x4<FMT>(x.w, s);
+        uint16_t* const o = static_cast<uint16_t*>(to) + ((long long)w.bh * p.n + i) * D + 16 * lane;
+        if (p.sectors) {
+          const float y[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(b.x), __uint_as_float(b.y),
+                              __uint_as_float(c.x), __uint_as_float(c.y), __uint_as_float(d.x), __uint_as_float(d.y)};
+          st_global_f32x8(o, y);
+        } else {
+          reinterpret_cast<uint4*>(o)[0] = make_uint4(a.x, a.y, b.x, b.y);
+          reinterpret_cast<uint4*>(o)[1] = make_uint4(c.x, c.y, d.x, d.y);
+        }
+      };
+      store(p.k_out, k[u], sk[u]);
+      store(p.v_out, v[u], sv[u]);
+    }
   }
 }
 
 namespace {
 
-unsigned blocks_for(long long rows, int rows_per_block, int sm_count) {
-  const long long need = (rows + rows_per_block - 1) / rows_per_block, most = (long long)sm_count * 8;
-  return (unsigned)(need < most ? need : most);
+dim3 grid_for(long long pieces) { return dim3((unsigned)(pieces < 0x7FFFFFFF ? pieces : 0x7FFFFFFF)); }
+template <int D, int FMT>
+cudaError_t quantize_t(const KvWrite& w, bool gather, cudaStream_t st) {
+  const long long pieces = Piece<D / 8>::count((long long)w.B * w.Hkv, w.n);
+  return gather ? launch_chained(kv_quantize_kernel<D, FMT, true>, grid_for(pieces), dim3(NT), 0, st, 1, w, pieces)
+                : launch_chained(kv_quantize_kernel<D, FMT, false>, grid_for(pieces), dim3(NT), 0, st, 1, w, pieces);
 }
 template <int D, int FMT>
-cudaError_t quantize_t(const KvWrite& w, bool gather, int sm_count, cudaStream_t st) {
-  const dim3 grid(blocks_for((long long)w.B * w.n * w.Hkv, NT / (D / 8), sm_count));
-  return gather ? launch_chained(kv_quantize_kernel<D, FMT, true>, grid, dim3(NT), 0, st, 1, w)
-                : launch_chained(kv_quantize_kernel<D, FMT, false>, grid, dim3(NT), 0, st, 1, w);
-}
-template <int D, int FMT>
-cudaError_t dequantize_t(const KvRead& r, int sm_count, cudaStream_t st) {
-  return launch_chained(kv_dequantize_kernel<D, FMT>, dim3(blocks_for((long long)r.B * r.n * r.Hkv, NT / (D / 16), sm_count)), dim3(NT), 0, st, 1, r);
+cudaError_t dequantize_t(const KvRead& r, cudaStream_t st) {
+  const long long pieces = Piece<D / 16>::count((long long)r.B * r.Hkv, r.n);
+  return launch_chained(kv_dequantize_kernel<D, FMT>, grid_for(pieces), dim3(NT), 0, st, 1, r, pieces);
 }
 
 }  // namespace
 
-cudaError_t launch_kv_quantize(const KvWrite& w, int format, int d, bool gather, int sm_count, cudaStream_t st) {
-  if (d == 128) return format == FMT_INT8 ? quantize_t<128, FMT_INT8>(w, gather, sm_count, st) : quantize_t<128, FMT_E4M3>(w, gather, sm_count, st);
-  return format == FMT_INT8 ? quantize_t<64, FMT_INT8>(w, gather, sm_count, st) : quantize_t<64, FMT_E4M3>(w, gather, sm_count, st);
+cudaError_t launch_kv_quantize(const KvWrite& w, int format, int d, bool gather, cudaStream_t st) {
+  if (d == 128) return format == FMT_INT8 ? quantize_t<128, FMT_INT8>(w, gather, st) : quantize_t<128, FMT_E4M3>(w, gather, st);
+  return format == FMT_INT8 ? quantize_t<64, FMT_INT8>(w, gather, st) : quantize_t<64, FMT_E4M3>(w, gather, st);
 }
-cudaError_t launch_kv_dequantize(const KvRead& r, int format, int d, int sm_count, cudaStream_t st) {
-  if (d == 128) return format == FMT_INT8 ? dequantize_t<128, FMT_INT8>(r, sm_count, st) : dequantize_t<128, FMT_E4M3>(r, sm_count, st);
-  return format == FMT_INT8 ? dequantize_t<64, FMT_INT8>(r, sm_count, st) : dequantize_t<64, FMT_E4M3>(r, sm_count, st);
+cudaError_t launch_kv_dequantize(const KvRead& r, int format, int d, cudaStream_t st) {
+  if (d == 128) return format == FMT_INT8 ? dequantize_t<128, FMT_INT8>(r, st) : dequantize_t<128, FMT_E4M3>(r, st);
+  return format == FMT_INT8 ? dequantize_t<64, FMT_INT8>(r, st) : dequantize_t<64, FMT_E4M3>(r, st);
 }
 
 }  // namespace pc
