@@ -133,7 +133,7 @@ PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n
 PhasePlan wide_plan(int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count) {
   PhasePlan p = {};
   p.wide = true;
-  p.pair = format == PC_KV_BF16 && d == 128 && rows > 128 && sm_count >= 2;
+  p.pair = d == 128 && rows > 128 && sm_count >= 2;
   const int64_t block = p.pair ? 256 : 128, blocks = (rows + block - 1) / block, units = p.pair ? sm_count / 2 : sm_count;
   const int tiles = (n_keys + 127) / 128;
   double least = -1.0;
@@ -191,15 +191,15 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
 
 int plan_sms() { const int n = pc::sm100_count(); return n > 0 ? n : 148; }
 
-// tensor maps over the first n entries of a cache, boxes of `keys` entries
-bool cache_maps(const pc_kv_cache* c, int n, int keys, CUtensorMap* tm_k, CUtensorMap* tm_v) {
+// tensor maps over the first n entries of a cache, boxes of `keys` entries (8-bit formats: and `cols` columns)
+bool cache_maps(const pc_kv_cache* c, int n, int keys, int cols, CUtensorMap* tm_k, CUtensorMap* tm_v) {
   const uint64_t d = (uint64_t)c->d, cap = (uint64_t)c->capacity;
   const uint64_t dims[4] = {d, (uint64_t)n, (uint64_t)c->Hkv, (uint64_t)c->B}, str[3] = {d, cap * d, (uint64_t)c->Hkv * cap * d};
   if (c->format == PC_KV_BF16) {
     const uint32_t box[4] = {64, (uint32_t)keys, 1, 1};
     return pc::make_tmap_bf16_4d(tm_k, c->k, dims, str, box) && pc::make_tmap_bf16_4d(tm_v, c->v, dims, str, box);
   }
-  const uint32_t box[4] = {(uint32_t)c->d, (uint32_t)keys, 1, 1};
+  const uint32_t box[4] = {(uint32_t)cols, (uint32_t)keys, 1, 1};
   return pc::make_tmap_u8_4d(tm_k, c->k, dims, str, box) && pc::make_tmap_u8_4d(tm_v, c->v, dims, str, box);
 }
 
@@ -279,14 +279,14 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
       const uint32_t box[4] = {64, 128, 1, 1};
       CUtensorMap maps[3] = {}, unused;
       bool made = pc::make_tmap_bf16_4d(&maps[0], plan.halves ? rows.halves : rows.rows, dims, str, box);
-      made = made && cache_maps(c, n, ph.pair ? 64 : 128, &maps[1], &unused) && cache_maps(c, n, 128, &unused, &maps[2]);
+      made = made && cache_maps(c, n, ph.pair ? 64 : 128, c->d, &maps[1], &unused) && cache_maps(c, n, 128, ph.pair ? 64 : c->d, &unused, &maps[2]);
       if (!made) { launched(e); return PC_ERR_CUDA; }
       e = pc::launch_cache_wide(maps, wp, c->format, a->d, ph.pair, sms, st);
       slot += ph.n_split;
       continue;
     }
     CUtensorMap tm_k, tm_v;
-    if (!cache_maps(c, n, pc::few_keys(c->format, c->d, ph.brief), &tm_k, &tm_v)) { launched(e); return PC_ERR_CUDA; }
+    if (!cache_maps(c, n, pc::few_keys(c->format, c->d, ph.brief), c->d, &tm_k, &tm_v)) { launched(e); return PC_ERR_CUDA; }
     e = pc::launch_cache_few(tm_k, tm_v, p, ph.finish ? &merge : nullptr, ph.brief, c->format, c->d, st);
     slot += ph.n_split;
   }

@@ -21,11 +21,13 @@ namespace {
 
 using namespace flash;
 
-// Ring and slots of the 8-bit build (single CTAs): K and V stages of whole tiles, raw slots of codes.
-template <int D_, int FMT_>
-struct Cfg8 : Cfg<D_, false> {
-  static constexpr int NK = D_ == 128 ? 1 : 3, NV = D_ == 128 ? 2 : 3, NS = NK + NV;
-  static constexpr int RAW = 3, RAW_BYTES = TILE * D_;
+// Ring and slots of the 8-bit builds: stages of a tile of K or V, of a pair 64 keys of K and 64 columns of V, as for bf16; raw slots of
+// the codes of a stage.
+template <int D_, bool PAIR_>
+struct Cfg8 : Cfg<D_, PAIR_> {
+  static constexpr bool WHOLE = D_ == 128 && !PAIR_;                          // stages of 32 KB
+  static constexpr int NK = WHOLE ? 1 : 3, NV = WHOLE ? 2 : 3, NS = NK + NV, NQ = 2;
+  static constexpr int RAW = PAIR_ ? 6 : 3, RAW_BYTES = TILE * D_ / (PAIR_ ? 2 : 1);
 };
 template <class C>
 struct Off8 {
@@ -35,10 +37,11 @@ struct Off8 {
 // key_scale: a tile's scales stay until its softmax has read them.  The converter is at most NK + 2 tiles ahead of that: a key stage is
 // free once the products of its tile have run, and those wait for the softmax to have read the logits before theirs.
 struct __align__(16) Extra8 {
-  uint64_t sc_full[8], raw_full[3], raw_free[3];
+  uint64_t sc_full[8], raw_full[6], raw_free[6];
   float key_scale[8][TILE];
 };
-static_assert(Off8<Cfg8<128, 1>>::EXTRA + sizeof(Extra8) <= 232448, "shared memory of a CTA");
+static_assert(Off8<Cfg8<128, false>>::EXTRA + sizeof(Extra8) <= 232448 && Off8<Cfg8<128, true>>::EXTRA + sizeof(Extra8) <= 232448,
+              "shared memory of a CTA");
 
 struct Item { int hkv, rg, split, j0, n; };
 __device__ __forceinline__ Item decode_item(const WidePhase& p, int item) {
@@ -89,24 +92,20 @@ __device__ __forceinline__ void half_of(int h, int n, int lag, bool& values, int
   else { values = true; t = both + (h - 2 * both); }
 }
 
-// The epilogue's warps between the raw slots and the ring; a warp has 32 rows of a half.
+// The epilogue's warps between the raw slots and the ring; a warp has a quarter of a stage's rows.
 template <class C, int FMT>
 struct Converter {
-  static constexpr int D = C::D, LPR = D / 16, PIECES = LPR;                // 16-byte pieces of a row; pieces of a lane
+  static constexpr int D = C::D;
   const Ctx2& cx;
   const WidePhase& prm;
   Extra8& ex;
   const uint8_t* raw;
-  // Row and piece of this lane in a step of 32 / LPR rows: of the eight lanes that store together at head size 128, four are in the
-  // next row, whose swizzle puts their chunks into the other banks.
-  int lane_row, piece;
   int warp, lane;
   uint32_t k = 0, v = 0, raws = 0, tile = 0;               // uses of the stages and of the slots; tiles of earlier items
   __device__ __forceinline__ Converter(const Ctx2& c, const WidePhase& p, Extra8& e, const uint8_t* raw_smem, int w, int l)
-      : cx(c), prm(p), ex(e), raw(raw_smem), lane_row(D == 128 ? (l >> 4) * 2 + ((l >> 2) & 1) : l / 4),
-        piece(D == 128 ? (l & 3) | ((l >> 1) & 4) : l & 3), warp(w), lane(l) {}
+      : cx(c), prm(p), ex(e), raw(raw_smem), warp(w), lane(l) {}
 
-  // scale of this lane's row (row `lane` of the warp's 32), 0 behind the last entry
+  // scale of key warp * 32 + lane of the tile, 0 behind the last entry
   __device__ __forceinline__ float scale_of(const Item& it, int h, int lag) const {
     bool values;
     int t;
@@ -119,23 +118,28 @@ struct Converter {
     Misc2& mi = *cx.mi;
     uint32_t& n = VALUES ? v : k;
     constexpr int FIRST = VALUES ? C::NK : 0, STAGES = VALUES ? C::NV : C::NK;
+    // rows of a stage and their bytes as codes; the steps in which a warp goes through its rows
+    constexpr int ROWS = C::PAIR && !VALUES ? 64 : 128, BYTES = C::PAIR && VALUES ? 64 : D, LPR = BYTES / 16, STEPS = ROWS / 4 * LPR / 32;
+    // Row and 16-byte piece of this lane in a step: of the eight lanes that store together in rows of 128 codes, four are in the next row,
+    // whose swizzle puts their chunks into the other banks.
+    const int lane_row = LPR == 8 ? (lane >> 4) * 2 + ((lane >> 2) & 1) : lane / 4, piece = LPR == 8 ? (lane & 3) | ((lane >> 1) & 4) : lane & 3;
     const int st = FIRST + n % STAGES, slot = raws % C::RAW;
     if (!WAIT2S(&mi.kv_free[st], free_par(n / STAGES), W2_KVFREE) || !WAIT2S(&ex.raw_full[slot], full_par(raws / C::RAW), W2_KVFULL)) return false;
     uint8_t* const to = cx.ring + st * C::STAGE_BYTES;
     const uint8_t* const from = raw + slot * C::RAW_BYTES;
 #pragma unroll
-    for (int i0 = 0; i0 < PIECES; i0 += 4) {               // four pieces at a time, their latencies side by side
+    for (int i0 = 0; i0 < STEPS; i0 += 4) {                // four pieces at a time, their latencies side by side
       uint4 in[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        uint32_t off = (warp * 32 + (i0 + u) * (32 / LPR) + lane_row) * D + piece * 16;
-        off ^= ((off >> 7) & (D == 128 ? 7 : 3)) << 4;
+        uint32_t off = (warp * (ROWS / 4) + (i0 + u) * (32 / LPR) + lane_row) * BYTES + piece * 16;
+        off ^= ((off >> 7) & (BYTES == 128 ? 7 : 3)) << 4;
         in[u] = *reinterpret_cast<const uint4*>(from + off);
       }
-      if (i0 + 4 == PIECES) warp_arrive(&ex.raw_free[slot]);
+      if (i0 + 4 == STEPS) warp_arrive(&ex.raw_free[slot]);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int local = (i0 + u) * (32 / LPR) + lane_row, row = warp * 32 + local;
+        const int local = (i0 + u) * (32 / LPR) + lane_row, row = warp * (ROWS / 4) + local;
         const uint4 x = in[u];
         uint4 a, b;
         if constexpr (VALUES) {
@@ -148,7 +152,7 @@ struct Converter {
           a = make_uint4(codes_to_half2<FMT, 0>(z0), codes_to_half2<FMT, 1>(z0), codes_to_half2<FMT, 0>(z1), codes_to_half2<FMT, 1>(z1));
           b = make_uint4(codes_to_half2<FMT, 0>(z2), codes_to_half2<FMT, 1>(z2), codes_to_half2<FMT, 0>(z3), codes_to_half2<FMT, 1>(z3));
         }
-        uint8_t* const base = to + (piece / 4) * 16384;    // elements 16 piece .. 16 piece + 15 of the row
+        uint8_t* const base = to + (piece / 4) * (ROWS * 128);               // elements 16 piece .. 16 piece + 15 of the row
         *reinterpret_cast<uint4*>(base + sw128_offset(row, (2 * piece) % 8)) = a;
         *reinterpret_cast<uint4*>(base + sw128_offset(row, (2 * piece + 1) % 8)) = b;
       }
@@ -159,7 +163,7 @@ struct Converter {
       warp_arrive(&ex.sc_full[at % 8]);
     }
     fence_proxy_async_smem();
-    warp_arrive(&mi.kv_full[st]);
+    warp_arrive(&mi.kv_full[st]);                          // (of a pair's peer: an issuer's warp there passes it on to the leader)
     ++n;
     ++raws;
     return true;
@@ -178,19 +182,42 @@ struct Converter {
   }
 };
 
+// The issuers' warps of a pair's peer: a stage that the peer's warps have filled is made known to the leader, with what they have written
+// (a release at the cluster's scope takes some 1400 cycles, which the converting warps do not have).
+template <class C>
+__device__ __forceinline__ void pass_on(const Ctx2& cx, bool values) {
+  Misc2& mi = *cx.mi;
+  uint32_t nd = 0, n = 0;
+  while (true) {
+    const Desc d = next_desc<C>(cx, nd, false);
+    if (d.kind == KIND_DONE) break;
+    for (int t = 0; t < d.t[1]; ++t, ++n) {
+      const int st = values ? C::NK + n % C::NV : n % C::NK;
+      if (!WAIT2I(&mi.kv_full[st], full_par(n / (values ? C::NV : C::NK)), W2_KVFULL)) break;
+      mbar_arrive_cluster(map_to_cta(&mi.kv_full[st], 0));
+    }
+  }
+}
+// the issuers' wait for a stage: of a pair also for what the peer has written
+template <class C>
+__device__ __forceinline__ void wait_operand(const Ctx2& cx, uint64_t* bar, uint32_t parity) {
+  if constexpr (C::PAIR) mbar_wait_cluster(bar, parity, cx.abort_flag, cx.status, C::CODE + W2_KVFULL);
+  else WAIT2I(bar, parity, W2_KVFULL);
+}
+
 }  // namespace
 
 // tensor maps: tm_q (rows of a kv-head, 64 x 128); bf16 (boxes of 64 d): tm_k (64 entries of a pair or 128), tm_v (128); 8 bits: codes of 128
-// entries.  Rows behind the end
+// entries, of a pair 64 entries of the keys and 64 columns of the values.  Rows behind the end
 // of a tensor read as zeros; the softmax masks the entries behind the last.
 template <int D, int FMT, bool PAIR>
 __global__ void __launch_bounds__(NT2, 1)
 cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                   const __grid_constant__ WidePhase prm) {
   constexpr bool Q8 = FMT != FMT_BF16;
-  using C = typename std::conditional<Q8, Cfg8<D, FMT>, Cfg<D, PAIR>>::type;
-  using O = typename std::conditional<Q8, Off8<Cfg8<D, FMT>>, Off<Cfg<D, PAIR>>>::type;
-  constexpr int NCTA = C::NCTA, NQ = Q8 ? 2 : C::NQ;
+  using C = typename std::conditional<Q8, Cfg8<D, PAIR>, Cfg<D, PAIR>>::type;
+  using O = typename std::conditional<Q8, Off8<Cfg8<D, PAIR>>, Off<Cfg<D, PAIR>>>::type;
+  constexpr int NCTA = C::NCTA, NQ = C::NQ;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int tid = threadIdx.x, warp = tid >> 5;
   const uint32_t rank = PAIR ? cluster_ctarank() : 0;
@@ -206,12 +233,12 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   cx.abort_flag = &cx.mi->abort_flag;
   cx.status = prm.c.status;
   Misc2& mi = *cx.mi;
-  Extra8& ex = *reinterpret_cast<Extra8*>(smem + Off8<Cfg8<D, FMT>>::EXTRA);       // (8-bit formats)
+  Extra8& ex = *reinterpret_cast<Extra8*>(smem + Off8<Cfg8<D, PAIR>>::EXTRA);       // (8-bit formats)
   if (tid == 0) {
-    init_barriers2<C>(mi, prm.c.wait_kcycles, leader, Q8 ? 4 : 1);       // four converting warps in the place of one copy
+    init_barriers2<C>(mi, prm.c.wait_kcycles, leader, !Q8 ? 1 : PAIR && leader ? 5 : 4, Q8);   // four converting warps, and the peer's word, in the place of a copy
     if constexpr (Q8) {
       for (int i = 0; i < 8; ++i) mbar_init(&ex.sc_full[i], 4);
-      for (int i = 0; i < 3; ++i) { mbar_init(&ex.raw_full[i], 1); mbar_init(&ex.raw_free[i], 4); }
+      for (int i = 0; i < 6; ++i) { mbar_init(&ex.raw_full[i], 1); mbar_init(&ex.raw_free[i], 4); }
       fence_mbar_init();
     }
   }
@@ -259,9 +286,10 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               int t;
               half_of(h, it.n, alt ? 2 : 1, values, t);
               const int slot = raws % C::RAW;
-              if (!WAIT2(&ex.raw_free[slot], free_par(raws / C::RAW), W2_KVFREE)) break;
+              if (!WAIT2I(&ex.raw_free[slot], free_par(raws / C::RAW), W2_KVFREE)) break;
               mbar_arrive_expect_tx(&ex.raw_full[slot], C::RAW_BYTES);
-              tma_load_4d(smem + O::RAW + slot * C::RAW_BYTES, values ? &tm_v : &tm_k, &ex.raw_full[slot], 0, (it.j0 + t) * TILE, it.hkv, 0);
+              tma_load_4d(smem + O::RAW + slot * C::RAW_BYTES, values ? &tm_v : &tm_k, &ex.raw_full[slot], PAIR && values ? (int)rank * 64 : 0,
+                          (it.j0 + t) * TILE + (PAIR && !values ? (int)rank * 64 : 0), it.hkv, 0);
             }
           } else {
             uint8_t* dst;
@@ -287,8 +315,9 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         publish<C>(cx, p, d);
         if constexpr (!Q8) drain_copies<C>(cx, p, leader);
         else if (*cx.abort_flag) {                          // every copy issued has landed before the exit
-          for (uint32_t i = (p.q > NQ ? p.q - NQ : 0); i < p.q; ++i) mbar_wait_drain(&mi.q_full[i % NQ], full_par(i / NQ), cx.abort_flag);
+          for (uint32_t i = (p.q > NQ ? p.q - NQ : 0); i < p.q && leader; ++i) mbar_wait_drain(&mi.q_full[i % NQ], full_par(i / NQ), cx.abort_flag);
           for (uint32_t i = (raws > C::RAW ? raws - C::RAW : 0); i < raws; ++i) mbar_wait_drain(&ex.raw_full[i % C::RAW], full_par(i / C::RAW), cx.abort_flag);
+          abort_grace_pause(cx.abort_flag);                // (of a pair the peer cannot see its last copy of queries land)
         }
       }
       __syncwarp();
@@ -306,7 +335,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             uint32_t k_u32;
             if constexpr (Q8) {
               const int st = is.k % C::NK;
-              WAIT2I(&mi.kv_full[st], full_par(is.k / C::NK), W2_KVFULL);
+              wait_operand<C>(cx, &mi.kv_full[st], full_par(is.k / C::NK));
               k_u32 = smem_u32(cx.ring) + st * C::STAGE_BYTES;
             } else {
               k_u32 = is.wait_k();
@@ -315,12 +344,13 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 #pragma unroll 1
             for (int b = first; b <= last; ++b) {
               if constexpr (Q8) {
-                constexpr uint32_t idesc = make_idesc_f16_f32(TILE, TILE);
+                constexpr uint32_t idesc = make_idesc_f16_f32(TILE * NCTA, TILE);
                 const int sb = C::TWO_S ? b : 0;
                 WAIT2I(&mi.s_read[sb], free_par(is.ns >> sb), W2_SREAD);
                 is.ns ^= 1u << sb;
                 tc_fence_after_sync();
-                if constexpr (D == 128) mma_ss_k128(cx.tmem + C::tm_s(b), b ? is.qa[1] : is.qa[0], k_u32, idesc);
+                if constexpr (PAIR) mma_ss_pair_k128<true>(cx.tmem + C::tm_s(b), b ? is.qa[1] : is.qa[0], k_u32, idesc);
+                else if constexpr (D == 128) mma_ss_k128(cx.tmem + C::tm_s(b), b ? is.qa[1] : is.qa[0], k_u32, idesc);
                 else mma_ss_k64(cx.tmem + C::tm_s(b), b ? is.qa[1] : is.qa[0], k_u32, idesc);
                 commit<C>(&mi.s_full[b]);
               } else {
@@ -333,6 +363,10 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
         commit<C>(&mi.mma_done);
       }
+      __syncwarp();
+    } else if (Q8 && PAIR && !leader && (warp == WARP_QK || warp == WARP_PV)) {
+      if constexpr (Q8 && PAIR)
+        if (elect_one()) pass_on<C>(cx, warp == WARP_PV);
       __syncwarp();
     } else if (warp == WARP_PV && leader) {
       // ================================================================ issuer of P V (of a pair: leader CTA)
@@ -347,20 +381,20 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
 #pragma unroll 1
             for (int b = first; b <= last; ++b) {
               if constexpr (Q8) {
-                constexpr uint32_t idesc = make_idesc_bf16_f32(TILE, D, false, true);
+                constexpr uint32_t idesc = make_idesc_bf16_f32(TILE * NCTA, D, false, true);
                 const uint32_t tO = cx.tmem + C::TM_O + b * D, tP = cx.tmem + C::TM_P + b * 64;
                 if (t < step) { is.wait_read_out(b); is.blocks ^= 1u << b; }
                 const uint32_t par = full_par(is.tiles >> b);
                 is.tiles ^= 1u << b;
                 WAIT2I(&mi.p_half[b], par, W2_PHALF);
                 const int st = C::NK + is.v % C::NV;
-                WAIT2I(&mi.kv_full[st], full_par(is.v / C::NV), W2_KVFULL);
+                wait_operand<C>(cx, &mi.kv_full[st], full_par(is.v / C::NV));
                 const uint32_t v_smem = smem_u32(cx.ring) + st * C::STAGE_BYTES;
                 tc_fence_after_sync();
-                mma_ts_k64<false>(tO, tP, v_smem, idesc, t >= step);
+                mma_ts_k64<PAIR>(tO, tP, v_smem, idesc, t >= step);
                 WAIT2I(&mi.p_full[b], par, W2_PFULL);
                 tc_fence_after_sync();
-                mma_ts_k64<false>(tO, tP + 32, v_smem + 8192, idesc, true);
+                mma_ts_k64<PAIR>(tO, tP + 32, v_smem + 8192, idesc, true);
                 commit<C>(&mi.pv_done[b]);
                 if (t + step >= n) commit<C>(&mi.o_full[b]);
               } else {
@@ -381,8 +415,8 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     const int r = tid & 127;
     const uint32_t lane_sel = static_cast<uint32_t>((warp & 3) * 32) << 16;
     uint32_t nd = 0, nq = 0, no[2] = {0, 0};
-    using Conv = Converter<Cfg8<D, Q8 ? FMT : FMT_INT8>, Q8 ? FMT : FMT_INT8>;
-    Conv conv(cx, prm, ex, smem + Off8<Cfg8<D, FMT>>::RAW, warp - WARP_EPI, tid & 31);
+    using Conv = Converter<Cfg8<D, PAIR>, Q8 ? FMT : FMT_INT8>;
+    Conv conv(cx, prm, ex, smem + Off8<Cfg8<D, PAIR>>::RAW, warp - WARP_EPI, tid & 31);
     while (true) {
       const Desc d = next_desc<C>(cx, nd, true);
       if (d.kind == KIND_DONE) break;
@@ -467,7 +501,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
       if (n > 0) {
         float scale_log2 = prm.c.q.scale_log2;
         if constexpr (Q8) {
-          const int row = first_row(d.h[0], b, 0) + r;
+          const int row = first_row(d.h[0], b, rank) + r;
           if (row < rows) scale_log2 = __ldg(prm.half_scale + (size_t)d.hkv * prm.c.total_rows + row);
         }
         RowState st = {-INFINITY, 0.0f};
@@ -504,7 +538,7 @@ namespace {
 template <int D, int FMT, bool PAIR>
 cudaError_t wide_t(const CUtensorMap* maps, const WidePhase& p, int sm_count, cudaStream_t st) {
   using C = Cfg<D, PAIR>;
-  constexpr int SMEM = FMT == FMT_BF16 ? Off<C>::TOTAL : Off8<Cfg8<D, FMT>>::EXTRA + (int)sizeof(Extra8);
+  constexpr int SMEM = FMT == FMT_BF16 ? Off<C>::TOTAL : Off8<Cfg8<D, PAIR>>::EXTRA + (int)sizeof(Extra8);
   if (cudaError_t e = cudaFuncSetAttribute(cache_wide_kernel<D, FMT, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM); e != cudaSuccess) return e;
   const long long n_items = (long long)p.c.Hkv * p.c.n_rg * p.c.n_split;
   const int units = sm_count / C::NCTA;
@@ -513,14 +547,18 @@ cudaError_t wide_t(const CUtensorMap* maps, const WidePhase& p, int sm_count, cu
                         maps[0], maps[1], maps[2], p);
 }
 
+template <int FMT>
+cudaError_t wide_d(const CUtensorMap* maps, const WidePhase& p, int d, bool pair, int sm_count, cudaStream_t st) {
+  if (d == 64) return wide_t<64, FMT, false>(maps, p, sm_count, st);
+  return pair ? wide_t<128, FMT, true>(maps, p, sm_count, st) : wide_t<128, FMT, false>(maps, p, sm_count, st);
+}
+
 }  // namespace
 
 cudaError_t launch_cache_wide(const CUtensorMap* maps, const WidePhase& p, int format, int d, bool pair, int sm_count, cudaStream_t st) {
-  if (format == FMT_BF16)
-    return d == 64 ? wide_t<64, FMT_BF16, false>(maps, p, sm_count, st) : pair ? wide_t<128, FMT_BF16, true>(maps, p, sm_count, st)
-                                                                               : wide_t<128, FMT_BF16, false>(maps, p, sm_count, st);
-  if (d == 64) return format == FMT_INT8 ? wide_t<64, FMT_INT8, false>(maps, p, sm_count, st) : wide_t<64, FMT_E4M3, false>(maps, p, sm_count, st);
-  return format == FMT_INT8 ? wide_t<128, FMT_INT8, false>(maps, p, sm_count, st) : wide_t<128, FMT_E4M3, false>(maps, p, sm_count, st);
+  return format == FMT_BF16   ? wide_d<FMT_BF16>(maps, p, d, pair, sm_count, st)
+         : format == FMT_INT8 ? wide_d<FMT_INT8>(maps, p, d, pair, sm_count, st)
+                              : wide_d<FMT_E4M3>(maps, p, d, pair, sm_count, st);
 }
 
 }  // namespace pc
