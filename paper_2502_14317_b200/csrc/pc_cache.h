@@ -71,6 +71,7 @@ struct CachePhase {
   const float *k_scale, *v_scale;                // [seqs,Hkv,capacity] (8-bit formats)
   long long capacity;
   int n_rg, n_split, slot0, n_slots, total_rows; // row groups of a sequence, key splits; total_rows = rows of a kv-head over all sequences
+  int causal;                                    // 1 (few rows, bf16, one split, brief for groups of 16): the entries are the new tokens themselves, token i sees 0 .. i
   CacheRows q;
   int rows_made;                                 // 1: the rows are in memory; 0: this launch makes them
   float* part_o;                                 // [Hkv,total_rows,n_slots,d]
@@ -80,12 +81,11 @@ struct CachePhase {
 };
 // Few rows (pc_cache_few.cu), groups of 8 or 16.  finish null: every split leaves its slot.  Else the splits of a (sequence, kv-head, row
 // group) are the CTAs of a cluster, and the kernel finishes its rows: its splits' results, finish's slots and the new tokens' keys.
-// brief: the build for many sequences with few entries.
+// group: 8 or 16 rows; brief: the build for many sequences with few entries.
 // maps of the cache's keys and values: boxes of few_keys() entries
 int few_keys(int format, int d, bool brief);     // keys of a stage
-int few_rows(int rows);                          // rows of a row group
-cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool brief, int format,
-                             int d, cudaStream_t st);
+cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, int group, bool brief,
+                             int format, int d, cudaStream_t st);
 
 // The same phase for more than 32 rows of one sequence (pc_cache_wide.cu), blocks of 128 rows.
 struct WidePhase {

@@ -91,9 +91,9 @@ int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0, const
 // ------------------------------------------------------------------------------------ attention over shared and own caches
 namespace {
 
-struct PhasePlan { bool wide, pair, brief, finish; int alt, n_rg, n_split; };
+struct PhasePlan { bool wide, pair, brief, finish; int alt, group, n_rg, n_split; };
 struct CachePlan {
-  PhasePlan prefix, own;
+  PhasePlan prefix, own, window;                 // window: the new tokens' keys as a phase of their own (n_split 0: not)
   int n_slots;                                   // results of a row in memory
   bool finished;                                 // the last phase finishes the rows: no merge
   int64_t total_rows;
@@ -107,15 +107,15 @@ struct CachePlan {
 // slots 1 + 0.1 a split for writing and merging them.
 PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, bool last, int sm_count) {
   PhasePlan p = {};
-  const int per = pc::few_rows((int)rows);
-  p.n_rg = (int)((rows + per - 1) / per);
+  p.group = rows <= 8 ? 8 : 16;
+  p.n_rg = (int)((rows + p.group - 1) / p.group);
   const double items = (double)seqs * Hkv * p.n_rg;
   p.brief = items > 2.0 * sm_count && n_keys <= 512;
   const int keys = pc::few_keys(format, d, p.brief), tiles = (n_keys + keys - 1) / keys;
   p.n_split = 1;
   p.finish = last;
   if (p.brief) return p;
-  const double tile_us = 2.0 * keys * d * (format == PC_KV_BF16 ? 2 : 1) / 6.5e6, alone = keys / 16 * (per == 8 ? 0.9 / 7 : 1.15 / 5);
+  const double tile_us = 2.0 * keys * d * (format == PC_KV_BF16 ? 2 : 1) / 6.5e6, alone = keys / 16 * (p.group == 8 ? 0.9 / 7 : 1.15 / 5);
   double least = -1.0;
   for (int s = 1; s <= 64 && s <= tiles; ++s) {
     const bool finish = last && s <= 8;
@@ -149,6 +149,11 @@ PhasePlan wide_plan(int64_t rows, int Hkv, int d, int format, int n_keys, int sm
   return p;
 }
 
+// whether rows [B,w,Hkv,d] with these strides can be fetched with TMA: none is 0 where it counts
+bool tma_strides(const int64_t* s, int64_t B, int64_t w, int64_t H) {
+  return (s[0] == 0 && s[1] == 0 && s[2] == 0) || ((s[0] != 0 || B == 1) && (s[1] != 0 || w == 1) && (s[2] != 0 || H == 1));
+}
+
 int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
   if (a->B < 1 || a->w < 1 || a->Hq < 1 || a->Hkv < 1 || a->Hq % a->Hkv != 0 || a->n_prefix < 0 || a->n_own < 0) return PC_ERR_INVALID_ARG;
   if (a->d != 64 && a->d != 128) return PC_ERR_UNSUPPORTED;
@@ -156,8 +161,10 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
   const int G = a->Hq / a->Hkv;
   p.total_rows = (int64_t)a->B * a->w * G;
   p.n_slots = 0;
-  p.prefix = p.own = {};
+  p.prefix = p.own = p.window = {};
   p.rows = p.halves = p.finished = false;
+  // More than 8 new tokens: their keys go through the matrix units, behind the caches' (up to 8: each row takes them one by one)
+  const bool window = a->k_win != nullptr && a->w > 8 && tma_strides(a->k_win_stride, a->B, a->w, a->Hkv) && tma_strides(a->v_win_stride, a->B, a->w, a->Hkv);
   for (int own = 0; own <= 1; ++own) {
     const pc_kv_cache* const c = own ? a->own : a->prefix;
     const int n = own ? a->n_own : a->n_prefix;
@@ -170,12 +177,21 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
       p.rows = true;
       p.halves = c->format != PC_KV_BF16;
     } else
-    ph = few_plan(own ? a->B : 1, own ? (int64_t)a->w * G : p.total_rows, a->Hkv, a->d, c->format, n, own || a->n_own == 0, sm_count);
+    ph = few_plan(own ? a->B : 1, own ? (int64_t)a->w * G : p.total_rows, a->Hkv, a->d, c->format, n, !window && (own || a->n_own == 0), sm_count);
     if ((own ? a->B : 1ll) * a->Hkv * ph.n_rg * ph.n_split > 0x7FFFFFFF) return PC_ERR_UNSUPPORTED;
     if (!ph.finish) p.n_slots += ph.n_split;
     p.finished |= ph.finish;
     // more than a round of CTAs: cheaper than each of them rotating its own
     if (!ph.wide && (own ? a->B : 1.0) * a->Hkv * ph.n_rg * ph.n_split > 2.0 * sm_count) p.rows = true;
+  }
+  if (window) {
+    const int64_t rows = (int64_t)a->w * G;
+    PhasePlan& ph = p.window;
+    ph.n_split = 1; ph.finish = p.finished = true;
+    ph.group = (double)a->B * a->Hkv * ((rows + 7) / 8) <= 2.0 * sm_count ? 8 : 16;
+    ph.brief = ph.group == 16;
+    ph.n_rg = (int)((rows + ph.group - 1) / ph.group);
+    if ((int64_t)a->B * a->Hkv * ph.n_rg > 2 * sm_count) p.rows = true;
   }
   if (p.n_slots == 0 && !p.finished) p.rows = true;
   size_t off = 0;
@@ -201,6 +217,17 @@ bool cache_maps(const pc_kv_cache* c, int n, int keys, int cols, CUtensorMap* tm
   }
   const uint32_t box[4] = {(uint32_t)cols, (uint32_t)keys, 1, 1};
   return pc::make_tmap_u8_4d(tm_k, c->k, dims, str, box) && pc::make_tmap_u8_4d(tm_v, c->v, dims, str, box);
+}
+
+// the same for the new tokens' keys or values
+bool window_map(const pc_cache_attn_args* a, const void* x, const long long stride[3], int keys, CUtensorMap* tm) {
+  const uint64_t dims[4] = {(uint64_t)a->d, (uint64_t)a->w, (uint64_t)a->Hkv, (uint64_t)a->B};
+  const uint64_t size[3] = {(uint64_t)a->B, (uint64_t)a->w, (uint64_t)a->Hkv};
+  uint64_t s[3];
+  for (int i = 0; i < 3; ++i) s[i] = size[i] > 1 ? (uint64_t)stride[i] : (uint64_t)a->d;          // (of one entry any stride will do)
+  const uint64_t str[3] = {s[1], s[2], s[0]};
+  const uint32_t box[4] = {64, (uint32_t)keys, 1, 1};
+  return pc::make_tmap_bf16_4d(tm, x, dims, str, box);
 }
 
 }  // namespace
@@ -236,6 +263,7 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
   const float scale_log2 = (float)(scale * 1.4426950408889634);
   rows.theta = a->rope_theta; rows.scale_log2 = scale_log2;
   cudaError_t e = cudaSuccess;
+  bool made = plan.rows;                                                         // the rows are in memory
   rows.rows = ws + plan.off_rows;
   if (plan.rows) {
     rows.clear = reinterpret_cast<int*>(ws + plan.off_counter);
@@ -252,23 +280,27 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
   merge.k_win = a->k_win; merge.v_win = a->v_win;
   merge.out = static_cast<__nv_bfloat16*>(a->out); merge.lse = a->lse;
   int slot = 0;
-  for (int own = 0; own <= 1 && e == cudaSuccess; ++own) {
+  for (int phase = 0; phase <= 2 && e == cudaSuccess; ++phase) {                 // the prefix, the own caches, the new tokens
+    const bool own = phase > 0, window = phase == 2;
     const pc_kv_cache* const c = own ? a->own : a->prefix;
-    const int n = own ? a->n_own : a->n_prefix;
-    if (n == 0) continue;
-    const PhasePlan& ph = own ? plan.own : plan.prefix;
+    const int n = window ? a->w : own ? a->n_own : a->n_prefix;
+    const PhasePlan& ph = window ? plan.window : own ? plan.own : plan.prefix;
+    if (ph.n_split == 0) continue;
     pc::CachePhase p = {};
     p.seqs = own ? a->B : 1;
     p.rows = own ? a->w * (a->Hq / a->Hkv) : (int)plan.total_rows;
-    p.Hkv = a->Hkv; p.n_keys = n; p.len = own ? a->own_len : nullptr;
-    p.k_scale = c->k_scale; p.v_scale = c->v_scale; p.capacity = c->capacity;
+    p.Hkv = a->Hkv; p.n_keys = n; p.len = own && !window ? a->own_len : nullptr;
+    if (!window) { p.k_scale = c->k_scale; p.v_scale = c->v_scale; p.capacity = c->capacity; }
     p.n_rg = ph.n_rg; p.n_split = ph.n_split; p.slot0 = slot; p.n_slots = plan.n_slots; p.total_rows = (int)plan.total_rows;
+    p.causal = window;
     p.q = rows;
-    p.rows_made = plan.rows || slot > 0;
+    p.rows_made = made;
     p.part_o = reinterpret_cast<float*>(ws + plan.off_o);
     p.part_ml = reinterpret_cast<float2*>(ws + plan.off_ml);
     p.status = a->status_word;
     p.wait_kcycles = pc::wait_limit_kcycles();
+    CUtensorMap maps[3] = {}, unused;
+    bool ok;
     if (ph.wide) {
       pc::WidePhase wp = {};
       wp.c = p; wp.alt = ph.alt; wp.n_tiles = (n + 127) / 128;
@@ -277,18 +309,18 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
       const uint64_t d = (uint64_t)a->d, R = (uint64_t)plan.total_rows;
       const uint64_t dims[4] = {d, R, (uint64_t)a->Hkv, 1}, str[3] = {d, R * d, R * d * (uint64_t)a->Hkv};
       const uint32_t box[4] = {64, 128, 1, 1};
-      CUtensorMap maps[3] = {}, unused;
-      bool made = pc::make_tmap_bf16_4d(&maps[0], plan.halves ? rows.halves : rows.rows, dims, str, box);
-      made = made && cache_maps(c, n, ph.pair ? 64 : 128, c->d, &maps[1], &unused) && cache_maps(c, n, 128, ph.pair ? 64 : c->d, &unused, &maps[2]);
-      if (!made) { launched(e); return PC_ERR_CUDA; }
-      e = pc::launch_cache_wide(maps, wp, c->format, a->d, ph.pair, sms, st);
-      slot += ph.n_split;
-      continue;
+      ok = pc::make_tmap_bf16_4d(&maps[0], plan.halves ? rows.halves : rows.rows, dims, str, box) &&
+           cache_maps(c, n, ph.pair ? 64 : 128, c->d, &maps[1], &unused) && cache_maps(c, n, 128, ph.pair ? 64 : c->d, &unused, &maps[2]);
+      if (ok) e = pc::launch_cache_wide(maps, wp, c->format, a->d, ph.pair, sms, st);
+    } else {
+      const int format = window ? PC_KV_BF16 : c->format, keys = pc::few_keys(format, a->d, ph.brief);
+      ok = window ? window_map(a, a->k_win, merge.k_stride, keys, &maps[1]) && window_map(a, a->v_win, merge.v_stride, keys, &maps[2])
+                  : cache_maps(c, n, keys, c->d, &maps[1], &maps[2]);
+      if (ok) e = pc::launch_cache_few(maps[1], maps[2], p, ph.finish ? &merge : nullptr, ph.group, ph.brief, format, a->d, st);
     }
-    CUtensorMap tm_k, tm_v;
-    if (!cache_maps(c, n, pc::few_keys(c->format, c->d, ph.brief), c->d, &tm_k, &tm_v)) { launched(e); return PC_ERR_CUDA; }
-    e = pc::launch_cache_few(tm_k, tm_v, p, ph.finish ? &merge : nullptr, ph.brief, c->format, c->d, st);
-    slot += ph.n_split;
+    if (!ok) { launched(e); return PC_ERR_CUDA; }
+    if (!ph.finish) slot += ph.n_split;
+    made = true;
   }
   if (e != cudaSuccess || plan.finished) return launched(e);
   return launched(pc::launch_cache_merge(merge, a->d, st));

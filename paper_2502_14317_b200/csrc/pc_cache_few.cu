@@ -25,10 +25,12 @@ namespace pc {
 
 namespace {
 
+// CAUSAL: the entries are the new tokens themselves, token i sees 0 .. i.
 // SHORT: four CTAs per SM (16 rows: three) of three consumer warps and stages of half the size, for many sequences with few entries
-template <int D_, int FMT_, int NT8_, bool SHORT_>
+template <int D_, int FMT_, int NT8_, bool SHORT_, bool CAUSAL_ = false>
 struct Few {
   static constexpr int D = D_, FMT = FMT_, NT8 = NT8_;
+  static constexpr bool CAUSAL = CAUSAL_;
   static constexpr int EB = FMT == FMT_BF16 ? 2 : 1;            // bytes of an element
   static constexpr int ROWB = D * EB, BOXES = ROWB > 128 ? 2 : 1, BOXB = ROWB / BOXES, EPB = BOXB / EB;
   // Consumer warps: with the producers 16 warps an SM, 128 registers a thread, or 12 and 168.
@@ -48,6 +50,7 @@ struct __align__(16) FewMisc {
   uint64_t full[C::NS], empty[C::NS];
   int abort_flag;                                               // these two words stay adjacent (bounded waits)
   int wait_kcycles;
+  int odd;                                                      // causal: a value that is no number
   float qs[C::N];                                               // scale of a row's logits, in log2 units
   float2 ml[C::WARPS][C::N], all[C::N];                         // maximum and sum of a row: of a warp, of the CTA
 };
@@ -117,6 +120,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     for (int i = 0; i < NS; ++i) { mbar_init(&mi.full[i], Q8 ? 33 : 1); mbar_init(&mi.empty[i], C::WARPS); }
     mi.abort_flag = 0;
     mi.wait_kcycles = prm.wait_kcycles;
+    mi.odd = 0;
     fence_mbar_init();
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
@@ -232,6 +236,15 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       for (int t = 0; t < NT8; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[j][t][e] = 0.0f;
+    // causal: a row sees the new tokens up to its own
+    [[maybe_unused]] int own[NT8][2];
+    if constexpr (C::CAUSAL) {
+      const int G = prm.q.Hq / prm.q.Hkv;
+#pragma unroll
+      for (int t = 0; t < NT8; ++t)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) own[t][e] = (row0 + 8 * t + 2 * a + e) / G % prm.q.w;
+    }
     // Places of this thread's chunks in a unit, whose rows begin at a multiple of 16: the swizzle of a row goes by its last bits.
     // K: chunk a CPT + h of keys g and g + 8;  V: chunk g of keys 2 a + e and 2 a + e + 8.
     uint32_t k_at[C::CPT], v_at[2];
@@ -323,6 +336,24 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
               for (int b = 0; b < C::BOXES; ++b)
 #pragma unroll
                 for (int y = 0; y < C::BOXB / 32; ++y) v[b][k][y] = 0;
+        }
+        if constexpr (C::CAUSAL) {
+#pragma unroll
+          for (int t = 0; t < NT8; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (key0 + g + (e < 2 ? 0 : 8) > own[t][e & 1]) z[t][e] = -INFINITY;
+          // A value that is no number would reach the rows that do not see it, times their zero: then the rows take these keys one by one.
+          {
+            bool odd = false;
+#pragma unroll
+            for (int b = 0; b < C::BOXES; ++b)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int y = 0; y < C::BOXB / 32; ++y) odd |= (v[b][k][y] & 0x7F80u) == 0x7F80u || (v[b][k][y] & 0x7F800000u) == 0x7F800000u;
+            if (odd) mi.odd = 1;
+          }
         }
         // ---- probabilities
         uint32_t pb[NT8][2];
@@ -441,7 +472,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       o.x = fmaf(f, y.x, o.x); o.y = fmaf(f, y.y, o.y); o.z = fmaf(f, y.z, o.z); o.w = fmaf(f, y.w, o.w);
     }
     const size_t at = part0 + (size_t)r * prm.n_slots;
-    const float2 ml = sum == 0.0f ? make_float2(-INFINITY, 0.0f) : make_float2(top, sum);
+    const float2 ml = sum == 0.0f || (C::CAUSAL && mi.odd) ? make_float2(-INFINITY, 0.0f) : make_float2(top, sum);
     if (finish) {
       reinterpret_cast<float4*>(smem)[r * (D / 4) + c] = o;
       if (c == 0) mi.all[r] = ml;
@@ -468,7 +499,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     sum.join(mine, prm.n_split, [&](int s, float (&y)[E]) { ld_cluster<E>(map_to_cta(reinterpret_cast<const float*>(smem) + r * D + lane * E, s), y); });
     const size_t slots = ((size_t)hkv * prm.total_rows + row) * fin.n_slots;
     sum.join_slots(fin.part_ml + slots, fin.part_o + slots * D, fin.n_slots, 0, 1, lane);
-    if (fin.k_win != nullptr) {
+    if (fin.k_win != nullptr && (!C::CAUSAL || mi.odd)) {
       uint32_t y[E / 2];
       float q[E];
 #pragma unroll
@@ -492,16 +523,22 @@ cudaError_t few_t(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CacheP
                         finish ? p.n_split : 1, tm_k, tm_v, p, finish ? *finish : CacheMerge{}, finish != nullptr ? 1 : 0);
 }
 template <int D, int FMT>
-cudaError_t few_n(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool brief, cudaStream_t st) {
-  if (few_rows(p.rows) == 8)
+cudaError_t few_n(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, int group, bool brief, cudaStream_t st) {
+  if (group == 8)
     return brief ? few_t<Few<D, FMT, 1, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT, 1, false>>(tm_k, tm_v, p, finish, st);
   return brief ? few_t<Few<D, FMT, 2, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT, 2, false>>(tm_k, tm_v, p, finish, st);
 }
 template <int D>
-cudaError_t few_d(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool brief, int format, cudaStream_t st) {
-  return format == FMT_INT8   ? few_n<D, FMT_INT8>(tm_k, tm_v, p, finish, brief, st)
-         : format == FMT_E4M3 ? few_n<D, FMT_E4M3>(tm_k, tm_v, p, finish, brief, st)
-                              : few_n<D, FMT_BF16>(tm_k, tm_v, p, finish, brief, st);
+cudaError_t few_causal(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, int group, cudaStream_t st) {
+  return group == 8 ? few_t<Few<D, FMT_BF16, 1, false, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT_BF16, 2, true, true>>(tm_k, tm_v, p, finish, st);
+}
+template <int D>
+cudaError_t few_d(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, int group, bool brief, int format,
+                  cudaStream_t st) {
+  if (p.causal) return few_causal<D>(tm_k, tm_v, p, finish, group, st);
+  return format == FMT_INT8   ? few_n<D, FMT_INT8>(tm_k, tm_v, p, finish, group, brief, st)
+         : format == FMT_E4M3 ? few_n<D, FMT_E4M3>(tm_k, tm_v, p, finish, group, brief, st)
+                              : few_n<D, FMT_BF16>(tm_k, tm_v, p, finish, group, brief, st);
 }
 template <bool SHORT>
 int keys_t(int format, int d) {
@@ -511,11 +548,10 @@ int keys_t(int format, int d) {
 
 }  // namespace
 
-int few_rows(int rows) { return rows <= 8 ? 8 : 16; }
 int few_keys(int format, int d, bool brief) { return brief ? keys_t<true>(format, d) : keys_t<false>(format, d); }
-cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool brief, int format,
-                             int d, cudaStream_t st) {
-  return d == 128 ? few_d<128>(tm_k, tm_v, p, finish, brief, format, st) : few_d<64>(tm_k, tm_v, p, finish, brief, format, st);
+cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, int group, bool brief,
+                             int format, int d, cudaStream_t st) {
+  return d == 128 ? few_d<128>(tm_k, tm_v, p, finish, group, brief, format, st) : few_d<64>(tm_k, tm_v, p, finish, group, brief, format, st);
 }
 
 }  // namespace pc
