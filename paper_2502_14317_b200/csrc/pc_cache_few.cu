@@ -427,6 +427,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             }
           }
       }
+      // (the products of the loop above have been issued, so what they need has been loaded: an arrival itself waits for no load)
       __syncwarp();
       if (lane == 0) mbar_arrive(&mi.empty[st]);
       if (++st == NS) { st = 0; ++lap; }

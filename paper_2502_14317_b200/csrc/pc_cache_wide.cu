@@ -136,7 +136,6 @@ struct Converter {
         off ^= ((off >> 7) & (BYTES == 128 ? 7 : 3)) << 4;
         in[u] = *reinterpret_cast<const uint4*>(from + off);
       }
-      if (i0 + 4 == STEPS) warp_arrive(&ex.raw_free[slot]);
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int local = (i0 + u) * (32 / LPR) + lane_row, row = warp * (ROWS / 4) + local;
@@ -163,6 +162,9 @@ struct Converter {
       warp_arrive(&ex.sc_full[at % 8]);
     }
     fence_proxy_async_smem();
+    // Behind the stores, which need what was loaded.  An arrival waits for no load that is still on its way: right behind the loads it let
+    // the next copy overtake them where the SM's shared memory was busy.
+    warp_arrive(&ex.raw_free[slot]);
     warp_arrive(&mi.kv_full[st]);                          // (of a pair's peer: an issuer's warp there passes it on to the leader)
     ++n;
     ++raws;

@@ -319,6 +319,61 @@ def test_same_results_every_time_on_any_stream_and_with_kept_buffers():
     torch.cuda.current_stream().wait_stream(side)
 
 
+@pytest.mark.parametrize("pf,of", [("int8", ""), ("e4m3", "int8"), ("bf16", "e4m3"), ("", "int8"), ("", "bf16")])
+@pytest.mark.parametrize("B,w,Hq,Hkv,d,n_prefix,n_own", [(256, 1, 32, 8, 128, 9000, 100), (128, 1, 32, 8, 64, 9000, 30), (64, 1, 32, 8, 128, 5000, 700),
+                                                         (70, 2, 8, 8, 128, 3000, 50), (20, 1, 16, 4, 64, 4000, 2000), (2, 40, 8, 2, 128, 5000, 90)])
+def test_calls_in_a_row(pf, of, B, w, Hq, Hkv, d, n_prefix, n_own):
+    """Calls that follow each other without a pause, on other inputs in between, give the bits of calls on an idle GPU."""
+    if not pf:
+        n_prefix = 0
+    states = []
+    for seed in (200, 220, 240):
+        q, kw, vw = _normal(seed, B, w, Hq, d).cuda(), _normal(seed + 1, B, w, Hkv, d).cuda(), _normal(seed + 2, B, w, Hkv, d).cuda()
+        prefix = _cache(seed + 3, 1, Hkv, n_prefix, 0, d, pf) if pf else None
+        own = _cache(seed + 5, B, Hkv, n_own, 0, d, of) if of else None
+        states.append((q, kw, vw, dict(prefix=prefix, own=own, rope_theta=1e4, q_pos0=100, want_lse=True, buffers={})))
+    call = lambda s: pc.cache_attn(*s[:3], **s[3])                                    # noqa: E731
+    alone = []
+    for s in states:
+        torch.cuda.synchronize()
+        r = call(s)
+        torch.cuda.synchronize()
+        alone.append((r["out"].clone(), r["lse"].clone()))
+    for i in range(12):
+        for j in (1, 2, 0):
+            r = call(states[(i + j) % 3])
+        assert torch.equal(r["out"], alone[i % 3][0]) and torch.equal(r["lse"], alone[i % 3][1]), i
+        assert r["status"].item() == 0
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "int8"])
+def test_a_later_token_that_is_no_number_stays_where_it_is_seen(fmt):
+    """Windows of more and of fewer than 8 tokens: NaN and infinity in a token's key or value reach no earlier row."""
+    for w, B in ((40, 1), (12, 20), (5, 3)):
+        q, kw, vw = _normal(150, B, w, 4, 64), _normal(151, B, w, 2, 64), _normal(152, B, w, 2, 64)
+        cache = _cache(153, 1, 2, 300, 0, 64, fmt)
+        want = ref.f64(pc.cache_attn(q.cuda(), kw.cuda(), vw.cuda(), prefix=cache)["out"])
+        t = w - 3
+        vw[:, t, 1, 5], kw[:, t + 1, 1, 9] = NAN, float("inf")
+        got = ref.f64(pc.cache_attn(q.cuda(), kw.cuda(), vw.cuda(), prefix=cache)["out"])
+        assert np.abs(got[:, :t] - want[:, :t]).max() <= 2.0 ** -7 * np.abs(want).max()      # a row's keys may be taken another way: a bf16 step
+        assert np.abs(got[:, :, :2] - want[:, :, :2]).max() <= 2.0 ** -7 * np.abs(want).max()
+        assert np.isnan(got[:, t:, 2:, 5]).all()
+
+
+def test_broadcast_windows():
+    """Keys and values of new tokens that are the same for all heads or sequences, through strides of 0, as copies of them give."""
+    for w in (3, 20):
+        q, one = _normal(160, 4, w, 4, 64).cuda(), _normal(161, 4, w, 1, 64).cuda()
+        cache = _cache(162, 1, 2, 200, 0, 64, "int8")
+        for win in (one.expand(4, w, 2, 64), one[:1].expand(4, w, 1, 64).repeat(1, 1, 2, 1)[:1].expand(4, w, 2, 64)):
+            a = pc.cache_attn(q, win, win, prefix=cache, want_lse=True)
+            b = pc.cache_attn(q, win.contiguous(), win.contiguous(), prefix=cache, want_lse=True)
+            # w = 20: strides of 0 take the keys one by one, copies go through the matrix units: P in bf16 (2^-9), the output a step
+            assert (a["out"].float() - b["out"].float()).abs().max() <= 2.0 ** -6 * b["out"].float().abs().max()
+            assert (a["lse"] - b["lse"]).abs().max() <= 1e-4
+
+
 def test_decoding_steps_over_a_growing_cache():
     """Step after step: attend, then append; the same as one call with the window over all of them."""
     B, Hq, Hkv, d, n0, steps = 2, 4, 2, 64, 30, 5
