@@ -84,6 +84,7 @@ struct CachePhase {
 // group: 8 or 16 rows; brief: the build for many sequences with few entries.
 // maps of the cache's keys and values: boxes of few_keys() entries
 int few_keys(int format, int d, bool brief);     // keys of a stage
+int few_clusters(int n);                         // clusters of n CTAs that the current device runs at a time (not brief)
 cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, int group, bool brief,
                              int format, int d, cudaStream_t st);
 

@@ -4,6 +4,7 @@
 #include "pc_kernels.h"
 #include "pc_tmap.h"
 
+#include <atomic>
 #include <cmath>
 
 namespace {
@@ -101,10 +102,24 @@ struct CachePlan {
   size_t off_counter, off_rows, off_halves, off_scale, off_ml, off_o, total;
 };
 
+// Clusters of n <= 8 CTAs of the kernel for few rows that the current device runs at a time (asked once per device).
+int few_fit(int n) {
+  static std::atomic<int> known[64][9];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
+  std::atomic<int>& k = known[dev][n];
+  int v = k.load(std::memory_order_relaxed);
+  if (v == 0) k.store(v = pc::few_clusters(n) + 1, std::memory_order_relaxed);
+  return v - 1;
+}
+
 // Splits of the keys, and whether the kernel finishes its rows itself (the last phase; up to 8 splits, the CTAs of a cluster)
-// or leaves slots for the merge.  Least time by a model in microseconds: rounds of the grid, two CTAs per SM, x (7 for the queries, the
-// first unit and the join + its tiles, at a unit in 0.9 (8 rows) or 1.15 for a warp, or at the CTA's share of the memory's rate), and for
-// slots 1 + 0.1 a split for writing and merging them.
+// or leaves slots for the merge.  Least time by a model in microseconds: rounds of the grid, two CTAs per SM, x (7.5 for the queries, the
+// first unit and the join + its tiles, at a unit in 1.1 (8 rows) or 1.4 for a warp, 0.63 or 0.95 where the SM has one CTA, or at the
+// CTA's share of the rate of L2 and memory), and for
+// slots 1 + 0.1 a split for writing and merging them.  Measured, us, finished / slots, best split of each: one token over 16401 int8
+// entries, 8 kv-heads 19.8 (8) / 15.7 (16); 2000 entries, four sequences 11.2 (8) / 11.8 (4); 4 tokens of 23 sequences of up to 5000,
+// head size 64 22.3 (3) / 23.9 (3); 40 sequences of 4000, one kv-head 16.4 (3) / 17.7 (3).
 PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, bool last, int sm_count) {
   PhasePlan p = {};
   p.group = rows <= 8 ? 8 : 16;
@@ -115,15 +130,20 @@ PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n
   p.n_split = 1;
   p.finish = last;
   if (p.brief) return p;
-  const double tile_us = 2.0 * keys * d * (format == PC_KV_BF16 ? 2 : 1) / 6.5e6, alone = keys / 16 * (p.group == 8 ? 0.9 / 7 : 1.15 / 5);
+  const double tile_us = 2.0 * keys * d * (format == PC_KV_BF16 ? 2 : 1) / 8.0e6, units = keys / 16;
   double least = -1.0;
-  for (int s = 1; s <= 64 && s <= tiles; ++s) {
-    const bool finish = last && s <= 8;
-    const double fit = std::floor(2.0 * sm_count / s);
+  auto look = [&](int s, bool finish) {
+    const double fit = finish && s > 1 ? few_fit(s) : std::floor(2.0 * sm_count / s);
+    if (fit < 1.0) return;
     const double rounds = std::ceil(items / fit), active = (items < fit ? items : fit) * s;
-    const double cost = rounds * (7.0 + (tile_us * active > alone ? tile_us * active : alone) * std::ceil((double)tiles / s)) +
-                        (finish ? 0.0 : 1.0 + 0.1 * s);
+    const bool single = active <= sm_count;                          // a CTA has its SM for itself
+    const double alone = units * (p.group == 8 ? (single ? 0.63 : 1.1) / 7 : (single ? 0.95 : 1.4) / 5), bytes = tile_us * active;
+    const double cost = rounds * (7.5 + (bytes > alone ? bytes : alone) * std::ceil((double)tiles / s)) + (finish ? 0.0 : 1.0 + 0.1 * s);
     if (least < 0.0 || cost < least) { least = cost; p.n_split = s; p.finish = finish; }
+  };
+  for (int s = 1; s <= 64 && s <= tiles; ++s) {
+    if (last && s <= 8) look(s, true);
+    look(s, false);
   }
   return p;
 }

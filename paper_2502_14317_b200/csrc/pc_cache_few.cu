@@ -541,6 +541,26 @@ cudaError_t few_d(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CacheP
          : format == FMT_E4M3 ? few_n<D, FMT_E4M3>(tm_k, tm_v, p, finish, group, brief, st)
                               : few_n<D, FMT_BF16>(tm_k, tm_v, p, finish, group, brief, st);
 }
+template <class C>
+int clusters_t(int n) {
+  constexpr int SMEM = C::OFF_MISC + (int)sizeof(FewMisc<C>);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)n);
+  cfg.blockDim = dim3(C::THREADS);
+  cfg.dynamicSmemBytes = SMEM;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {(unsigned)n, 1, 1};
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int fit = 0;
+  if (cudaFuncSetAttribute(cache_few_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM) != cudaSuccess ||
+      cudaOccupancyMaxActiveClusters(&fit, cache_few_kernel<C>, &cfg) != cudaSuccess) {
+    cudaGetLastError();
+    return 0;
+  }
+  return fit;
+}
 template <bool SHORT>
 int keys_t(int format, int d) {
   if (format == FMT_BF16) return d == 128 ? Few<128, FMT_BF16, 1, SHORT>::KEYS : Few<64, FMT_BF16, 1, SHORT>::KEYS;
@@ -549,6 +569,7 @@ int keys_t(int format, int d) {
 
 }  // namespace
 
+int few_clusters(int n) { return clusters_t<Few<128, FMT_INT8, 2, false>>(n); }      // (all builds take half an SM's shared memory)
 int few_keys(int format, int d, bool brief) { return brief ? keys_t<true>(format, d) : keys_t<false>(format, d); }
 cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, int group, bool brief,
                              int format, int d, cudaStream_t st) {
