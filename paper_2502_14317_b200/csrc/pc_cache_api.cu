@@ -125,7 +125,9 @@ PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n
   p.group = rows <= 8 ? 8 : 16;
   p.n_rg = (int)((rows + p.group - 1) / p.group);
   const double items = (double)seqs * Hkv * p.n_rg;
-  p.brief = items > 2.0 * sm_count && n_keys <= 512;
+  // More than a round of CTAs over short caches: four smaller ones per SM (16 rows: three).  Measured, us, two / four (three), 320 items of 60 entries
+  // 14.3 / 10.0, of 1000 30.6 / 29.4, 1024 of 60 29.2 / 18.2, of 2000 102.4 / 98.9; 16 rows, 640 of 60 17.4 / 14.1, 2048 of 1000 71.4 / 77.2.
+  p.brief = items > 2.0 * sm_count && n_keys <= (p.group == 8 ? 2048 : 1024);
   const int keys = pc::few_keys(format, d, p.brief), tiles = (n_keys + keys - 1) / keys;
   p.n_split = 1;
   p.finish = last;
@@ -202,7 +204,7 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     if (!ph.finish) p.n_slots += ph.n_split;
     p.finished |= ph.finish;
     // more than a round of CTAs: cheaper than each of them rotating its own
-    if (!ph.wide && (own ? a->B : 1.0) * a->Hkv * ph.n_rg * ph.n_split > 2.0 * sm_count) p.rows = true;
+    if (!ph.wide && (own ? a->B : 1.0) * a->Hkv * ph.n_rg * ph.n_split > (ph.brief ? ph.group == 8 ? 4.0 : 3.0 : 2.0) * sm_count) p.rows = true;
   }
   if (window) {
     const int64_t rows = (int64_t)a->w * G;
