@@ -125,9 +125,12 @@ PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n
   p.group = rows <= 8 ? 8 : 16;
   p.n_rg = (int)((rows + p.group - 1) / p.group);
   const double items = (double)seqs * Hkv * p.n_rg;
-  // More than a round of CTAs over short caches: four smaller ones per SM (16 rows: three).  Measured, us, two / four (three), 320 items of 60 entries
-  // 14.3 / 10.0, of 1000 30.6 / 29.4, 1024 of 60 29.2 / 18.2, of 2000 102.4 / 98.9; 16 rows, 640 of 60 17.4 / 14.1, 2048 of 1000 71.4 / 77.2.
-  p.brief = items > 2.0 * sm_count && n_keys <= (p.group == 8 ? 2048 : 1024);
+  // Short caches: four smaller CTAs per SM (16 rows: three) where they take fewer rounds than two; up to 2048 entries for half the rounds, else 1024.
+  // Measured, us, two / four (three), full int8 caches of head size 128.  8 rows: 320 items of 60 entries 14.6 / 8.9, of 1000 30.5 / 28.2, of 2000
+  // 49.8 / 47.7 (ragged, up to 1000 21.8 / 23.6, up to 2000 37.5 / 39.4); 768 of 1000 54.0 / 55.9 (ragged 42.8 / 38.7), of 2000 84.3 / 92.0.
+  // 16 rows: 384 of 1000 57.0 / 41.4; 512 (as many rounds) 56.4 / 67.7; 768 81.5 / 79.2, of 2000 120.5 / 124.2.
+  const double small = (p.group == 8 ? 4.0 : 3.0) * sm_count, rounds2 = std::ceil(items / (2.0 * sm_count)), rounds4 = std::ceil(items / small);
+  p.brief = rounds4 < rounds2 && n_keys <= (2.0 * rounds4 <= rounds2 ? 2048 : 1024);
   const int keys = pc::few_keys(format, d, p.brief), tiles = (n_keys + keys - 1) / keys;
   p.n_split = 1;
   p.finish = last;
@@ -203,7 +206,8 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     if ((own ? a->B : 1ll) * a->Hkv * ph.n_rg * ph.n_split > 0x7FFFFFFF) return PC_ERR_UNSUPPORTED;
     if (!ph.finish) p.n_slots += ph.n_split;
     p.finished |= ph.finish;
-    // more than a round of CTAs: cheaper than each of them rotating its own
+    // More than a round of CTAs: cheaper than each of them rotating its own.  Measured, us, rotated ahead / by the CTAs, short CTAs of one round:
+    // 320 items of 60 entries 10.3 / 8.9, 384 of 16 rows of 1000 43.1 / 41.4.
     if (!ph.wide && (own ? a->B : 1.0) * a->Hkv * ph.n_rg * ph.n_split > (ph.brief ? ph.group == 8 ? 4.0 : 3.0 : 2.0) * sm_count) p.rows = true;
   }
   if (window) {
