@@ -751,26 +751,19 @@ def hot_path_from_host(hq, hk, hv, *, w, rope_theta, m, k_keep, softmax_scale=0.
 
 
 # ------------------------------------------------------------------------------------ 8-bit caches, attention over shared and own caches
-class _KvCache(Structure):                                 # pc_kv_cache for gather_kv_quantize; the calls beside it fill it in csrc/pc_host.cpp
-    _fields_ = [("format", c_int32), ("B", c_int32), ("Hkv", c_int32), ("d", c_int32), ("capacity", c_int64), ("k", c_void_p), ("v", c_void_p),
-                ("k_scale", c_void_p), ("v_scale", c_void_p)]
-
-
 _ALL = -2 ** 63                                           # as many entries as a cache holds
-_FORMATS = {"bf16": (0, torch.bfloat16), "int8": (1, torch.int8), "e4m3": (2, torch.float8_e4m3fn)}
+_FORMATS = {"bf16": torch.bfloat16, "int8": torch.int8, "e4m3": torch.float8_e4m3fn}
 
 
 class _CacheCalls:
-    """The calls below on a library's entry points, those that csrc/pc_host.cpp makes with their addresses."""
+    """The calls below: csrc/pc_host.cpp makes them, with the addresses of a library's entry points."""
 
     def __init__(self, lib):
         host = _host_module()
         self.quantize = functools.partial(host.kv_quantize, _address(lib.pc_kv_quantize))
         self.dequantize = functools.partial(host.kv_dequantize, _address(lib.pc_kv_dequantize))
         self.attn = functools.partial(host.cache_attn, _address(lib.pc_cache_attn_workspace_bytes), _address(lib.pc_cache_attn))
-        self.gather = lib.pc_gather_kv_quantize
-        self.gather.restype = c_int32
-        self.gather.argtypes = [c_void_p, c_void_p, POINTER(c_int64), c_void_p, c_void_p, c_int32, c_int32, POINTER(_KvCache), c_void_p, c_void_p]
+        self.gather = functools.partial(host.gather_kv_quantize, _address(lib.pc_gather_kv_quantize))
 
 
 def _cache_calls():
@@ -786,7 +779,7 @@ def kv_cache(B, Hkv, capacity, d, format, device="cuda"):
     [B,Hkv,capacity] fp32.  The tensors of an existing bf16 cache serve as {"format": "bf16", "k": k, "v": v}."""
     if format not in _FORMATS:
         raise PcError("format must be one of %s" % ", ".join(_FORMATS))
-    k, v = (torch.zeros((B, Hkv, capacity, d), dtype=_FORMATS[format][1], device=device) for _ in range(2))
+    k, v = (torch.zeros((B, Hkv, capacity, d), dtype=_FORMATS[format], device=device) for _ in range(2))
     ks, vs = (None, None) if format == "bf16" else (torch.zeros((B, Hkv, capacity), dtype=torch.float32, device=device) for _ in range(2))
     return {"format": format, "k": k, "v": v, "k_scale": ks, "v_scale": vs}
 
@@ -810,33 +803,13 @@ def gather_kv_quantize(k_src, v_src, kept, idx, cache=None, *, format="int8", po
     """pc_gather_kv_quantize: as gather_kv, into an 8-bit cache of one sequence (made here if none is given).
 
     Returns (cache, pos [Hkv, m*k] or None)."""
-    calls = _cache_calls()
-    _need_cuda(k_src, v_src, kept, idx)
-    C, L, Hkv, d = k_src.shape
-    m, _, k = idx.shape
-    dev = k_src.device
-    if not _same_rows(k_src, v_src) or not (k_src.dtype is v_src.dtype is torch.bfloat16) or v_src.shape != k_src.shape or v_src.device != dev:
-        raise PcError("k_src and v_src must be bfloat16 and share strides with a contiguous head dimension")
-    if idx.shape[1] != Hkv or kept.shape != (m,) or not (idx.dtype is kept.dtype is torch.int32 and idx.is_contiguous() and kept.is_contiguous()
-                                                         and idx.device == kept.device == dev):
-        raise PcError("idx must be contiguous int32 [m, Hkv, k], kept contiguous int32 [m]")
     if cache is None:
-        cache = kv_cache(1, Hkv, m * k, d, format, dev)
-    number, dtype = _FORMATS.get(cache["format"], (0, None))
-    kc, scales = cache["k"], (cache.get("k_scale"), cache.get("v_scale"))
-    if number == 0 or kc.dim() != 4 or kc.shape[:2] != (1, Hkv) or kc.shape[2] < m * k or kc.shape[3] != d or \
-            not all(t.shape == kc.shape and t.dtype is dtype and t.is_contiguous() and t.device == dev for t in (kc, cache["v"])) or \
-            not all(t is not None and t.shape == kc.shape[:3] and t.dtype is torch.float32 and t.is_contiguous() and t.device == dev for t in scales):
-        raise PcError("the cache must be an 8-bit one that holds m * k entries of one sequence, with the Hkv and d of k_src")
-    if pos_out is None and want_pos:
-        pos_out = torch.empty((Hkv, m * k), dtype=torch.int32, device=dev)
-    if pos_out is not None and (pos_out.shape != (Hkv, m * k) or pos_out.dtype is not torch.int32 or not pos_out.is_contiguous() or
-                                pos_out.device != dev):
-        raise PcError("pos_out must be contiguous int32 [Hkv, m*k]")
-    desc = _KvCache(number, 1, Hkv, d, kc.shape[2], kc.data_ptr(), cache["v"].data_ptr(), scales[0].data_ptr(), scales[1].data_ptr())
-    _check(calls.gather(k_src.data_ptr(), v_src.data_ptr(), _Strides(*k_src.stride()[:3]), kept.data_ptr(), idx.data_ptr(), m, k,
-                        ctypes.byref(desc), _ptr(pos_out), _stream()), "pc_gather_kv_quantize")
-    return cache, pos_out
+        m, Hkv, k = idx.shape
+        cache = kv_cache(1, Hkv, m * k, k_src.shape[-1], format, k_src.device)
+    got = _cache_calls().gather(_stream(), True, k_src, v_src, kept, idx, cache, pos_out, want_pos)
+    if got[0] != 0:
+        _refused(got if isinstance(got, str) else got[0], "pc_gather_kv_quantize")
+    return cache, got[1]
 
 
 def kv_dequantize(cache, n=None, *, at=0, k_out=None, v_out=None):

@@ -289,6 +289,46 @@ PyObject* kv_quantize(PyObject*, PyObject* args) {
   END_HANDLE_TH_ERRORS
 }
 
+// gather_kv_quantize(run, stream, need_cuda, k_src, v_src, kept, idx, cache, pos_out or None, want_pos) -> (result code, pos or None), or the
+// reason of a refusal
+PyObject* gather_kv_quantize(PyObject*, PyObject* args) {
+  HANDLE_TH_ERRORS
+  unsigned long long run, stream;
+  int cuda, want_pos;
+  PyObject *src[2], *which[2], *dict, *pos_out;
+  if (!PyArg_ParseTuple(args, "KKpOOOOOOp", &run, &stream, &cuda, &src[0], &src[1], &which[0], &which[1], &dict, &pos_out, &want_pos)) return nullptr;
+  return refusing([&]() -> PyObject* {
+    const char* const bad = "k_src and v_src must be bfloat16 [C, L, Hkv, d] and share strides with a contiguous head dimension, on one device";
+    const char* const bad_idx = "idx must be contiguous int32 [m, Hkv, k], kept contiguous int32 [m], on the device of k_src";
+    at::Tensor k, v, kept, idx, pos;
+    need(is_tensor(src[0], k, bad) && is_tensor(src[1], v, bad) && k.dim() == 4 && k.sizes().equals(v.sizes()) && k.strides().equals(v.strides()) &&
+         k.stride(3) == 1 && k.scalar_type() == at::kBFloat16 && v.scalar_type() == at::kBFloat16 && k.device() == v.device(), bad);
+    need(!cuda || k.is_cuda(), "tensors must live on a CUDA device");
+    need(is_tensor(which[0], kept, bad_idx) && is_tensor(which[1], idx, bad_idx) && idx.dim() == 3 && kept.dim() == 1 && kept.size(0) == idx.size(0) &&
+         idx.size(1) == k.size(2) && idx.size(0) <= INT32_MAX && idx.size(2) <= INT32_MAX, bad_idx);
+    for (const at::Tensor* t : {&kept, &idx}) need(t->scalar_type() == at::kInt && t->is_contiguous() && t->device() == k.device(), bad_idx);
+    const int64_t m = idx.size(0), Hkv = idx.size(1), n = idx.size(2);
+    const Cache c(dict);
+    need(c.c.format != PC_KV_BF16 && c.c.B == 1 && c.c.Hkv == Hkv && c.c.capacity >= m * n && c.c.d == k.size(3) && c.device == k.device(),
+         "the cache must be an 8-bit one that holds m * k entries of one sequence, with the Hkv and d of k_src, on its device");
+    const char* const bad_pos = "pos_out must be contiguous int32 [Hkv, m*k] on the device of k_src";
+    const int64_t sizes[2] = {Hkv, m * n};
+    const bool given = is_tensor(pos_out, pos, bad_pos);
+    if (given)
+      need(pos.sizes().equals(sizes) && pos.scalar_type() == at::kInt && pos.is_contiguous() && pos.device() == k.device(), bad_pos);
+    else if (want_pos)
+      pos = at::empty(sizes, at::TensorOptions().dtype(at::kInt).device(k.device()));
+    const int64_t stride[3] = {k.stride(0), k.stride(1), k.stride(2)};
+    using fn = int32_t (*)(const void*, const void*, const int64_t*, const int32_t*, const int32_t*, int32_t, int32_t, const pc_kv_cache*, int32_t*, void*);
+    const int32_t rc = entry<fn>(run)(k.data_ptr(), v.data_ptr(), stride, static_cast<const int32_t*>(kept.data_ptr()),
+                                      static_cast<const int32_t*>(idx.data_ptr()), (int32_t)m, (int32_t)n, &c.c,
+                                      pos.defined() ? static_cast<int32_t*>(pos.data_ptr()) : nullptr, entry<void*>(stream));
+    PyObject* const x = given ? (Py_INCREF(pos_out), pos_out) : pos.defined() ? THPVariable_Wrap(pos) : (Py_INCREF(Py_None), Py_None);
+    return Py_BuildValue("iN", (int)rc, x);
+  });
+  END_HANDLE_TH_ERRORS
+}
+
 // kv_dequantize(run, stream, need_cuda, cache, n or None, at, k_out or None, v_out or None) -> (result code, k, v), or the reason of a refusal
 PyObject* kv_dequantize(PyObject*, PyObject* args) {
   HANDLE_TH_ERRORS
@@ -440,6 +480,7 @@ PyObject* cache_attn(PyObject*, PyObject* args) {
 
 PyMethodDef methods[] = {{"hot_path", hot_path, METH_VARARGS, "See binding.py."},
                          {"kv_quantize", kv_quantize, METH_VARARGS, "See binding.py."},
+                         {"gather_kv_quantize", gather_kv_quantize, METH_VARARGS, "See binding.py."},
                          {"kv_dequantize", kv_dequantize, METH_VARARGS, "See binding.py."},
                          {"cache_attn", cache_attn, METH_VARARGS, "See binding.py."},
                          {nullptr, nullptr, 0, nullptr}};
