@@ -158,6 +158,8 @@ PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n
 PhasePlan wide_plan(int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count) {
   PhasePlan p = {};
   p.wide = true;
+  // CTA pairs for more rows than a block has.  Measured, us, without / with, 65536 entries: 128 rows bf16 57.5 / 66.9, int8 72.8 / 91.6; 256 rows 78.8 / 73.0,
+  // 127.3 / 96.7; 1024 rows 266.0 / 245.4, 314.7 / 268.1.
   p.pair = d == 128 && rows > 128 && sm_count >= 2;
   const int64_t block = p.pair ? 256 : 128, blocks = (rows + block - 1) / block, units = p.pair ? sm_count / 2 : sm_count;
   const int tiles = (n_keys + 127) / 128;
@@ -188,8 +190,10 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
   p.n_slots = 0;
   p.prefix = p.own = p.window = {};
   p.rows = p.halves = p.finished = false;
-  // More than 8 new tokens: their keys go through the matrix units, behind the caches' (up to 8: each row takes them one by one)
-  const bool window = a->k_win != nullptr && a->w > 8 && tma_strides(a->k_win_stride, a->B, a->w, a->Hkv) && tma_strides(a->v_win_stride, a->B, a->w, a->Hkv);
+  // More than 24 new tokens: their keys go through the matrix units, behind the caches' (up to 24: each row takes them one by one).  Measured, us, one by
+  // one / units, 32/8 heads of 128 over 2000 int8 entries, a sequence and 16 of them: 12 tokens 18.1 / 24.2, 70.8 / 76.6; 24 22.2 / 25.1, 144.8 / 134.5;
+  // 32 24.4 / 26.0, 197.7 / 167.7; 64 47.9 / 32.4, 442 / 320.
+  const bool window = a->k_win != nullptr && a->w > 24 && tma_strides(a->k_win_stride, a->B, a->w, a->Hkv) && tma_strides(a->v_win_stride, a->B, a->w, a->Hkv);
   for (int own = 0; own <= 1; ++own) {
     const pc_kv_cache* const c = own ? a->own : a->prefix;
     const int n = own ? a->n_own : a->n_prefix;
@@ -197,7 +201,10 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     if (int32_t rc = check_cache(c, false); rc != PC_OK) return rc;
     if (c->B != (own ? a->B : 1) || c->Hkv != a->Hkv || c->d != a->d || n > c->capacity) return PC_ERR_INVALID_ARG;
     PhasePlan& ph = own ? p.own : p.prefix;
-    if (!own && p.total_rows > 32) {
+    // More than 16 rows over the prefix: the kernel for many; over codes, whose conversion that makes for each of its few CTAs, and long prefixes more
+    // than 32.  Measured, us, few / many, head size 128, 16 rows 12.7 / 12.9 (bf16, 2000 entries), 22.7 / 27.8 (int8, 16000); 24 rows 14.3 / 13.3,
+    // 103.8 / 90.2 (131072), int8 16.0 / 14.4, 28.5 / 27.6, 117.3 / 119.8, e4m3 15.7 / 14.5, 26.8 / 26.8, 101.0 / 118.7; 40 rows int8 16.5 / 14.7, 166.0 / 121.0.
+    if (!own && p.total_rows > (c->format == PC_KV_BF16 || n <= 16384 ? 16 : 32)) {
       ph = wide_plan(p.total_rows, a->Hkv, a->d, c->format, n, sm_count);
       p.rows = true;
       p.halves = c->format != PC_KV_BF16;
@@ -214,10 +221,12 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     const int64_t rows = (int64_t)a->w * G;
     PhasePlan& ph = p.window;
     ph.n_split = 1; ph.finish = p.finished = true;
-    ph.group = (double)a->B * a->Hkv * ((rows + 7) / 8) <= 2.0 * sm_count ? 8 : 16;
-    ph.brief = ph.group == 16;
-    ph.n_rg = (int)((rows + ph.group - 1) / ph.group);
-    if ((int64_t)a->B * a->Hkv * ph.n_rg > 2 * sm_count) p.rows = true;
+    // Groups of 8 rows, more than a round of them on the short CTAs.  Measured, us, long / short, 16 tokens behind 4000 int8 entries, two sequences
+    // 27.0 / 29.7, 16 sequences 65.4 / 55.9 (long ones of 16 rows 63.3, short ones 67.0); 128 tokens 43.3 / 39.2 (42.8, 46.7).
+    ph.group = 8;
+    ph.n_rg = (int)((rows + 7) / 8);
+    ph.brief = (double)a->B * a->Hkv * ph.n_rg > 2.0 * sm_count;
+    if ((double)a->B * a->Hkv * ph.n_rg > 4.0 * sm_count) p.rows = true;
   }
   if (p.n_slots == 0 && !p.finished) p.rows = true;
   size_t off = 0;

@@ -530,13 +530,13 @@ cudaError_t few_n(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CacheP
   return brief ? few_t<Few<D, FMT, 2, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT, 2, false>>(tm_k, tm_v, p, finish, st);
 }
 template <int D>
-cudaError_t few_causal(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, int group, cudaStream_t st) {
-  return group == 8 ? few_t<Few<D, FMT_BF16, 1, false, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT_BF16, 2, true, true>>(tm_k, tm_v, p, finish, st);
+cudaError_t few_causal(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, bool brief, cudaStream_t st) {
+  return brief ? few_t<Few<D, FMT_BF16, 1, true, true>>(tm_k, tm_v, p, finish, st) : few_t<Few<D, FMT_BF16, 1, false, true>>(tm_k, tm_v, p, finish, st);
 }
 template <int D>
 cudaError_t few_d(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, int group, bool brief, int format,
                   cudaStream_t st) {
-  if (p.causal) return few_causal<D>(tm_k, tm_v, p, finish, group, st);
+  if (p.causal) return few_causal<D>(tm_k, tm_v, p, finish, brief, st);
   return format == FMT_INT8   ? few_n<D, FMT_INT8>(tm_k, tm_v, p, finish, group, brief, st)
          : format == FMT_E4M3 ? few_n<D, FMT_E4M3>(tm_k, tm_v, p, finish, group, brief, st)
                               : few_n<D, FMT_BF16>(tm_k, tm_v, p, finish, group, brief, st);
