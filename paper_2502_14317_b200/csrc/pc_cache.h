@@ -47,7 +47,9 @@ struct CacheRows {
   float theta, scale_log2;
   void *rows, *halves;           // halves: or null
   float* half_scale;             // [Hkv,B*w*G]
-  int *clear, *clear_too;        // words that are set to 0, or null
+  int *clear, *clear_too;        // two words and one that are set to 0, or null
+  float2* part_ml;               // slots of the rows, n_slots each, that are marked as empty, or null (a phase for many rows leaves out items without keys)
+  int n_slots;
 };
 cudaError_t launch_cache_rows(const CacheRows& p, int d, cudaStream_t st);
 
@@ -88,11 +90,11 @@ int few_clusters(int n);                         // clusters of n CTAs that the 
 cudaError_t launch_cache_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const CacheMerge* finish, int group, bool brief,
                              int format, int d, cudaStream_t st);
 
-// The same phase for more than 32 rows of one sequence (pc_cache_wide.cu), blocks of 128 rows.
+// The same phase for many rows of a sequence (pc_cache_wide.cu), blocks of 128 rows.  With len, which bf16 caches do not have here, the slots are marked
+// as empty ahead.
 struct WidePhase {
   CachePhase c;                  // n_rg, n_split: of the blocks below
   int alt;                       // 1: the two blocks of a CTA hold the same rows and take alternate key tiles; 0: different rows
-  int n_tiles;                   // 128-key tiles
   const float* half_scale;       // [Hkv,total_rows] (8-bit formats)
   int* counter;                  // work queue, zeroed
 };

@@ -98,7 +98,8 @@ struct CachePlan {
   int n_slots;                                   // results of a row in memory
   bool finished;                                 // the last phase finishes the rows: no merge
   int64_t total_rows;
-  bool rows, halves;                             // a launch for the rows (for a wide phase, or no phase at all), as halves as well (over 8-bit codes)
+  bool rows, halves, mark;                       // a launch for the rows (for a wide phase, or no phase at all), as halves as well (over 8-bit codes);
+                                                 // it marks the slots as empty (a wide phase over lengths)
   size_t off_counter, off_rows, off_halves, off_scale, off_ml, off_o, total;
 };
 
@@ -155,7 +156,7 @@ PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n
 
 // Row groups and splits of the kernel for many rows: least time by a model in microseconds, as for the query windows - rounds
 // of the grid x (5 for an item + a tile), and the partial results through memory twice.
-PhasePlan wide_plan(int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count) {
+PhasePlan wide_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count) {
   PhasePlan p = {};
   p.wide = true;
   // CTA pairs for more rows than a block has.  Measured, us, without / with, 65536 entries: 128 rows bf16 57.5 / 66.9, int8 72.8 / 91.6; 256 rows 78.8 / 73.0,
@@ -168,8 +169,8 @@ PhasePlan wide_plan(int64_t rows, int Hkv, int d, int format, int n_keys, int sm
     const int64_t n_rg = alt ? blocks : (blocks + 1) / 2;
     const double tile_us = alt ? 1.2 : 2.2;
     for (int s = 1; s <= 64 && (s == 1 || 2 * s <= tiles + 1); ++s) {
-      const double rounds = std::ceil((double)(Hkv * n_rg * s) / (double)units);
-      const double cost = rounds * (5.0 + tile_us * std::ceil((double)tiles / s)) + (double)(rows * Hkv * s) * d * 8.0 / 4.0e6;
+      const double rounds = std::ceil((double)seqs * (double)(Hkv * n_rg * s) / (double)units);
+      const double cost = rounds * (5.0 + tile_us * std::ceil((double)tiles / s)) + (double)seqs * (double)(rows * Hkv * s) * d * 8.0 / 4.0e6;
       if (least < 0.0 || cost < least) { least = cost; p.alt = alt; p.n_rg = (int)n_rg; p.n_split = s; }
     }
   }
@@ -189,7 +190,7 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
   p.total_rows = (int64_t)a->B * a->w * G;
   p.n_slots = 0;
   p.prefix = p.own = p.window = {};
-  p.rows = p.halves = p.finished = false;
+  p.rows = p.halves = p.mark = p.finished = false;
   // More than 24 new tokens: their keys go through the matrix units, behind the caches' (up to 24: each row takes them one by one).  Measured, us, one by
   // one / units, 32/8 heads of 128 over 2000 int8 entries, a sequence and 16 of them: 12 tokens 18.1 / 24.2, 70.8 / 76.6; 24 22.2 / 25.1, 144.8 / 134.5;
   // 32 24.4 / 26.0, 197.7 / 167.7; 64 47.9 / 32.4, 442 / 320.
@@ -204,18 +205,28 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     // More than 16 rows over the prefix: the kernel for many; over codes, whose conversion that makes for each of its few CTAs, and long prefixes more
     // than 32.  Measured, us, few / many, head size 128, 16 rows 12.7 / 12.9 (bf16, 2000 entries), 22.7 / 27.8 (int8, 16000); 24 rows 14.3 / 13.3,
     // 103.8 / 90.2 (131072), int8 16.0 / 14.4, 28.5 / 27.6, 117.3 / 119.8, e4m3 15.7 / 14.5, 26.8 / 26.8, 101.0 / 118.7; 40 rows int8 16.5 / 14.7, 166.0 / 121.0.
-    if (!own && p.total_rows > (c->format == PC_KV_BF16 || n <= 16384 ? 16 : 32)) {
-      ph = wide_plan(p.total_rows, a->Hkv, a->d, c->format, n, sm_count);
+    const int64_t seqs = own ? a->B : 1, rows = p.total_rows / seqs;
+    // Own caches: more than 48 rows of a sequence; bf16 more than 16, at head size 64 and little work 32 (what stands behind a length may be no number, and bf16
+    // values go to the matrix unit as they are: with lengths never).  Measured, us, few / many, 16 sequences of 2000 entries, 8 kv-heads: int8 d = 128 32 rows
+    // 46.7 / 54.7, 48 70.8 / 67.6, 64 94.5 / 73.1, 256 320.7 / 159.5; ragged e4m3 d = 64 48 39.9 / 48.3, 128 93.0 / 63.4; bf16 d = 128 16 34.2 / 35.1,
+    // 24 38.7 / 37.0, 64 85.2 / 56.8, d = 64 24 26.3 / 30.0, 48 43.4 / 39.1; 64 sequences, d = 64, 24 rows 94.7 / 78.7.
+    const bool bf16 = c->format == PC_KV_BF16;
+    const bool many = own ? rows > (!bf16 ? 48 : a->d == 128 || (double)seqs * a->Hkv > 2.0 * sm_count ? 16 : 32) && (!bf16 || a->own_len == nullptr)
+                          : rows > (bf16 || n <= 16384 ? 16 : 32);
+    if (many) {
+      ph = wide_plan(seqs, rows, a->Hkv, a->d, c->format, n, sm_count);
       p.rows = true;
-      p.halves = c->format != PC_KV_BF16;
-    } else
-    ph = few_plan(own ? a->B : 1, own ? (int64_t)a->w * G : p.total_rows, a->Hkv, a->d, c->format, n, !window && (own || a->n_own == 0), sm_count);
-    if ((own ? a->B : 1ll) * a->Hkv * ph.n_rg * ph.n_split > 0x7FFFFFFF) return PC_ERR_UNSUPPORTED;
+      p.halves |= !bf16;
+      p.mark |= own && a->own_len != nullptr;
+    } else {
+      ph = few_plan(seqs, rows, a->Hkv, a->d, c->format, n, !window && (own || a->n_own == 0), sm_count);
+    }
+    if (seqs * a->Hkv * ph.n_rg * ph.n_split > 0x7FFF0000) return PC_ERR_UNSUPPORTED;      // (a queue's counter goes on by the CTAs)
     if (!ph.finish) p.n_slots += ph.n_split;
     p.finished |= ph.finish;
     // More than a round of CTAs: cheaper than each of them rotating its own.  Measured, us, rotated ahead / by the CTAs, short CTAs of one round:
     // 320 items of 60 entries 10.3 / 8.9, 384 of 16 rows of 1000 43.1 / 41.4.
-    if (!ph.wide && (own ? a->B : 1.0) * a->Hkv * ph.n_rg * ph.n_split > (ph.brief ? ph.group == 8 ? 4.0 : 3.0 : 2.0) * sm_count) p.rows = true;
+    if (!ph.wide && (double)seqs * a->Hkv * ph.n_rg * ph.n_split > (ph.brief ? ph.group == 8 ? 4.0 : 3.0 : 2.0) * sm_count) p.rows = true;
   }
   if (window) {
     const int64_t rows = (int64_t)a->w * G;
@@ -303,6 +314,7 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
   if (plan.rows) {
     rows.clear = reinterpret_cast<int*>(ws + plan.off_counter);
     rows.clear_too = a->clear_status ? a->status_word : nullptr;
+    if (plan.mark) { rows.part_ml = reinterpret_cast<float2*>(ws + plan.off_ml); rows.n_slots = plan.n_slots; }
     if (plan.halves) { rows.halves = ws + plan.off_halves; rows.half_scale = reinterpret_cast<float*>(ws + plan.off_scale); }
     e = pc::launch_cache_rows(rows, a->d, st);
   } else if (a->clear_status && a->status_word) {
@@ -338,13 +350,13 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
     bool ok;
     if (ph.wide) {
       pc::WidePhase wp = {};
-      wp.c = p; wp.alt = ph.alt; wp.n_tiles = (n + 127) / 128;
+      wp.c = p; wp.alt = ph.alt;
       wp.half_scale = rows.half_scale;
-      wp.counter = rows.clear;
+      wp.counter = rows.clear + phase;
       const uint64_t d = (uint64_t)a->d, R = (uint64_t)plan.total_rows;
       const uint64_t dims[4] = {d, R, (uint64_t)a->Hkv, 1}, str[3] = {d, R * d, R * d * (uint64_t)a->Hkv};
       const uint32_t box[4] = {64, 128, 1, 1};
-      ok = pc::make_tmap_bf16_4d(&maps[0], plan.halves ? rows.halves : rows.rows, dims, str, box) &&
+      ok = pc::make_tmap_bf16_4d(&maps[0], c->format != PC_KV_BF16 ? rows.halves : rows.rows, dims, str, box) &&
            cache_maps(c, n, ph.pair ? 64 : 128, c->d, &maps[1], &unused) && cache_maps(c, n, 128, ph.pair ? 64 : c->d, &unused, &maps[2]);
       if (ok) e = pc::launch_cache_wide(maps, wp, c->format, a->d, ph.pair, sms, st);
     } else {

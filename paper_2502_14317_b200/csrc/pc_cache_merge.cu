@@ -16,7 +16,7 @@ __global__ void __launch_bounds__(256) cache_rows_kernel(const CacheRows p) {
   RowTurner<D> turner(p.theta, lane);
   chain();
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
-    if (p.clear != nullptr) *p.clear = 0;
+    if (p.clear != nullptr) p.clear[0] = p.clear[1] = 0;
     if (p.clear_too != nullptr) *p.clear_too = 0;
   }
   const int h = blockIdx.y * 8 + (threadIdx.x >> 5);
@@ -26,6 +26,8 @@ __global__ void __launch_bounds__(256) cache_rows_kernel(const CacheRows p) {
     turner.row(p, false, hkv, row, lane, x);
     const size_t at = (size_t)hkv * p.B * p.w * G + row;
     RowTurner<D>::store(p.rows, at, lane, x);
+    if (p.part_ml != nullptr)
+      for (int s = lane; s < p.n_slots; s += 32) p.part_ml[at * p.n_slots + s] = make_float2(-INFINITY, 0.0f);
     if (p.halves == nullptr) return;
     uint32_t m = 0;
 #pragma unroll

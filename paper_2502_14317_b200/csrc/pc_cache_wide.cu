@@ -1,14 +1,20 @@
-// Attention of more than 32 query rows over one cache, in bf16 or 8 bits (the shared prefix of pc_cache_attn).
+// Attention of many query rows over the caches of pc_cache_attn, in bf16 or 8 bits: the shared prefix with the rows of all sequences, or each
+// sequence's own cache with its own.
 //
 // Two 128-row blocks per CTA with a softmax warpgroup each, roles, rings and work queue as in pc_flash.cuh; rows are the new tokens
-// of all sequences times the q-heads of a kv-head, so a tile of the cache is read once for 256 of them (512 on CTA pairs: bf16, head size
-// 128).  alt = 1: both blocks hold the same rows and take alternate key tiles.  Every item (kv-head, row group, key split) leaves
-// partial results, which the merge kernel joins with the sequences' own.
+// (of all sequences over a prefix) times the q-heads of a kv-head, so a tile of the cache is read once for 256 of them (512 on CTA pairs: head
+// size 128).  alt = 1: both blocks hold the same rows and take alternate key tiles.  Every item (sequence, kv-head, row group, key split) leaves
+// partial results, which the merge kernel joins with the others' and the new tokens' own keys; an item without keys is left out.
 //
 // 8-bit caches: the epilogue's warps, which have nothing to do while an item's tiles go through, make operands of the codes.  These
-// arrive in three slots of half a tile (keys or values), and go into the ring's stages as halves (keys, exactly; the scale of a key multiplies its column of S in the softmax
-// warps, the power of two of a query row is part of the row's softmax scale) or as bf16 (values, code * scale rounded once, as they are read back:
-// the probabilities beside them are rounded to bf16 too).
+// arrive in three slots of a tile's keys or values (pairs: six of half of them), and go into the ring's stages as halves (keys, exactly; the scale of a
+// key multiplies its column of S in the softmax warps, the power of two of a query row is part of the row's softmax scale) or as bf16 (values,
+// code * scale rounded once, as they are read back: the probabilities beside them are rounded to bf16 too).
+//
+// Bound by the products and exponentials of a row (4 d operations and an exponential per key) from some 256 rows on, below by the step of a tile itself:
+// 65536 entries, 8 kv-heads, d = 128, us: 64 rows bf16 54 (268 MB, 5.0 TB/s), int8 69; 256 rows 72, 98; 1024 rows bf16 230 (1195 TFLOP/s), int8 267
+// (1030).  Of the difference at 64 rows, 15, the conversion's arithmetic is 9 at least (without it 60).  A whole call with a tile or two for
+// every CTA takes 13 (24 rows over 2000 bf16 entries): three launches.
 #include "pc_cache.h"
 #include "pc_flash.cuh"
 #include "pc_kernels.h"
@@ -43,15 +49,20 @@ struct __align__(16) Extra8 {
 static_assert(Off8<Cfg8<128, false>>::EXTRA + sizeof(Extra8) <= 232448 && Off8<Cfg8<128, true>>::EXTRA + sizeof(Extra8) <= 232448,
               "shared memory of a CTA");
 
-struct Item { int hkv, rg, split, j0, n; };
+struct Item { int seq, hkv, rg, split, keys, j0, n; };          // keys: entries of the sequence; n tiles from j0, 0: none
 __device__ __forceinline__ Item decode_item(const WidePhase& p, int item) {
   Item it;
   it.split = item % p.c.n_split;
-  const int x = item / p.c.n_split;
+  int x = item / p.c.n_split;
   it.rg = x % p.c.n_rg;
-  it.hkv = x / p.c.n_rg;
-  it.j0 = (int)((long long)p.n_tiles * it.split / p.c.n_split);
-  it.n = (int)((long long)p.n_tiles * (it.split + 1) / p.c.n_split) - it.j0;
+  x /= p.c.n_rg;
+  it.hkv = x % p.c.Hkv;
+  it.seq = x / p.c.Hkv;
+  it.keys = p.c.n_keys;
+  if (p.c.len != nullptr) it.keys = max(0, min(it.keys, __ldg(p.c.len + it.seq)));
+  const int tiles = (it.keys + TILE - 1) / TILE;
+  it.j0 = (int)((long long)tiles * it.split / p.c.n_split);
+  it.n = (int)((long long)tiles * (it.split + 1) / p.c.n_split) - it.j0;
   return it;
 }
 
@@ -99,10 +110,10 @@ struct Converter {
   const Ctx2& cx;
   const WidePhase& prm;
   Extra8& ex;
-  const uint8_t* raw;
+  uint8_t* raw;
   int warp, lane;
   uint32_t k = 0, v = 0, raws = 0, tile = 0;               // uses of the stages and of the slots; tiles of earlier items
-  __device__ __forceinline__ Converter(const Ctx2& c, const WidePhase& p, Extra8& e, const uint8_t* raw_smem, int w, int l)
+  __device__ __forceinline__ Converter(const Ctx2& c, const WidePhase& p, Extra8& e, uint8_t* raw_smem, int w, int l)
       : cx(c), prm(p), ex(e), raw(raw_smem), warp(w), lane(l) {}
 
   // scale of key warp * 32 + lane of the tile, 0 behind the last entry
@@ -111,10 +122,10 @@ struct Converter {
     int t;
     half_of(h, it.n, lag, values, t);
     const int key = (it.j0 + t) * TILE + warp * 32 + lane;
-    return key < prm.c.n_keys ? __ldg((values ? prm.c.v_scale : prm.c.k_scale) + (size_t)it.hkv * prm.c.capacity + key) : 0.0f;
+    return key < it.keys ? __ldg((values ? prm.c.v_scale : prm.c.k_scale) + ((size_t)it.seq * prm.c.Hkv + it.hkv) * prm.c.capacity + key) : 0.0f;
   }
   template <bool VALUES>
-  __device__ __forceinline__ bool convert(int t, float scale) {
+  __device__ __forceinline__ bool convert(int t, float scale, int valid) {             // valid: rows of the tile that are entries
     Misc2& mi = *cx.mi;
     uint32_t& n = VALUES ? v : k;
     constexpr int FIRST = VALUES ? C::NK : 0, STAGES = VALUES ? C::NV : C::NK;
@@ -126,7 +137,15 @@ struct Converter {
     const int st = FIRST + n % STAGES, slot = raws % C::RAW;
     if (!WAIT2S(&mi.kv_free[st], free_par(n / STAGES), W2_KVFREE) || !WAIT2S(&ex.raw_full[slot], full_par(raws / C::RAW), W2_KVFULL)) return false;
     uint8_t* const to = cx.ring + st * C::STAGE_BYTES;
-    const uint8_t* const from = raw + slot * C::RAW_BYTES;
+    uint8_t* const from = raw + slot * C::RAW_BYTES;
+    // What stands behind a sequence's length may be codes that are no number, and those times 0 are none either.  (Behind n_keys a copy has zeros.)
+    if constexpr (VALUES && FMT == FMT_E4M3) {
+      if (prm.c.len != nullptr && valid < TILE) {
+        for (int i = lane; i < ROWS / 4 * LPR; i += 32)
+          if (warp * (ROWS / 4) + i / LPR >= valid) *reinterpret_cast<uint4*>(from + (warp * (ROWS / 4) * LPR + i) * 16) = make_uint4(0, 0, 0, 0);
+        __syncwarp();
+      }
+    }
 #pragma unroll
     for (int i0 = 0; i0 < STEPS; i0 += 4) {                // four pieces at a time, their latencies side by side
       uint4 in[4];
@@ -178,7 +197,8 @@ struct Converter {
       bool values;
       int t;
       half_of(h, it.n, lag, values, t);
-      if (!(values ? convert<true>(t, scale) : convert<false>(t, scale))) break;
+      const int valid = it.keys - (it.j0 + t) * TILE;
+      if (!(values ? convert<true>(t, scale, valid) : convert<false>(t, scale, valid))) break;
     }
     tile += it.n;
   }
@@ -257,17 +277,18 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     if (warp == WARP_PRODUCER) {
       // ================================================================ work queue, queries, and for bf16 the cache (both CTAs of a pair)
       if (elect_one()) {
-        const int n_items = prm.c.Hkv * prm.c.n_rg * prm.c.n_split;
+        const int n_items = prm.c.seqs * prm.c.Hkv * prm.c.n_rg * prm.c.n_split;
         Prod p;
         [[maybe_unused]] uint32_t raws = 0;                // uses of the raw slots
         while (!*cx.abort_flag) {
           const int item = next_item<C>(cx, p, leader, prm.counter, n_items);
           if (item >= n_items) break;
           const Item it = decode_item(prm, item);
+          if (it.n == 0) continue;                           // (its slots say so already)
           Desc d;
           d.kind = KIND_FLASH;
-          d.c = 0; d.hkv = it.hkv; d.len = it.split;
-          d.h[0] = it.rg; d.h[1] = 0;
+          d.c = it.seq; d.hkv = it.hkv; d.len = it.split;
+          d.h[0] = it.rg; d.h[1] = it.keys;
           d.t[0] = it.j0; d.t[1] = it.n;
           d.n[0] = alt ? (it.n + 1) / 2 : it.n;
           d.n[1] = alt ? it.n / 2 : (first_row(it.rg, 1, 0) < rows ? it.n : 0);
@@ -279,7 +300,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
             if (leader) mbar_arrive_expect_tx(&mi.q_full[qs], NCTA * C::Q_BYTES);
             const uint32_t bar = in_cta<C>(&mi.q_full[qs], 0);
             for (int a = 0; a < C::ATOMS; ++a)             // (rows behind the last are zeros and count as copied)
-              load_box<C>(cx.sQ + qs * C::Q_BYTES + a * 16384, &tm_q, bar, a * 64, first_row(it.rg, b, rank), it.hkv, 0);
+              load_box<C>(cx.sQ + qs * C::Q_BYTES + a * 16384, &tm_q, bar, a * 64, it.seq * rows + first_row(it.rg, b, rank), it.hkv, 0);
             ++p.q;
           }
           if constexpr (Q8) {
@@ -291,7 +312,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               if (!WAIT2I(&ex.raw_free[slot], free_par(raws / C::RAW), W2_KVFREE)) break;
               mbar_arrive_expect_tx(&ex.raw_full[slot], C::RAW_BYTES);
               tma_load_4d(smem + O::RAW + slot * C::RAW_BYTES, values ? &tm_v : &tm_k, &ex.raw_full[slot], PAIR && values ? (int)rank * 64 : 0,
-                          (it.j0 + t) * TILE + (PAIR && !values ? (int)rank * 64 : 0), it.hkv, 0);
+                          (it.j0 + t) * TILE + (PAIR && !values ? (int)rank * 64 : 0), it.hkv, it.seq);
             }
           } else {
             uint8_t* dst;
@@ -299,7 +320,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               const uint32_t bar = ring_stage<C, false>(cx, p, leader, &dst);
               if (!bar) return;
               for (int a = 0; a < C::ATOMS; ++a)
-                load_box<C>(dst + a * (PAIR ? 8192 : 16384), &tm_k, bar, a * 64, (it.j0 + t) * TILE + (PAIR ? (int)rank * 64 : 0), it.hkv, 0);
+                load_box<C>(dst + a * (PAIR ? 8192 : 16384), &tm_k, bar, a * 64, (it.j0 + t) * TILE + (PAIR ? (int)rank * 64 : 0), it.hkv, it.seq);
             };
             const int lag = alt ? 2 : 1;
             for (int t = 0; t < lag && t < it.n; ++t) load_k(t);
@@ -307,7 +328,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
               const uint32_t bar = ring_stage<C, true>(cx, p, leader, &dst);
               if (bar)
                 for (int a = 0; a < (PAIR ? 1 : C::ATOMS); ++a)
-                  load_box<C>(dst + a * 16384, &tm_v, bar, PAIR ? (int)rank * 64 : a * 64, (it.j0 + t) * TILE, it.hkv, 0);
+                  load_box<C>(dst + a * 16384, &tm_v, bar, PAIR ? (int)rank * 64 : a * 64, (it.j0 + t) * TILE, it.hkv, it.seq);
               if (t + lag < it.n) load_k(t + lag);
             }
           }
@@ -422,7 +443,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
     while (true) {
       const Desc d = next_desc<C>(cx, nd, true);
       if (d.kind == KIND_DONE) break;
-      if constexpr (Q8) conv.item(Item{d.hkv, d.h[0], d.len, d.t[0], d.t[1]}, alt ? 2 : 1);
+      if constexpr (Q8) conv.item(Item{d.c, d.hkv, d.h[0], d.len, d.h[1], d.t[0], d.t[1]}, alt ? 2 : 1);
 #pragma unroll 1
       for (int b0 = 0; b0 < (alt ? 1 : 2); ++b0) {
         // one output block: block b0, or with alt the sum of both (the second may have had no tile)
@@ -453,7 +474,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         ++nq;
         const int row = first_row(d.h[0], b0, rank) + r;
         const bool valid = row < rows;
-        const size_t prow = ((size_t)d.hkv * prm.c.total_rows + row) * prm.c.n_slots + prm.c.slot0 + d.len;
+        const size_t prow = ((size_t)d.hkv * prm.c.total_rows + (size_t)d.c * rows + row) * prm.c.n_slots + prm.c.slot0 + d.len;
         uint4* const out = reinterpret_cast<uint4*>(prm.c.part_o + prow * D);
         const uint32_t tO = cx.tmem + C::TM_O + (alt ? 0 : b0 * D) + lane_sel;
 #pragma unroll 1
@@ -504,12 +525,12 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         float scale_log2 = prm.c.q.scale_log2;
         if constexpr (Q8) {
           const int row = first_row(d.h[0], b, rank) + r;
-          if (row < rows) scale_log2 = __ldg(prm.half_scale + (size_t)d.hkv * prm.c.total_rows + row);
+          if (row < rows) scale_log2 = __ldg(prm.half_scale + (size_t)d.hkv * prm.c.total_rows + (size_t)d.c * rows + row);
         }
         RowState st = {-INFINITY, 0.0f};
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {
-          const int t = alt ? 2 * i + b : i, j = d.t[0] + t, vis = prm.c.n_keys - j * TILE;            // ragged last tile
+          const int t = alt ? 2 * i + b : i, j = d.t[0] + t, vis = d.h[1] - j * TILE;                  // ragged last tile
           WAIT2S(&mi.s_full[b], full_par(n_s), W2_SFULL);
           ++n_s;
           if constexpr (Q8) {
@@ -542,7 +563,7 @@ cudaError_t wide_t(const CUtensorMap* maps, const WidePhase& p, int sm_count, cu
   using C = Cfg<D, PAIR>;
   constexpr int SMEM = FMT == FMT_BF16 ? Off<C>::TOTAL : Off8<Cfg8<D, PAIR>>::EXTRA + (int)sizeof(Extra8);
   if (cudaError_t e = cudaFuncSetAttribute(cache_wide_kernel<D, FMT, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM); e != cudaSuccess) return e;
-  const long long n_items = (long long)p.c.Hkv * p.c.n_rg * p.c.n_split;
+  const long long n_items = (long long)p.c.seqs * p.c.Hkv * p.c.n_rg * p.c.n_split;
   const int units = sm_count / C::NCTA;
   if (units < 1) return cudaErrorInvalidConfiguration;
   return launch_chained(cache_wide_kernel<D, FMT, PAIR>, dim3((unsigned)((n_items < units ? (int)n_items : units) * C::NCTA)), dim3(NT2), SMEM, st, C::NCTA,

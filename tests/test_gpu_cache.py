@@ -207,6 +207,22 @@ def test_sequences_of_different_lengths(fmt, window, B, w, Hq, Hkv, d, n):
     _check(ref.f64(got["out"][1:]), want[1:], "out", got["lse"][1:].cpu().numpy(), want_lse[1:])
 
 
+@pytest.mark.parametrize("fmt", ["int8", "e4m3", "bf16"])
+@pytest.mark.parametrize("ragged", [True, False])
+@pytest.mark.parametrize("B,w,Hq,Hkv,d,n", [(3, 40, 4, 2, 64, 300), (11, 24, 4, 1, 128, 400), (2, 70, 8, 2, 128, 1000), (5, 33, 2, 1, 128, 129), (12, 20, 8, 2, 64, 2500),
+                                            (1, 128, 4, 1, 128, 5000), (1, 128, 8, 2, 64, 1), (13, 9, 16, 2, 128, 128)])
+def test_many_rows_over_own_caches(fmt, ragged, B, w, Hq, Hkv, d, n):
+    """More than 32 rows of a kv-head in every sequence; lengths from zero on, NaN codes behind them."""
+    _run(B, w, Hq, Hkv, d, 0, "", n, fmt, ragged=ragged)
+
+
+@pytest.mark.parametrize("pf,of", [("int8", "e4m3"), ("bf16", "int8"), ("e4m3", "bf16")])
+@pytest.mark.parametrize("window", [True, False])
+@pytest.mark.parametrize("B,w,Hq,Hkv,d,n_prefix,n_own", [(3, 34, 4, 2, 128, 300, 200), (1, 12, 4, 1, 64, 20000, 700), (2, 64, 8, 2, 128, 129, 3000)])
+def test_many_rows_over_prefix_and_own_caches(pf, of, window, B, w, Hq, Hkv, d, n_prefix, n_own):
+    _run(B, w, Hq, Hkv, d, n_prefix, pf, n_own, of, ragged=True, window=window)
+
+
 @pytest.mark.parametrize("pf,of", [("bf16", "bf16"), ("int8", "int8"), ("e4m3", "bf16"), ("bf16", "int8"), ("int8", "e4m3"), ("e4m3", "")])
 @pytest.mark.parametrize("B,w,Hq,Hkv,d,n_prefix,n_own", [
     (2, 1, 4, 2, 64, 100, 7), (5, 1, 8, 2, 128, 700, 33), (3, 4, 8, 1, 128, 500, 64), (40, 1, 8, 2, 128, 300, 20), (9, 5, 14, 2, 64, 1030, 5),
