@@ -19,6 +19,7 @@ struct KvWrite {
   const int* at;                                 // append: [B] or null
   const int *kept, *idx;                         // gather: chunk ids [m], positions [m,Hkv,per_chunk]
   int per_chunk;
+  unsigned chunk_mul, chunk_shift;               // e / per_chunk = e * chunk_mul >> chunk_shift for e < 2^28
   int* pos_out;                                  // gather: [Hkv,n] or null
   int* status;
 };

@@ -75,6 +75,10 @@ int32_t pc_gather_kv_quantize(const void* k_src, const void* v_src, const int64_
   w.capacity = cache->capacity;
   w.B = 1; w.Hkv = cache->Hkv; w.n = m * k;
   w.kept = kept; w.idx = idx; w.per_chunk = k; w.pos_out = pos_out;
+  unsigned bits = 0;                             // 2^bits >= k: with 2^(28 + bits) / k rounded up the product is off by less than 1 / k for e < 2^28
+  while ((1ll << bits) < k) ++bits;
+  w.chunk_shift = 28 + bits;
+  w.chunk_mul = (unsigned)(((1ull << w.chunk_shift) + k - 1) / k);
   return launched(pc::launch_kv_quantize(w, cache->format, cache->d, true, static_cast<cudaStream_t>(stream)));
 }
 
@@ -202,9 +206,10 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     if (int32_t rc = check_cache(c, false); rc != PC_OK) return rc;
     if (c->B != (own ? a->B : 1) || c->Hkv != a->Hkv || c->d != a->d || n > c->capacity) return PC_ERR_INVALID_ARG;
     PhasePlan& ph = own ? p.own : p.prefix;
-    // More than 16 rows over the prefix: the kernel for many; over codes, whose conversion that makes for each of its few CTAs, and long prefixes more
-    // than 32.  Measured, us, few / many, head size 128, 16 rows 12.7 / 12.9 (bf16, 2000 entries), 22.7 / 27.8 (int8, 16000); 24 rows 14.3 / 13.3,
-    // 103.8 / 90.2 (131072), int8 16.0 / 14.4, 28.5 / 27.6, 117.3 / 119.8, e4m3 15.7 / 14.5, 26.8 / 26.8, 101.0 / 118.7; 40 rows int8 16.5 / 14.7, 166.0 / 121.0.
+    // More than 32 rows over the prefix: the kernel for many; at head size 128 more than 16, over codes, whose conversion it makes in each of its few CTAs, up
+    // to 16384 entries.  Measured, us, few / many, 16 rows 12.7 / 12.9 (bf16, 2000 entries), 22.7 / 27.8 (int8, 16000); 24 rows 14.3 / 13.3, 103.8 / 90.2
+    // (131072), int8 16.0 / 14.4, 28.5 / 27.6, 117.3 / 119.8, e4m3 15.7 / 14.5, 26.8 / 26.8, 101.0 / 118.7; 40 rows int8 16.5 / 14.7, 166.0 / 121.0; head size
+    // 64, 24 rows over 8000 bf16 14.7 / 16.3.
     const int64_t seqs = own ? a->B : 1, rows = p.total_rows / seqs;
     // Own caches: more than 48 rows of a sequence; bf16 more than 16, at head size 64 and little work 32 (what stands behind a length may be no number, and bf16
     // values go to the matrix unit as they are: with lengths never).  Measured, us, few / many, 16 sequences of 2000 entries, 8 kv-heads: int8 d = 128 32 rows
@@ -212,7 +217,7 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     // 24 38.7 / 37.0, 64 85.2 / 56.8, d = 64 24 26.3 / 30.0, 48 43.4 / 39.1; 64 sequences, d = 64, 24 rows 94.7 / 78.7.
     const bool bf16 = c->format == PC_KV_BF16;
     const bool many = own ? rows > (!bf16 ? 48 : a->d == 128 || (double)seqs * a->Hkv > 2.0 * sm_count ? 16 : 32) && (!bf16 || a->own_len == nullptr)
-                          : rows > (bf16 || n <= 16384 ? 16 : 32);
+                          : rows > (a->d == 128 && (bf16 || n <= 16384) ? 16 : 32);
     if (many) {
       ph = wide_plan(seqs, rows, a->Hkv, a->d, c->format, n, sm_count);
       p.rows = true;

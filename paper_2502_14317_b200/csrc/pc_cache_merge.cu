@@ -1,5 +1,6 @@
 // What stands before and behind the attention kernels of pc_cache_attn: the queries as rows of a kv-head, and the join of a
 // row's partial results with the new tokens' own keys.
+// Both are latency, alone and cold: 256 rows of 8 kv-heads turned 4.5 to 5.1 us, 1024 8.4 to 9.0; 4 rows of 8 kv-heads joined from 17 slots 8.0.
 #include "pc_cache_finish.cuh"
 #include "pc_cache_rows.cuh"
 #include "pc_kernels.h"
