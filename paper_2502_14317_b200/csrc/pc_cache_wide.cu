@@ -13,7 +13,8 @@
 //
 // Bound by the products and exponentials of a row (4 d operations and an exponential per key) from some 256 rows on, below by the step of a tile itself:
 // 65536 entries, 8 kv-heads, d = 128, us: 64 rows bf16 54 (268 MB, 5.0 TB/s), int8 69; 256 rows 72, 98; 1024 rows bf16 230 (1195 TFLOP/s), int8 267
-// (1030).  Of the difference at 64 rows, 15, the conversion's arithmetic is 9 at least (without it 60).  A whole call with a tile or two for
+// (1030).  Over codes the converting warps are busy throughout, 900 to 1100 of a tile's 2500 to 3000 cycles (256 rows, pair) in conversions, and the softmax
+// waits for them; keys and values on two warps each, with slots of their own, took 1.2 to 1.5 times as long.  A whole call with a tile or two for
 // every CTA takes 13 (24 rows over 2000 bf16 entries): three launches.
 #include "pc_cache.h"
 #include "pc_flash.cuh"
