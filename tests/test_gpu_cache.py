@@ -406,6 +406,35 @@ def test_decoding_steps_over_a_growing_cache():
         lens += 1
 
 
+@pytest.mark.parametrize("fmt,capacity", [("int8", 17_000_003), ("bf16", 9_000_001)])
+@pytest.mark.parametrize("B", [1, 40])
+def test_offsets_beyond_32_bits(fmt, capacity, B):
+    """Two kv-heads of a cache whose second begins beyond 2^31 bytes (int8) and elements, read from end to end: zeros but for its last entries.
+    A zero key has weight 1 and adds nothing, so the answer is a sum over the last ones."""
+    Hkv, d, n = 2, 128, 60
+    q = _normal(170, B, 1, Hkv, d)
+    k, v = _normal(171, 1, n, Hkv, d), _normal(172, 1, n, Hkv, d)
+    for j in range(min(B, n)):
+        k[0, j] = (q[j, 0].float() * 1.5).to(torch.bfloat16)             # a logit of some 17: as much as the zeros together
+    cache = pc.kv_cache(1, Hkv, capacity, d, fmt)
+    if fmt == "bf16":
+        cache["k"][:, :, -n:], cache["v"][:, :, -n:] = k.transpose(1, 2).cuda(), v.transpose(1, 2).cuda()
+        ks, vs = ref.f64(k.transpose(1, 2)), ref.f64(v.transpose(1, 2))
+    else:
+        small = pc.kv_cache(1, Hkv, n, d, fmt)
+        pc.kv_quantize(small, k.cuda(), v.cuda())
+        pc.kv_quantize(cache, k.cuda(), v.cuda(), at=capacity - n)
+        got = pc.kv_dequantize(cache, n, at=torch.tensor([capacity - n], dtype=torch.int32, device="cuda"))
+        assert all(torch.equal(x, y) for x, y in zip(got, pc.kv_dequantize(small)))
+        assert not cache["k"][:, :, :-n].any() and not cache["v_scale"][:, :, :-n].any()
+        ks, vs = _values(small)
+    got = pc.cache_attn(q.cuda(), prefix=cache, want_lse=True)
+    assert got["status"].item() == 0
+    e = np.exp(np.einsum("bhd,hnd->bhn", ref.f64(q[:, 0]), ks[0]) * d ** -0.5)
+    total = e.sum(-1) + capacity - n
+    _check(ref.f64(got["out"])[:, 0], np.einsum("bhn,hnd->bhd", e, vs[0]) / total[..., None], "out", got["lse"][..., 0].cpu().numpy(), np.log(total))
+
+
 def test_a_wait_that_runs_out_is_reported():
     """Nothing is broken for it: the limit is set so low that an ordinary wait for a copy may exceed it; the call returns and the next is right."""
     lib = pc.load_library()
