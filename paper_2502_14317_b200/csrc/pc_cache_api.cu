@@ -147,7 +147,7 @@ PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n
     if (fit < 1.0) return;
     const double rounds = std::ceil(items / fit), active = (items < fit ? items : fit) * s;
     const bool single = active <= sm_count;                          // a CTA has its SM for itself
-    const double alone = units * (p.group == 8 ? (single ? 0.63 : 1.1) / 7 : (single ? 0.95 : 1.4) / 5), bytes = tile_us * active;
+    const double alone = units * (p.group == 8 ? (single ? 0.63 : 1.1) / 7 : (single ? 0.95 : 1.4) / (d == 64 ? 7 : 5)), bytes = tile_us * active;
     const double cost = rounds * (7.5 + (bytes > alone ? bytes : alone) * std::ceil((double)tiles / s)) + (finish ? 0.0 : 1.0 + 0.1 * s);
     if (least < 0.0 || cost < least) { least = cost; p.n_split = s; p.finish = finish; }
   };
