@@ -17,8 +17,8 @@
 // results are added in shared memory, the splits' through distributed shared memory or by the merge kernel.
 // Measured, 32/8 heads of 128: 64 sequences over 16384 int8 entries each, 2.2 GB, 340 us = 6.5 TB/s, in a loop at the power cap (1.56 GHz) 386 = 5.7 TB/s;
 // one sequence 15.3 (splits as slots; rows, first copies, a tile, join and merge: latency); 16 rows a kv-head over 8000 entries 251 us, bf16 312 =
-// 6.7 TB/s.  16 rows of codes at head size 64 (23 sequences of 4 tokens, up to 5000 e4m3 entries) 23 to 26: chains of dependent
-// instructions of a few warps, 35 % of the issue slots.
+// 6.7 TB/s.  28 rows, two groups, of codes at head size 64 (23 sequences of 4 tokens, up to 5000 e4m3 entries) 22: chains of dependent
+// instructions of few warps.
 #include "pc_cache_finish.cuh"
 #include "pc_cache_rows.cuh"
 #include "pc_kernels.h"
