@@ -74,7 +74,7 @@ struct CachePhase {
   const float *k_scale, *v_scale;                // [seqs,Hkv,capacity] (8-bit formats)
   long long capacity;
   int n_rg, n_split, slot0, n_slots, total_rows; // row groups of a sequence, key splits; total_rows = rows of a kv-head over all sequences
-  int causal;                                    // 1 (few rows, bf16, one split, brief for groups of 16): the entries are the new tokens themselves, token i sees 0 .. i
+  int causal;                                    // 1 (few rows in groups of 8, bf16, one split): the entries are the new tokens themselves, token i sees 0 .. i
   CacheRows q;
   int rows_made;                                 // 1: the rows are in memory; 0: this launch makes them
   float* part_o;                                 // [Hkv,total_rows,n_slots,d]
