@@ -15,6 +15,7 @@ void note_launch() { g_launches.fetch_add(1, std::memory_order_relaxed); }
 static std::atomic<int> g_wait_kcycles{1 << 21};            // limit of the device-side waits, units of 1024 cycles (~1 s)
 static std::atomic<int> g_skip_final_publication{0};        // test hook, see pc_debug_bounded_wait_test
 int wait_limit_kcycles() { return g_wait_kcycles.load(); }
+int skip_final_publication() { return g_skip_final_publication.load(); }
 }  // namespace pc
 
 namespace {

@@ -81,6 +81,7 @@ struct CachePhase {
   float2* part_ml;                               // [Hkv,total_rows,n_slots]
   int* status;
   int wait_kcycles;
+  int skip_final_publication;                    // test hook of the bounded waits (see pc_debug_bounded_wait_test in pc.h)
 };
 // Few rows (pc_cache_few.cu), groups of 8 or 16.  finish null: every split leaves its slot.  Else the splits of a (sequence, kv-head, row
 // group) are the CTAs of a cluster, and the kernel finishes its rows: its splits' results, finish's slots and the new tokens' keys.

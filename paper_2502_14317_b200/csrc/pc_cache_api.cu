@@ -351,6 +351,7 @@ int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
     p.part_ml = reinterpret_cast<float2*>(ws + plan.off_ml);
     p.status = a->status_word;
     p.wait_kcycles = pc::wait_limit_kcycles();
+    p.skip_final_publication = pc::skip_final_publication();
     CUtensorMap maps[3] = {}, unused;
     bool ok;
     if (ph.wide) {

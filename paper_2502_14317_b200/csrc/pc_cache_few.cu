@@ -219,6 +219,10 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       load(i);
     }
     for (int k = i > NS ? i - NS : 0; k < i; ++k) mbar_wait_drain(&mi.full[k % NS], full_par(k / NS), abort_flag);   // every copy has landed before exit
+    // test hook: the last stage is given back once and no more, and a second wait for it runs out
+    if (prm.skip_final_publication != 0)
+      for (int k = 0; k < 2; ++k) mbar_wait(&mi.empty[(nt - 1) % NS], free_par((nt - 1) / NS + 1 + k), abort_flag, prm.status, WF_EMPTY);
+    abort_grace_pause(abort_flag);
   } else {
     // ================================================================ a warp: 16 keys at a time
     const int g = lane >> 2, a = lane & 3;
@@ -448,18 +452,21 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
     named_barrier_sync(1, 32 * C::WARPS);                        // every warp has read its last stage
     float* const part = reinterpret_cast<float*>(smem) + (size_t)warp * N * D;
+    // (after a wait that has run out copies may still be on their way into the ring: the producer lets them land)
+    if (!*abort_flag) {
 #pragma unroll
-    for (int t = 0; t < NT8; ++t)
+      for (int t = 0; t < NT8; ++t)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float f = Q8 ? 1.0f / cw[t][e] : 1.0f;
+        for (int e = 0; e < 2; ++e) {
+          const float f = Q8 ? 1.0f / cw[t][e] : 1.0f;
 #pragma unroll
-        for (int j = 0; j < C::MT; ++j) {
-          constexpr int PER = C::MT / C::BOXES;
-          const int d = (j / PER) * C::EPB + g * (C::EPB / 8) + 2 * (j % PER);
-          *reinterpret_cast<float2*>(part + (8 * t + 2 * a + e) * D + d) = make_float2(acc[j][t][e] * f, acc[j][t][2 + e] * f);
+          for (int j = 0; j < C::MT; ++j) {
+            constexpr int PER = C::MT / C::BOXES;
+            const int d = (j / PER) * C::EPB + g * (C::EPB / 8) + 2 * (j % PER);
+            *reinterpret_cast<float2*>(part + (8 * t + 2 * a + e) * D + d) = make_float2(acc[j][t][e] * f, acc[j][t][2 + e] * f);
+          }
         }
-      }
+    }
   }
   __syncthreads();
   // ---- the warps' results added up, into the first warp's place or the slot

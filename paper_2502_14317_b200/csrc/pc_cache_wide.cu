@@ -336,7 +336,9 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
         Desc d;
         d.kind = KIND_DONE; d.c = d.hkv = d.len = 0;
-        publish<C>(cx, p, d);
+        publish<C>(cx, p, d, prm.c.skip_final_publication == 0);
+        // test hook: nobody takes the message, so this wait runs out as the consumers' do, and the copies are drained as after any abort
+        if (prm.c.skip_final_publication != 0) WAIT2(&mi.d_free[(p.d - 1) % NDESC], free_par((p.d - 1) / NDESC + 1), W2_DESC);
         if constexpr (!Q8) drain_copies<C>(cx, p, leader);
         else if (*cx.abort_flag) {                          // every copy issued has landed before the exit
           for (uint32_t i = (p.q > NQ ? p.q - NQ : 0); i < p.q && leader; ++i) mbar_wait_drain(&mi.q_full[i % NQ], full_par(i / NQ), cx.abort_flag);

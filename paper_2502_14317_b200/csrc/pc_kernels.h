@@ -10,6 +10,7 @@ namespace pc {
 // Every kernel launch of the library is counted here (see pc_launch_count in pc.h).
 void note_launch();
 int wait_limit_kcycles();                        // limit of the device-side waits, units of 1024 cycles
+int skip_final_publication();                    // test hook, see pc_debug_bounded_wait_test in pc.h
 int sm100_count();                               // SMs of the current device, 0 if it is not an sm_100
 
 // Launches of one call, and of calls on one stream, follow each other closely: every kernel is launched with programmatic

@@ -90,11 +90,13 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
 }
 
 // Wait that ignores the abort flag (used only to drain copies and tensor-core work in flight before
-// exit); gives up after an eighth of the wait limit.
+// exit); gives up after an eighth of the wait limit, or after DRAIN_CYCLES where that is more: what is in flight needs its time
+// however short a limit was set, and must not land in shared memory that is used again or has been left.
+constexpr long long DRAIN_CYCLES = 1 << 18;                  // some 0.14 ms
 __device__ __forceinline__ void mbar_wait_drain(uint64_t* bar, uint32_t parity, const volatile int* abort_flag) {
-  const long long t0 = clock64();
+  const long long t0 = clock64(), limit = static_cast<long long>(abort_flag[1]) << 7;
   while (!mbar_try_wait(bar, parity)) {
-    if (clock64() - t0 > (static_cast<long long>(abort_flag[1]) << 7)) return;
+    if (clock64() - t0 > (limit > DRAIN_CYCLES ? limit : DRAIN_CYCLES)) return;
   }
 }
 // After an abort: a fixed pause (a tenth of a millisecond) that outlasts any copy this CTA may still have in
