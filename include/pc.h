@@ -120,14 +120,16 @@ PC_API int32_t pc_chunk_prefill_attn(const pc_prefill_desc* desc, const void* q,
  * flight and return; the host then treats the call's results as undefined (PC_ERR_TIMEOUT).
  *   wait_limit_cycles      limit for all later launches of this process (0: the default of
  *                          about 2e9 cycles, a second);
- *   skip_final_publication non-zero: the chunk-prefill kernel of head size 64, the parallel-attention kernel for more
- *                          than 32 query rows and pc_cache_attn's kernel for many rows leave out ONE signal that carries no data - the "no more work"
+ *   skip_final_publication non-zero: the chunk-prefill kernel of head size 64 and the parallel-attention kernel for more
+ *                          than 32 query rows leave out ONE signal that carries no data - the "no more work"
  *                          message to the consumer warps after the last work item, when nothing is in flight any
- *                          more - so that their wait (in the latter two also the producer's for the message to be
- *                          taken, behind which it drains its copies) runs out.  pc_cache_attn's kernel for few rows waits
- *                          once more for a stage that has been given back for good.  Outputs of such a call are complete (not the scores of a call whose
+ *                          more - so that their wait (in the latter also the producer's for the message to be
+ *                          taken, behind which it drains its copies) runs out.  Outputs of such a call are complete (not the scores of a call whose
  *                          sweeps are items of their own: they wait for blocks that end with that signal); its status_word
- *                          is non-zero.  Zero switches the hook off again.
+ *                          is non-zero.  pc_cache_attn's kernel for many rows asks for an arrival more than it gets on every block's
+ *                          second message (where no block has two work items that is "no more work", and outputs are complete), the
+ *                          one for few rows on every copy: its warps give up with the copies landed, and nothing is computed.
+ *                          Zero switches the hook off again.
  * Host-side settings, read at every launch.
  */
 PC_API int32_t pc_debug_bounded_wait_test(int64_t wait_limit_cycles, int32_t skip_final_publication);

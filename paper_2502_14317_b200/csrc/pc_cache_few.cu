@@ -103,6 +103,16 @@ __device__ __forceinline__ void ld_cluster(uint32_t addr, float (&x)[E]) {
   else
     asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x[0]), "=f"(x[1]) : "r"(addr) : "memory");
 }
+// A wait that gives up pauses first: the warps are about to leave their results in the ring, into which copies may still be on their way.  (A warp
+// that has seen all its tiles has seen every copy land.)
+static __device__ __noinline__ bool wait_over(long long t0, volatile int* abort_flag, int* status, int where) {
+  if (!mbar_wait_over(t0, abort_flag, status, where)) return false;
+  abort_grace_pause(abort_flag);
+  return true;
+}
+__device__ __forceinline__ bool ring_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int where) {
+  return mbar_wait_ns<SPIN_BACKOFF_NS, wait_over>(bar, parity, abort_flag, status, where);
+}
 
 }  // namespace
 
@@ -122,7 +132,8 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   const int hkv = x % prm.Hkv, seq = x / prm.Hkv;
 
   if (tid == C::WARPS * 32) {
-    for (int i = 0; i < NS; ++i) { mbar_init(&mi.full[i], Q8 ? 33 : 1); mbar_init(&mi.empty[i], C::WARPS); }
+    const int hook = prm.skip_final_publication != 0 ? 1 : 0;    // test hook: an arrival that nobody makes, so that the waits for copies run out
+    for (int i = 0; i < NS; ++i) { mbar_init(&mi.full[i], (Q8 ? 33 : 1) + hook); mbar_init(&mi.empty[i], C::WARPS); }
     mi.abort_flag = 0;
     mi.wait_kcycles = prm.wait_kcycles;
     mi.odd = 0;
@@ -215,14 +226,10 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
   if (warp == C::WARPS) {
     int i = NS < nt ? NS : nt;
     for (; i < nt && !*abort_flag; ++i) {
-      if (!mbar_wait(&mi.empty[i % NS], free_par(i / NS), abort_flag, prm.status, WF_EMPTY)) break;
+      if (!ring_wait(&mi.empty[i % NS], free_par(i / NS), abort_flag, prm.status, WF_EMPTY)) break;
       load(i);
     }
     for (int k = i > NS ? i - NS : 0; k < i; ++k) mbar_wait_drain(&mi.full[k % NS], full_par(k / NS), abort_flag);   // every copy has landed before exit
-    // test hook: the last stage is given back once and no more, and a second wait for it runs out
-    if (prm.skip_final_publication != 0)
-      for (int k = 0; k < 2; ++k) mbar_wait(&mi.empty[(nt - 1) % NS], free_par((nt - 1) / NS + 1 + k), abort_flag, prm.status, WF_EMPTY);
-    abort_grace_pause(abort_flag);
   } else {
     // ================================================================ a warp: 16 keys at a time
     const int g = lane >> 2, a = lane & 3;
@@ -267,7 +274,7 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
     int st = 0, u = warp;
     uint32_t lap = 0;
     for (int i = 0; i < nt; ++i) {
-      if (!mbar_wait(&mi.full[st], lap & 1u, abort_flag, prm.status, WF_FULL)) break;
+      if (!ring_wait(&mi.full[st], lap & 1u, abort_flag, prm.status, WF_FULL)) break;
       for (; u < (i + 1) * C::UNITS; u += C::WARPS) {
         const int r0 = (u - i * C::UNITS) * 16, key0 = (j0 + i) * KEYS + r0;
         if (key0 >= n) continue;
@@ -452,21 +459,18 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
       }
     named_barrier_sync(1, 32 * C::WARPS);                        // every warp has read its last stage
     float* const part = reinterpret_cast<float*>(smem) + (size_t)warp * N * D;
-    // (after a wait that has run out copies may still be on their way into the ring: the producer lets them land)
-    if (!*abort_flag) {
 #pragma unroll
-      for (int t = 0; t < NT8; ++t)
+    for (int t = 0; t < NT8; ++t)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float f = Q8 ? 1.0f / cw[t][e] : 1.0f;
+      for (int e = 0; e < 2; ++e) {
+        const float f = Q8 ? 1.0f / cw[t][e] : 1.0f;
 #pragma unroll
-          for (int j = 0; j < C::MT; ++j) {
-            constexpr int PER = C::MT / C::BOXES;
-            const int d = (j / PER) * C::EPB + g * (C::EPB / 8) + 2 * (j % PER);
-            *reinterpret_cast<float2*>(part + (8 * t + 2 * a + e) * D + d) = make_float2(acc[j][t][e] * f, acc[j][t][2 + e] * f);
-          }
+        for (int j = 0; j < C::MT; ++j) {
+          constexpr int PER = C::MT / C::BOXES;
+          const int d = (j / PER) * C::EPB + g * (C::EPB / 8) + 2 * (j % PER);
+          *reinterpret_cast<float2*>(part + (8 * t + 2 * a + e) * D + d) = make_float2(acc[j][t][e] * f, acc[j][t][2 + e] * f);
         }
-    }
+      }
   }
   __syncthreads();
   // ---- the warps' results added up, into the first warp's place or the slot

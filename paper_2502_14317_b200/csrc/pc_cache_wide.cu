@@ -258,7 +258,9 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
   Misc2& mi = *cx.mi;
   Extra8& ex = *reinterpret_cast<Extra8*>(smem + Off8<Cfg8<D, PAIR>>::EXTRA);       // (8-bit formats)
   if (tid == 0) {
-    init_barriers2<C>(mi, prm.c.wait_kcycles, leader, !Q8 ? 1 : PAIR && leader ? 5 : 4, Q8);   // four converting warps, and the peer's word, in the place of a copy
+    // Four converting warps, and the peer's word, in the place of a copy.  Test hook: the second message, of a CTA with one item the last, asks
+    // for an arrival more than it gets, and the waits for it run out.
+    init_barriers2<C>(mi, prm.c.wait_kcycles, leader, !Q8 ? 1 : PAIR && leader ? 5 : 4, Q8, prm.c.skip_final_publication != 0 ? 2 : 1);
     if constexpr (Q8) {
       for (int i = 0; i < 8; ++i) mbar_init(&ex.sc_full[i], 4);
       for (int i = 0; i < 6; ++i) { mbar_init(&ex.raw_full[i], 1); mbar_init(&ex.raw_free[i], 4); }
@@ -336,9 +338,7 @@ cache_wide_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constan
         }
         Desc d;
         d.kind = KIND_DONE; d.c = d.hkv = d.len = 0;
-        publish<C>(cx, p, d, prm.c.skip_final_publication == 0);
-        // test hook: nobody takes the message, so this wait runs out as the consumers' do, and the copies are drained as after any abort
-        if (prm.c.skip_final_publication != 0) WAIT2(&mi.d_free[(p.d - 1) % NDESC], free_par((p.d - 1) / NDESC + 1), W2_DESC);
+        publish<C>(cx, p, d);
         if constexpr (!Q8) drain_copies<C>(cx, p, leader);
         else if (*cx.abort_flag) {                          // every copy issued has landed before the exit
           for (uint32_t i = (p.q > NQ ? p.q - NQ : 0); i < p.q && leader; ++i) mbar_wait_drain(&mi.q_full[i % NQ], full_par(i / NQ), cx.abort_flag);

@@ -184,7 +184,8 @@ __device__ __forceinline__ void mbar_wait_cluster(uint64_t* bar, uint32_t parity
 }
 
 template <class C>
-__device__ __forceinline__ void init_barriers2(Misc2& mi, int wait_kcycles, bool leader, uint32_t kv_arrivals = 1, bool all_issuers = false) {
+__device__ __forceinline__ void init_barriers2(Misc2& mi, int wait_kcycles, bool leader, uint32_t kv_arrivals = 1, bool all_issuers = false,
+                                               uint32_t second_message = 1) {
   constexpr int N = C::NCTA;
   for (int i = 0; i < C::NQ; ++i) { mbar_init(&mi.q_full[i], 1); mbar_init(&mi.q_free[i], 1); }
   for (int i = 0; i < C::NS; ++i) { mbar_init(&mi.kv_full[i], kv_arrivals); mbar_init(&mi.kv_free[i], 1); }
@@ -195,7 +196,7 @@ __device__ __forceinline__ void init_barriers2(Misc2& mi, int wait_kcycles, bool
     mbar_init(&mi.s_read[b], 4 * N); mbar_init(&mi.pv_done[b], 1);
     mbar_init(&mi.lm_full[b], 4); mbar_init(&mi.lm_free[b], 4);
   }
-  for (int i = 0; i < NDESC; ++i) { mbar_init(&mi.d_full[i], 1); mbar_init(&mi.d_free[i], leader || all_issuers ? 14 : 12); }   // warps, issuers
+  for (int i = 0; i < NDESC; ++i) { mbar_init(&mi.d_full[i], i == 1 ? second_message : 1); mbar_init(&mi.d_free[i], leader || all_issuers ? 14 : 12); }   // warps, issuers
   mbar_init(&mi.item_full, 1); mbar_init(&mi.item_free, 1);
   mbar_init(&mi.lse_rdy, 4 * N);
   mbar_init(&mi.sweep_go, 1);

@@ -70,8 +70,8 @@ static __device__ __noinline__ bool mbar_wait_over(long long t0, volatile int* a
 // flag and the wait limit in units of 1024 cycles.  Once the flag is non-zero every wait
 // returns immediately (the result data is then garbage and the status word says so).
 // Returns false if the wait gave up.
-// NS: pause between two polls.
-template <unsigned NS>
+// NS: pause between two polls.  OVER: what is looked at after every 64 polls.
+template <unsigned NS, bool (*OVER)(long long, volatile int*, int*, int) = mbar_wait_over>
 __device__ __forceinline__ bool mbar_wait_ns(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
                                              int* status_word, int where) {
   if (mbar_try_wait(bar, parity)) return true;
@@ -79,7 +79,7 @@ __device__ __forceinline__ bool mbar_wait_ns(uint64_t* bar, uint32_t parity, vol
   uint32_t spins = 0;
   while (!mbar_try_wait(bar, parity)) {
     if (NS > 0) __nanosleep(NS);                             // a hot spin takes issue slots from the warps that share the scheduler
-    if ((++spins & 63u) == 0u && mbar_wait_over(t0, abort_flag, status_word, where)) return false;
+    if ((++spins & 63u) == 0u && OVER(t0, abort_flag, status_word, where)) return false;
   }
   return true;
 }

@@ -20,30 +20,32 @@ def _cache(seed, B, Hkv, n, d, fmt):
     return cache
 
 
-FEW = 412                                                           # few rows: the producer's wait for a stage
+FEW = 411                                                           # few rows: a warp's wait for a copy
 WIDE, PAIR = 101, 201                                               # many rows: the wait for a work item, single CTAs and pairs
 
 
 @pytest.mark.parametrize("fmt", ["int8", "e4m3", "bf16"])
-@pytest.mark.parametrize("own,B,w,Hq,Hkv,d,n,code", [
-    (True, 1, 1, 8, 2, 128, 9000, FEW),                             # splits left as slots, or a cluster's
-    (False, 1, 4, 8, 2, 64, 100, FEW),                              # a split, 16 rows
-    (True, 4, 1, 4, 2, 64, 3000, FEW),
-    (True, 160, 1, 2, 2, 128, 70, FEW),                             # short builds
-    (False, 1, 30, 2, 1, 128, 40, WIDE),                            # and the new tokens as a phase for few rows: the first code stays
-    (False, 64, 1, 4, 2, 128, 3000, WIDE),
-    (False, 100, 1, 4, 2, 128, 3000, PAIR),
-    (False, 100, 1, 4, 2, 64, 3000, WIDE),
-    (False, 1, 20, 16, 2, 128, 700, PAIR),
+@pytest.mark.parametrize("cache,B,w,Hq,Hkv,d,n,code", [
+    ("own", 1, 1, 8, 2, 128, 1500, FEW),                            # splits left as slots
+    ("own", 4, 1, 8, 2, 64, 2000, FEW),                             # or joined by a cluster
+    ("prefix", 1, 4, 8, 2, 64, 100, FEW),                           # 16 rows
+    ("own", 160, 1, 2, 2, 128, 70, FEW),                            # short builds
+    ("own", 160, 4, 8, 2, 128, 30, FEW),
+    ("", 2, 60, 4, 2, 128, 0, FEW),                                 # new tokens alone, causal
+    ("prefix", 40, 1, 2, 1, 128, 200, WIDE),                        # one work item each: the message that is missed is the last
+    ("prefix", 90, 1, 2, 1, 64, 256, WIDE),
+    ("prefix", 100, 1, 2, 1, 128, 256, PAIR),
+    ("prefix", 1, 20, 8, 1, 128, 7, PAIR),
+    ("own", 1, 60, 1, 1, 64, 130, WIDE),                            # and the new tokens behind it: the first code stays
 ])
-def test_a_wait_that_runs_out_is_reported_with_its_code(fmt, own, B, w, Hq, Hkv, d, n, code):
-    """The kernels wait for one signal that nobody gives, when nothing is in flight any more: 2e6 cycles, about a millisecond."""
+def test_a_wait_that_runs_out_is_reported_with_its_code(fmt, cache, B, w, Hq, Hkv, d, n, code):
+    """The kernels wait for one arrival that nobody makes, with nothing in flight: 2e6 cycles, about a millisecond."""
     lib = pc.load_library()
     q, win = _normal(1, B, w, Hq, d), _normal(2, B, w, Hkv, d)
-    cache = _cache(3, B if own else 1, Hkv, n, d, fmt)
+    kept = {cache: _cache(3, B if cache == "own" else 1, Hkv, n, d, fmt)} if cache else {}
 
     def run():
-        r = pc.cache_attn(q, win, win, rope_theta=1e4, want_lse=True, **{"own" if own else "prefix": cache})
+        r = pc.cache_attn(q, win, win, rope_theta=1e4, want_lse=True, **kept)
         return r["status"].item(), r["out"].clone(), r["lse"].clone()
 
     clean = run()
@@ -56,5 +58,5 @@ def test_a_wait_that_runs_out_is_reported_with_its_code(fmt, own, B, w, Hq, Hkv,
     assert hit[0] == code
     again = run()
     assert again[0] == 0
-    for r in (hit, again):                                          # all work was done before the missing signal
+    for r in (hit, again) if code != FEW and w == 1 else (again,):  # many rows: all work was done before the missing signal
         assert torch.equal(r[1], clean[1]) and torch.equal(r[2], clean[2])
