@@ -382,8 +382,8 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
             over = fmaxf(over, above);
             p[e] = fast_exp2(above);
             w[e] = p[e];
-            if constexpr (Q8) {
-              w[e] = p[e] * ((e < 2 ? sv0 : sv1) * cw[t][e & 1]);
+            if constexpr (Q8) {                                  // (scale times cw may be infinite where p is 0)
+              w[e] = p[e] * (e < 2 ? sv0 : sv1) * cw[t][e & 1];
               heavy = fmaxf(heavy, w[e]);
             }
           }
@@ -402,8 +402,8 @@ cache_few_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant
                 const float most = fmaxf(fmaxf(before, max_over_keys(fmaxf(p[e] * sv0, p[2 + e] * sv1))), 0x1p-100f);
                 cw[t][e] = 1024.0f / most;
                 f = before / most;
-                w[e] = p[e] * (sv0 * cw[t][e]);
-                w[2 + e] = p[2 + e] * (sv1 * cw[t][e]);
+                w[e] = p[e] * sv0 * cw[t][e];
+                w[2 + e] = p[2 + e] * sv1 * cw[t][e];
               }
 #pragma unroll
               for (int j = 0; j < C::MT; ++j) { acc[j][t][e] *= f; acc[j][t][2 + e] *= f; }
