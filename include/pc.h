@@ -466,8 +466,9 @@ PC_API int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0
  * they are computed in fp64), where pc_parallel_attn rounds the fp64 rotation; rope_theta = 0: queries come rotated.  q, k_win and v_win through element
  * strides (sequence, token, head; 0,0,0 -> contiguous), multiples of 8.  A row that sees nothing gets zeros and lse -infinity.
  * out [B,w,Hq,d] bf16 and lse [B,Hq,w] fp32 (natural log; may be NULL) contiguous.
- * 1 <= w <= 128, d in {64, 128}, any Hq / Hkv.  Workspace: pc_cache_attn_workspace_bytes(args) (reads the sizes and the caches'
- * descriptors alone), aligned to 32 bytes.
+ * 1 <= w <= 128, d in {64, 128}, any Hq / Hkv, Hq <= 2^18, B * w * Hq <= 2^24.  Workspace: pc_cache_attn_workspace_bytes(args), aligned to 32 bytes; it
+ * reads the sizes (B to n_own) and the caches' descriptors alone and holds for calls on the current device with those, whatever their other fields say
+ * (with or without k_win and v_win, their strides, own_len); 0: a bad argument.
  */
 typedef struct {
   int32_t B, w, Hq, Hkv, d;

@@ -186,7 +186,16 @@ bool tma_strides(const int64_t* s, int64_t B, int64_t w, int64_t H) {
   return (s[0] == 0 && s[1] == 0 && s[2] == 0) || ((s[0] != 0 || B == 1) && (s[1] != 0 || w == 1) && (s[2] != 0 || H == 1));
 }
 
-int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
+// More new tokens than these: their keys go through the matrix units, behind the caches' (up to them each row takes them one by one).  Measured, us, one by
+// one / units, 32/8 heads of 128 over 2000 int8 entries, a sequence and 16 of them: 12 tokens 18.1 / 24.2, 70.8 / 76.6; 24 22.2 / 25.1, 144.8 / 134.5;
+// 32 24.4 / 26.0, 197.7 / 167.7; 64 47.9 / 32.4, 442 / 320.
+constexpr int WINDOW_TOKENS = 24;
+bool window_phase(const pc_cache_attn_args* a) {
+  return a->k_win != nullptr && a->w > WINDOW_TOKENS && tma_strides(a->k_win_stride, a->B, a->w, a->Hkv) && tma_strides(a->v_win_stride, a->B, a->w, a->Hkv);
+}
+
+// window: the new tokens' keys are a phase of their own; lens: the own caches have lengths.  Nothing else is read of `a` but its sizes and the caches' descriptors.
+int32_t cache_plan(const pc_cache_attn_args* a, bool window, bool lens, int sm_count, CachePlan& p) {
   if (a->B < 1 || a->w < 1 || a->Hq < 1 || a->Hkv < 1 || a->Hq % a->Hkv != 0 || a->n_prefix < 0 || a->n_own < 0) return PC_ERR_INVALID_ARG;
   if (a->d != 64 && a->d != 128) return PC_ERR_UNSUPPORTED;
   if (a->w > 128 || a->Hq > (1 << 18) || (int64_t)a->B * a->w * a->Hq > (1 << 24)) return PC_ERR_UNSUPPORTED;
@@ -195,10 +204,6 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
   p.n_slots = 0;
   p.prefix = p.own = p.window = {};
   p.rows = p.halves = p.mark = p.finished = false;
-  // More than 24 new tokens: their keys go through the matrix units, behind the caches' (up to 24: each row takes them one by one).  Measured, us, one by
-  // one / units, 32/8 heads of 128 over 2000 int8 entries, a sequence and 16 of them: 12 tokens 18.1 / 24.2, 70.8 / 76.6; 24 22.2 / 25.1, 144.8 / 134.5;
-  // 32 24.4 / 26.0, 197.7 / 167.7; 64 47.9 / 32.4, 442 / 320.
-  const bool window = a->k_win != nullptr && a->w > 24 && tma_strides(a->k_win_stride, a->B, a->w, a->Hkv) && tma_strides(a->v_win_stride, a->B, a->w, a->Hkv);
   for (int own = 0; own <= 1; ++own) {
     const pc_kv_cache* const c = own ? a->own : a->prefix;
     const int n = own ? a->n_own : a->n_prefix;
@@ -216,13 +221,13 @@ int32_t cache_plan(const pc_cache_attn_args* a, int sm_count, CachePlan& p) {
     // 46.7 / 54.7, 48 70.8 / 67.6, 64 94.5 / 73.1, 256 320.7 / 159.5; ragged e4m3 d = 64 48 39.9 / 48.3, 128 93.0 / 63.4; bf16 d = 128 16 34.2 / 35.1,
     // 24 38.7 / 37.0, 64 85.2 / 56.8, d = 64 24 26.3 / 30.0, 48 43.4 / 39.1; 64 sequences, d = 64, 24 rows 94.7 / 78.7.
     const bool bf16 = c->format == PC_KV_BF16;
-    const bool many = own ? rows > (!bf16 ? 48 : a->d == 128 || (double)seqs * a->Hkv > 2.0 * sm_count ? 16 : 32) && (!bf16 || a->own_len == nullptr)
+    const bool many = own ? rows > (!bf16 ? 48 : a->d == 128 || (double)seqs * a->Hkv > 2.0 * sm_count ? 16 : 32) && (!bf16 || !lens)
                           : rows > (a->d == 128 && (bf16 || n <= 16384) ? 16 : 32);
     if (many) {
       ph = wide_plan(seqs, rows, a->Hkv, a->d, c->format, n, sm_count);
       p.rows = true;
       p.halves |= !bf16;
-      p.mark |= own && a->own_len != nullptr;
+      p.mark |= own && lens;
     } else {
       ph = few_plan(seqs, rows, a->Hkv, a->d, c->format, n, !window && (own || a->n_own == 0), sm_count);
     }
@@ -286,15 +291,26 @@ bool window_map(const pc_cache_attn_args* a, const void* x, const long long stri
 extern "C" {
 
 size_t pc_cache_attn_workspace_bytes(const pc_cache_attn_args* a) {
-  CachePlan p;
-  return a != nullptr && cache_plan(a, plan_sms(), p) == PC_OK ? p.total : 0;
+  if (a == nullptr) return 0;
+  // The most over what the call may come with beside its sizes: new tokens or none (or ones that TMA cannot fetch), lengths or none.  Where either makes no
+  // difference it is not asked for: plans are host time of every call.
+  const bool windows = a->w > WINDOW_TOKENS,
+             lengths = a->n_own > 0 && a->own != nullptr && a->own->format == PC_KV_BF16 && a->Hkv > 0 && (int64_t)a->w * a->Hq / a->Hkv > 16;
+  size_t most = 0;
+  for (int window = 0; window <= (windows ? 1 : 0); ++window)
+    for (int lens = 0; lens <= (lengths ? 1 : 0); ++lens) {
+      CachePlan p;
+      if (cache_plan(a, window != 0, lens != 0, plan_sms(), p) != PC_OK) return 0;
+      if (p.total > most) most = p.total;
+    }
+  return most;
 }
 
 int32_t pc_cache_attn(const pc_cache_attn_args* a, void* stream) {
   if (a == nullptr) return PC_ERR_INVALID_ARG;
   CachePlan plan;
   const int sms = pc::sm100_count();
-  if (int32_t rc = cache_plan(a, sms > 0 ? sms : 148, plan); rc != PC_OK) return rc;
+  if (int32_t rc = cache_plan(a, window_phase(a), a->own_len != nullptr, sms > 0 ? sms : 148, plan); rc != PC_OK) return rc;
   if (!a->q || !a->out || !aligned(a->q, 16) || !aligned(a->out, 16) || (a->k_win == nullptr) != (a->v_win == nullptr)) return PC_ERR_INVALID_ARG;
   if (!aligned(a->k_win, 16) || !aligned(a->v_win, 16) || !aligned(a->workspace, 32)) return PC_ERR_INVALID_ARG;
   if (a->n_prefix == 0 && a->n_own == 0 && a->k_win == nullptr) return PC_ERR_INVALID_ARG;              // nothing to attend to
