@@ -826,8 +826,8 @@ def cache_attn(q, k_win=None, v_win=None, *, prefix=None, n_prefix=None, own=Non
     caches and their own keys and values k_win, v_win [B,w,Hkv,d] (causal; None: not).
 
     n_prefix, n_own: valid entries (the capacities); own_len: int32 [B], entries of each sequence; positions of the queries:
-    q_pos0 + q_pos[b] + i.  ``buffers`` (dict) keeps out, lse, status and workspace between calls.
-    Returns dict(out, lse, status, workspace)."""
+    q_pos0 + q_pos[b] + i.  ``buffers`` (dict) keeps out, lse, status and workspace between calls; a call that needs less than is
+    kept has views of it.  Returns dict(out, lse, status, workspace)."""
     got = _cache_calls().attn(_stream(), True, q, k_win, v_win, prefix, own, own_len, q_pos, (out, lse_out, status, workspace), buffers,
                               _ALL if n_prefix is None else n_prefix, _ALL if n_own is None else n_own, q_pos0, want_lse, rope_theta, softmax_scale)
     if got[0] != 0:

@@ -418,6 +418,7 @@ PyObject* cache_attn(PyObject*, PyObject* args) {
     need(!keeps || PyDict_Check(buffers), "buffers must be a dict");
     at::Tensor t[4];
     PyObject* same[4] = {};                                          // objects that are returned as they came
+    bool serves[4] = {};                                             // what is kept stays, though this call may have a view of its first elements alone
     const int64_t s_out[4] = {B, w, Hq, d}, s_lse[3] = {B, Hq, w}, s_one[1] = {1};
     const at::IntArrayRef sizes[3] = {s_out, s_lse, s_one};
     const at::ScalarType types[4] = {at::kBFloat16, at::kFloat, at::kInt, at::kByte};
@@ -442,7 +443,7 @@ PyObject* cache_attn(PyObject*, PyObject* args) {
         if (t[i].sizes().equals(sizes[i])) { same[i] = p; continue; }
         int64_t count = 1;
         for (int64_t x : sizes[i]) count *= x;
-        if (t[i].numel() >= count) { t[i] = t[i].view(-1).narrow(0, 0, count).view(sizes[i]); continue; }
+        if (t[i].numel() >= count) { t[i] = t[i].view(-1).narrow(0, 0, count).view(sizes[i]); serves[i] = true; continue; }
         let_go(t[i]);
       }
       t[i] = at::empty(sizes[i], at::TensorOptions().dtype(types[i]).device(device));
@@ -469,7 +470,7 @@ PyObject* cache_attn(PyObject*, PyObject* args) {
     for (int i = 0; i < 4; ++i) {
       PyObject* const x = same[i] ? (Py_INCREF(same[i]), same[i]) : t[i].defined() ? THPVariable_Wrap(t[i]) : (Py_INCREF(Py_None), Py_None);
       const bool ok = x != nullptr && PyDict_SetItemString(result, names[i], x) == 0 &&
-                      (rc != PC_OK || !keeps || !t[i].defined() || PyDict_SetItemString(buffers, names[i], x) == 0);
+                      (rc != PC_OK || !keeps || !t[i].defined() || serves[i] || PyDict_SetItemString(buffers, names[i], x) == 0);
       Py_XDECREF(x);
       if (!ok) { Py_DECREF(result); return nullptr; }
     }
