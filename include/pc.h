@@ -431,7 +431,7 @@ typedef struct {
 
 /* Writes n new tokens of every sequence: token i of sequence b becomes entry at0 + (at ? at[b] : 0) + i.
  * k_src, v_src [B,n,Hkv,d] bf16 through element strides (sequence, token, head; host arrays of 3; 0,0,0 -> contiguous),
- * multiples of 8; at: device int32 [B] or NULL.  An entry outside [0, capacity) is not written, and status_word (may be
+ * multiples of 8; at: device int32 [B] or NULL; n <= 2^30.  An entry outside [0, capacity) is not written, and status_word (may be
  * NULL) then gets the code 401 (without `at` such a call is refused).  8-bit formats only.
  */
 PC_API int32_t pc_kv_quantize(const pc_kv_cache* cache, const void* k_src, const int64_t* k_stride, const void* v_src,
@@ -446,7 +446,7 @@ PC_API int32_t pc_gather_kv_quantize(const void* k_src, const void* v_src, const
                               void* stream);
 
 /* Reads n entries of every sequence back: k_out, v_out [B,Hkv,n,d] bf16 contiguous get code * scale rounded to bf16 of the
- * entries at0 + (at ? at[b] : 0) + i; entries outside [0, capacity) read as zeros.  8-bit formats only.
+ * entries at0 + (at ? at[b] : 0) + i; entries outside [0, capacity) read as zeros.  n <= 2^30.  8-bit formats only.
  */
 PC_API int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0, const int32_t* at, void* k_out, void* v_out,
                          void* stream);

@@ -11,6 +11,7 @@ namespace {
 
 constexpr size_t ALIGN = 256;
 size_t align_up(size_t x) { return (x + ALIGN - 1) / ALIGN * ALIGN; }
+constexpr int32_t MOST_ENTRIES = 1 << 30;        // of a call, inside a cache or not: the kernels round up to whole pieces in 32 bits
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 int32_t launched(cudaError_t e) {
   const cudaError_t pending = cudaGetLastError();
@@ -45,7 +46,7 @@ extern "C" {
 int32_t pc_kv_quantize(const pc_kv_cache* cache, const void* k_src, const int64_t* k_stride, const void* v_src, const int64_t* v_stride,
                        int32_t n, int32_t at0, const int32_t* at, int32_t* status_word, void* stream) {
   if (int32_t rc = check_cache(cache, true); rc != PC_OK) return rc;
-  if (!k_src || !v_src || !aligned(k_src, 16) || !aligned(v_src, 16) || n < 1) return PC_ERR_INVALID_ARG;
+  if (!k_src || !v_src || !aligned(k_src, 16) || !aligned(v_src, 16) || n < 1 || n > MOST_ENTRIES) return PC_ERR_INVALID_ARG;
   if (at == nullptr && (at0 < 0 || (int64_t)at0 + n > cache->capacity)) return PC_ERR_INVALID_ARG;
   pc::KvWrite w = {};
   if (!strides(k_stride, n, cache->Hkv, cache->d, w.k_stride) || !strides(v_stride, n, cache->Hkv, cache->d, w.v_stride)) return PC_ERR_INVALID_ARG;
@@ -84,7 +85,7 @@ int32_t pc_gather_kv_quantize(const void* k_src, const void* v_src, const int64_
 
 int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0, const int32_t* at, void* k_out, void* v_out, void* stream) {
   if (int32_t rc = check_cache(cache, true); rc != PC_OK) return rc;
-  if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16) || n < 1) return PC_ERR_INVALID_ARG;
+  if (!k_out || !v_out || !aligned(k_out, 16) || !aligned(v_out, 16) || n < 1 || n > MOST_ENTRIES) return PC_ERR_INVALID_ARG;
   if (pc::sm100_count() == 0) return PC_ERR_UNSUPPORTED;
   const pc::KvRead r = {static_cast<const uint8_t*>(cache->k), static_cast<const uint8_t*>(cache->v), cache->k_scale, cache->v_scale,
                         cache->capacity, cache->B, cache->Hkv, n, at0, at, k_out, v_out, aligned(k_out, 32) && aligned(v_out, 32)};
