@@ -463,9 +463,15 @@ PC_API int32_t pc_kv_dequantize(const pc_kv_cache* cache, int32_t n, int32_t at0
  * One softmax over all of them.  prefix and own may have different formats; entries behind those named are never used, whatever
  * they hold.  Keys are rotated already; token i of sequence b is rotated here at position p = q_pos0 + (q_pos ? q_pos[b] : 0) + i
  * and rounded to bf16: in fp32 (angles are the fp32 products p * theta^(-2t/d), as models compute them; from p = 2^15 on
- * they are computed in fp64), where pc_parallel_attn rounds the fp64 rotation; rope_theta = 0: queries come rotated.  q, k_win and v_win through element
+ * they are computed in fp64), where pc_parallel_attn and the rotated keys of this library have the fp64 rotation rounded once: below 2^15 the two
+ * differ by up to p * 2^-22 of an element's pair; rope_theta = 0: queries come rotated, by the caller's own rule.  q, k_win and v_win through element
  * strides (sequence, token, head; 0,0,0 -> contiguous), multiples of 8.  A row that sees nothing gets zeros and lse -infinity.
  * out [B,w,Hq,d] bf16 and lse [B,Hq,w] fp32 (natural log; may be NULL) contiguous.
+ * Logits, maxima, sums and accumulators are fp32.  Probabilities are rounded to bf16 or, few rows over codes, half precision.  Up to some 16 to 48 rows of
+ * a kv-head (the new tokens times Hq / Hkv, over a prefix of all sequences) the codes of an 8-bit cache are exact operands; from there on its values
+ * are taken as code * scale rounded to bf16, as pc_kv_dequantize returns them.
+ * Which call: pc_parallel_attn (and pc_parallel_attn_append) for bf16 caches whose sequences all have one length, as the path leaves them; this one
+ * for 8-bit caches, for lengths on the device, for a prefix that is shared, or for new tokens that are in the cache already.
  * 1 <= w <= 128, d in {64, 128}, any Hq / Hkv, Hq <= 2^18, B * w * Hq <= 2^24.  Workspace: pc_cache_attn_workspace_bytes(args), aligned to 32 bytes; it
  * reads the sizes (B to n_own) and the caches' descriptors alone and holds for calls on the current device with those, whatever their other fields say
  * (with or without k_win and v_win, their strides, own_len); 0: a bad argument.

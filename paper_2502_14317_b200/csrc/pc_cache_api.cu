@@ -132,9 +132,15 @@ PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n
   p.n_rg = (int)((rows + p.group - 1) / p.group);
   const double items = (double)seqs * Hkv * p.n_rg;
   // Short caches: four smaller CTAs per SM (16 rows: three) where they take fewer rounds than two; up to 2048 entries for half the rounds, else 1024.
-  // Measured, us, two / four (three), full int8 caches of head size 128.  8 rows: 320 items of 60 entries 14.6 / 8.9, of 1000 30.5 / 28.2, of 2000
-  // 49.8 / 47.7 (ragged, up to 1000 21.8 / 23.6, up to 2000 37.5 / 39.4); 768 of 1000 54.0 / 55.9 (ragged 42.8 / 38.7), of 2000 84.3 / 92.0.
-  // 16 rows: 384 of 1000 57.0 / 41.4; 512 (as many rounds) 56.4 / 67.7; 768 81.5 / 79.2, of 2000 120.5 / 124.2.
+  // Measured, us, two / four (three), int8 caches, G = 8, full and (ragged).
+  // 8 rows, head size 128: 320 items of 60 entries 15.4 / 11.2 (15.8 / 10.9), of 1000 30.5 / 29.7 (21.5 / 25.2), of 2000 51.3 / 50.1 (35.8 / 40.9);
+  // 512 of 1000 39.7 / 33.8 (31.7 / 27.9); 768 of 1000 56.6 / 60.9 (45.1 / 43.6), of 2000 86.9 / 94.9 (61.4 / 64.3).  Head size 64: 320 of 1000 25.8 / 20.4
+  // (18.6 / 18.5); 512 of 2000 43.4 / 35.9 (35.3 / 30.3); 768 of 2000 62.3 / 63.3 (48.5 / 45.2).
+  // 16 rows, head size 128: 320 of 1000 56.6 / 40.9 (43.7 / 36.2), of 2000 76.0 / 65.1 (52.0 / 56.6); 512 (as many rounds) of 1000 61.8 / 70.6 (50.7 / 52.4);
+  // 768 of 1000 89.2 / 84.4 (73.1 / 70.1).  Head size 64: 320 of 2000 51.4 / 37.9 (36.9 / 33.6); 512 of 1000 40.8 / 45.8 (35.8 / 37.9); 768 of 1000 61.7 / 55.3
+  // (50.3 / 46.0), of 2000 85.0 / 78.0 (67.2 / 64.5).
+  // The rule goes by the most entries that lengths may name, not by the lengths, which the host does not see.  Where it loses most: ragged, one round of
+  // short CTAs at head size 128, up to 17 % (8 rows), 9 % (16); 593 to 600 items of 16 rows at head size 64, ragged bf16, 11 %; else up to 8 %.
   const double small = (p.group == 8 ? 4.0 : 3.0) * sm_count, rounds2 = std::ceil(items / (2.0 * sm_count)), rounds4 = std::ceil(items / small);
   p.brief = rounds4 < rounds2 && n_keys <= (2.0 * rounds4 <= rounds2 ? 2048 : 1024);
   const int keys = pc::few_keys(format, d, p.brief), tiles = (n_keys + keys - 1) / keys;
@@ -160,8 +166,9 @@ PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n
 }
 
 // Row groups and splits of the kernel for many rows: least time by a model in microseconds, as for the query windows - rounds
-// of the grid x (5 for an item + a tile), and the partial results through memory twice.
-PhasePlan wide_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count) {
+// of the grid x (5 for an item + a tile), and the partial results through memory twice.  A tile has one price for all formats and head sizes, that of alt 1.2
+// (measured on CTA pairs at head size 128: bf16 0.9, codes 1.3); it weighs rounds against splits and no more.
+PhasePlan wide_plan(int64_t seqs, int64_t rows, int Hkv, int d, int n_keys, int sm_count) {
   PhasePlan p = {};
   p.wide = true;
   // CTA pairs for more rows than a block has.  Measured, us, without / with, 65536 entries: 128 rows bf16 57.5 / 66.9, int8 72.8 / 91.6; 256 rows 78.8 / 73.0,
@@ -225,7 +232,7 @@ int32_t cache_plan(const pc_cache_attn_args* a, bool window, bool lens, int sm_c
     const bool many = own ? rows > (!bf16 ? 48 : a->d == 128 || (double)seqs * a->Hkv > 2.0 * sm_count ? 16 : 32) && (!bf16 || !lens)
                           : rows > (a->d == 128 && (bf16 || n <= 16384) ? 16 : 32);
     if (many) {
-      ph = wide_plan(seqs, rows, a->Hkv, a->d, c->format, n, sm_count);
+      ph = wide_plan(seqs, rows, a->Hkv, a->d, n, sm_count);
       p.rows = true;
       p.halves |= !bf16;
       p.mark |= own && lens;

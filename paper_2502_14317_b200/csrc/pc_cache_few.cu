@@ -30,14 +30,15 @@ namespace pc {
 namespace {
 
 // CAUSAL: the entries are the new tokens themselves, token i sees 0 .. i.
-// SHORT: four CTAs per SM (16 rows: three) of three consumer warps and stages of half the size, for many sequences with few entries
+// SHORT: for many sequences with few entries, four CTAs per SM (16 rows: three) instead of two, with half the ring: three consumer warps (16 rows at head
+// size 64: four) instead of seven (16 rows at 128: five), stages of half the size (codes at head size 64, 16 KB: the same, and half as many).
 template <int D_, int FMT_, int NT8_, bool SHORT_, bool CAUSAL_ = false>
 struct Few {
   static constexpr int D = D_, FMT = FMT_, NT8 = NT8_;
   static constexpr bool CAUSAL = CAUSAL_;
   static constexpr int EB = FMT == FMT_BF16 ? 2 : 1;            // bytes of an element
   static constexpr int ROWB = D * EB, BOXES = ROWB > 128 ? 2 : 1, BOXB = ROWB / BOXES, EPB = BOXB / EB;
-  // Consumer warps: with the producers 16 warps an SM, 128 registers a thread, or for 16 rows at head size 128 12 and 168.  (16 rows at head size 64, 12 / 16
+  // Consumer warps: with the producers 16 warps an SM (15 of the short build for 16 rows), 128 registers a thread, or for 16 rows at head size 128 12 and 168.  (16 rows at head size 64, 12 / 16
   // warps, us: 64 sequences of 2000 e4m3 entries, 8 kv-heads 60.5 / 55.2, of 8000 146.7 / 133.8, int8 164.2 / 150.8, bf16 167.5 / 165.2; 23 of up to 5000 22.4 / 21.4.)
   static constexpr int CTAS = SHORT_ ? (NT8 == 1 ? 4 : 3) : 2, WARPS = (NT8 == 1 || D == 64 ? 16 : 12) / CTAS - 1;
   static constexpr int UNITS = (ROWB == 256 ? 4 : 8) / (SHORT_ && ROWB != 64 ? 2 : 1);             // of a stage

@@ -1,8 +1,8 @@
 // The rotated queries of pc_cache_attn, a row per warp: lane l holds the elements E l .. E l + E - 1, E = d / 32.
 //
 // In fp32, pairs (t, t + d/2), angle = position * theta^(-2t/d) as one fp32 product, as models compute it: off by at most 2^-22 of
-// itself, up to position 8192, the longest chunk, by less than half a step of the bf16 result.  From position 2^15 on, where the fp32
-// product would be off by whole steps, the angle is computed in fp64.
+// itself, up to position 8192, the longest chunk, by less than half a step of the bf16 result, at 2^15 by up to two.  From there on the angle is
+// computed in fp64.  A caller who wants the fp64 rotation everywhere, as the keys of this library have it, rotates the queries and gives theta 0.
 #pragma once
 #include "pc_cache.h"
 #include "pc_sm100.cuh"
