@@ -497,6 +497,102 @@ PC_API size_t pc_cache_attn_workspace_bytes(const pc_cache_attn_args* args);
 
 PC_API int32_t pc_cache_attn(const pc_cache_attn_args* args, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Paged caches.  A pool is a pc_kv_cache in any of its formats whose B "sequences" are pages and whose capacity is the entries of a
+ * page: k, v [pages,Hkv,page,d].  Entry e of sequence b is entry e % page of page table[b * table_stride + e / page] (device int32; n_table
+ * pages a sequence, whether used or not; table_stride 0: all sequences have the same).  Sequences may share pages that none of them
+ * writes.  A page has a multiple of 16 entries, or any number if n_table = 1; page * n_table <= 2^28.  An id that is no page of the pool is
+ * never followed: what would be written there is not, what would be read counts as zeros, and status_word (may be NULL) gets the code 421.
+ *
+ * pc_page_append: new tokens into their sequences' pages.  Token j < n of sequence b becomes entry at0 + (at ? at[b] : 0) + j; its key
+ * is rotated to position p = pos0 + (pos ? pos[b] : its sequence's first new entry) + j on the way (pairs (t, t + d/2), angle p * theta^(-2t/d) with
+ * p and the angle in fp64, sine, cosine and products in fp32, rounded once to the format; rope_theta = 0: keys come rotated).
+ *   count    device int32 [B]: only the first count[b] tokens (clamped into [0, n]) are written; NULL: n.
+ *   pick     device int32 [B,n] (pick_stride elements a sequence): token j is token pick[b,j] of the n_src tokens of k and v; an index
+ *            outside [0, n_src) leaves entry j as it was.  NULL: token j of n.
+ *   parents  device int32 [B,n], n <= 64: drafted tokens, as in pc_tree_attn: token j is rotated to the position of its depth, entry by
+ *            entry they stand one behind the other; a token that is not there leaves its entry as it was.  Not with pick.
+ * A sequence whose first entry is negative is left out.  An entry beyond the table is not written, code 421.  8-bit formats: as pc_kv_quantize, from
+ * the fp32 rotation.  k, v [B,n (n_src),Hkv,d] bf16 through element strides (sequence, token, head; 0,0,0 -> contiguous), multiples of 8.  An entry
+ * that is named twice in one call holds one of the two.
+ */
+typedef struct {
+  int32_t B, n, n_src, at0, pos0, n_table;
+  float rope_theta;
+  const pc_kv_cache* pages;
+  const int32_t* table;
+  int64_t table_stride;
+  const void *k, *v;
+  int64_t k_stride[3], v_stride[3];
+  const int32_t *at, *pos, *count, *pick, *parents;
+  int64_t pick_stride, parents_stride;
+  int32_t* status_word;
+} pc_page_append_args;
+
+PC_API int32_t pc_page_append(const pc_page_append_args* args, void* stream);
+
+/* Attention of drafted tokens over paged caches.  Each of B sequences has lens[b] entries and, behind them, w <= 64 new tokens that are in its pages
+ * already (pc_page_append with at = lens): entries lens[b] .. lens[b] + w - 1.  New token i sees the entries before lens[b], its ancestors and
+ * itself.  parents (device int32 [B,w], parents_stride elements a sequence, 0: one tree for all): parents[b,i] in [0, i) is token i's
+ * parent, -1: it has none (the context's end is); anything else says that the token is not there (so are its descendants).  NULL: each token's parent
+ * is the one before it (causal); w = 1: a decoding step.
+ * Token i is rotated to pos0 + (pos ? pos[b] : lens[b]) + its depth (the number of its ancestors), rounded to bf16; rope_theta = 0: queries come rotated.
+ * lens[b] < 0: no such sequence.  Rows of tokens or sequences that are not there get zeros and lse -infinity.  lens[b] > max_len or
+ * lens[b] + w > page * n_table: as if there were no such sequence, and status_word gets the code 422.  max_len + w <= page * n_table; a max_len
+ * near the longest plans the launch best.
+ * What a mask hides, what stands behind a sequence's end and in pages that it does not name does not reach a row, whatever it holds, NaN included.
+ * Precision as for pc_cache_attn.  q [B,w,Hq,d] through element strides; out [B,w,Hq,d] bf16, lse [B,Hq,w] fp32 (natural log; may be NULL) contiguous.
+ * d, Hkv: the pool's; any Hq / Hkv, Hq <= 2^18, B * w * Hq <= 2^24.  Workspace: pc_tree_attn_workspace_bytes(args), aligned to 32 bytes; it reads
+ * B, w, Hq, max_len and the pool's descriptor alone; 0: a bad argument.
+ */
+typedef struct {
+  int32_t B, w, Hq, n_table, max_len, pos0, clear_status;
+  float rope_theta, softmax_scale;               /* softmax_scale 0 -> 1/sqrt(d) */
+  const void* q;
+  int64_t q_stride[3];
+  const pc_kv_cache* pages;
+  const int32_t* table;
+  int64_t table_stride;
+  const int32_t *lens, *pos, *parents;
+  int64_t parents_stride;
+  void* out;
+  float* lse;
+  int32_t* status_word;
+  void* workspace;
+  size_t workspace_bytes;
+} pc_tree_attn_args;
+
+PC_API size_t pc_tree_attn_workspace_bytes(const pc_tree_attn_args* args);
+
+PC_API int32_t pc_tree_attn(const pc_tree_attn_args* args, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * Log probabilities.  Paper: Eq. 3, I_c = -log P(X^q | X^c): with the logits of the query window behind every chunk, nll with group = w is the
+ * chunk score that pc_select_chunks and pc_hot_path take.  And what a server needs of drafted tokens.
+ * logits: N rows of V in fp32, bf16 or fp16, `stride` elements apart (0: one row for all), any alignment.  Of row i, z = scale * logits:
+ *   logprob[i]       z[tokens[i]] - log sum exp z (tokens: device int32 [N]; both NULL: not).  A token < 0 gets 0 (it adds nothing to a sum), >= V NaN
+ *   entropy[i]       - sum p log p, natural log; NULL: not
+ *   top_id, top_logprob [N,top]  the `top` <= 32 largest logits in descending order, equal ones by the lower index
+ *   nll[g]           - (sum of logprob over the `group` rows of group g), N % group = 0; NULL: not.  The order of the sum is always the same
+ * A row of nothing but -infinity: log probabilities -infinity, entropy 0, tokens 0, 1, 2, ..  A row with a NaN or +infinity: NaN, tokens -1.
+ * Exponents and sums are fp32.  Nothing is allocated, no workspace.
+ */
+#define PC_MOST_ALTERNATIVES 32
+enum { PC_LOGITS_F32 = 0, PC_LOGITS_BF16 = 1, PC_LOGITS_F16 = 2 };
+
+typedef struct {
+  int32_t type, N, V, top, group;
+  float scale;
+  int64_t stride;
+  const void* logits;
+  const int32_t* tokens;
+  float *logprob, *entropy, *top_logprob;
+  int32_t* top_id;
+  float* nll;
+} pc_token_logprobs_args;
+
+PC_API int32_t pc_token_logprobs(const pc_token_logprobs_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

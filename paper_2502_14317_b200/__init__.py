@@ -12,4 +12,5 @@ from .binding import (  # noqa: F401
     parallel_attn_static, parallel_attn_static_scratch_bytes, hot_path, hot_path_from_host,
     queue_init, queue_update, queue_gather, queue_select_gather, queue_emit, hot_path_streaming,
     kv_cache, kv_quantize, gather_kv_quantize, kv_dequantize, cache_attn,
+    page_append, tree_attn, token_logprobs,
 )

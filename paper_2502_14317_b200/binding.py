@@ -833,3 +833,63 @@ def cache_attn(q, k_win=None, v_win=None, *, prefix=None, n_prefix=None, own=Non
     if got[0] != 0:
         _refused(got if isinstance(got, str) else got[0], "pc_cache_attn")
     return got[1]
+
+
+# ------------------------------------------------------------------------------------ paged caches, drafted tokens, log probabilities
+class _TreeCalls:
+    """The calls below, made by csrc/pc_host.cpp as those on 8-bit caches."""
+
+    def __init__(self, lib):
+        host = _host_module()
+        self.append = functools.partial(host.page_append, _address(lib.pc_page_append))
+        self.attn = functools.partial(host.tree_attn, _address(lib.pc_tree_attn_workspace_bytes), _address(lib.pc_tree_attn))
+        self.logprobs = functools.partial(host.token_logprobs, _address(lib.pc_token_logprobs))
+
+
+def _tree_calls():
+    lib = _LIB or load_library()
+    calls = getattr(lib, "_tree_calls", None)
+    if calls is None:
+        calls = lib._tree_calls = _TreeCalls(lib)
+    return calls
+
+
+def page_append(cache, k, v, table, *, at, rope_theta=0.0, pos=None, pos0=0, count=None, pick=None, parents=None, status=None):
+    """pc_page_append: k, v [B,n,Hkv,d] bf16 into the pages of their sequences, keys rotated on the way.
+
+    cache: a pool of pages, kv_cache(pages, Hkv, entries of a page, d, format); table: int32 [B, pages of a sequence], the pool's pages that a
+    sequence's entries stand in, in order.  Token j of sequence b becomes entry at + j (at: a number or int32 [B]) and its key is rotated to
+    position pos0 + (pos[b], or its sequence's first new entry) + j; rope_theta 0: keys come rotated.  count: int32 [B], tokens of each sequence; pick:
+    int32 [B,m], token j is token pick[b,j] of k and v (m tokens are written; -1: none); parents: as in tree_attn, positions by depth.
+    Entries that have no page are not written, and ``status`` (int32) says so."""
+    rc = _tree_calls().append(_stream(), True, cache, k, v, table, at, pos, count, pick, parents, status, pos0, rope_theta)
+    if rc != 0:
+        _refused(rc, "pc_page_append")
+    return cache
+
+
+def tree_attn(q, cache, table, lens, *, parents=None, pos=None, pos0=0, rope_theta=0.0, softmax_scale=0.0, max_len=None, out=None, lse_out=None,
+              want_lse=False, status=None, workspace=None, buffers=None):
+    """pc_tree_attn: w <= 64 drafted tokens of B sequences, q [B,w,Hq,d], over the pages of their sequences.
+
+    lens: int32 [B], entries before the new tokens, which are in the pages already, from entry lens[b] on (page_append with at=lens); -1: no
+    such sequence.  parents: int32 [B,w] or [w], the token that each new token follows, -1: the context's end, -2: the token is not there; None:
+    the one before it.  A token sees the context, its ancestors and itself.  Positions of the queries: pos0 + (pos[b] or lens[b]) + depth.  max_len: the
+    most of lens (as many as the table holds).  ``buffers`` as in cache_attn.  Returns dict(out, lse, status, workspace)."""
+    got = _tree_calls().attn(_stream(), True, q, cache, table, lens, pos, parents, (out, lse_out, status, workspace), buffers,
+                             _ALL if max_len is None else max_len, pos0, want_lse, rope_theta, softmax_scale)
+    if got[0] != 0:
+        _refused(got if isinstance(got, str) else got[0], "pc_tree_attn")
+    return got[1]
+
+
+def token_logprobs(logits, tokens=None, *, top=0, group=0, want_entropy=False, scale=1.0):
+    """pc_token_logprobs: rows of logits [N,V] fp32, bf16 or fp16 (times ``scale``, 1 / temperature) -> dict of
+
+    logprob [N] of tokens (int32 [N]; negative: 0), entropy [N], top_id and top_logprob [N,top] (the most probable tokens, equal ones by the
+    lower id), nll [N / group] (minus the sum of logprob over each group of rows: with the logits of the query window behind every
+    chunk and group = w, the chunk_score that hot_path takes).  What is not asked for is None."""
+    got = _tree_calls().logprobs(_stream(), True, logits, tokens, top, group, want_entropy, scale)
+    if got[0] != 0:
+        _refused(got if isinstance(got, str) else got[0], "pc_token_logprobs")
+    return got[1]

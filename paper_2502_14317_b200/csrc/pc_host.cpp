@@ -361,6 +361,85 @@ PyObject* kv_dequantize(PyObject*, PyObject* args) {
   END_HANDLE_TH_ERRORS
 }
 
+// Outputs and workspace of an attention call (out, lse, status, workspace): given, kept from an earlier call (through a view where that had other
+// sizes), or new.
+struct AttnOut {
+  static constexpr const char* names[4] = {"out", "lse", "status", "workspace"};
+  static constexpr at::ScalarType types[4] = {at::kBFloat16, at::kFloat, at::kInt, at::kByte};
+  at::Device device;
+  PyObject *const *given, *buffers;
+  const bool keeps;
+  at::Tensor t[4];
+  PyObject* same[4] = {};                                            // objects that are returned as they came
+  bool serves[4] = {};                                               // what is kept stays, though this call may have a view of its first elements alone
+  int32_t clear_status = 0;
+
+  void fits(int i, const char* why) const { need(t[i].scalar_type() == types[i] && t[i].device() == device && t[i].is_contiguous(), why); }
+  PyObject* kept(int i) const { return keeps ? PyDict_GetItemString(buffers, names[i]) : nullptr; }
+  static void let_go(at::Tensor& x) {
+    if (x.is_cuda()) x.record_stream(c10::impl::VirtualGuardImpl(x.device().type()).getStream(x.device()));
+  }
+  AttnOut(at::Device dev, PyObject* const (&g)[4], PyObject* b, bool want_lse, int64_t B, int64_t w, int64_t Hq, int64_t d)
+      : device(dev), given(g), buffers(b), keeps(b != Py_None) {
+    need(!keeps || PyDict_Check(buffers), "buffers must be a dict");
+    const int64_t s_out[4] = {B, w, Hq, d}, s_lse[3] = {B, Hq, w}, s_one[1] = {1};
+    const at::IntArrayRef sizes[3] = {s_out, s_lse, s_one};
+    for (int i = 0; i < 3; ++i) {
+      if (i == 1 && !want_lse && given[1] == Py_None) continue;
+      if (is_tensor(given[i], t[i], "out, lse_out and status must be tensors")) {
+        static const char* const bad[3] = {"out must be contiguous bfloat16 [B, w, Hq, d]", "lse_out must be contiguous float32 [B, Hq, w]",
+                                           "status must be a contiguous int32 tensor"};
+        fits(i, bad[i]);
+        need(i == 2 ? t[i].numel() >= 1 : t[i].sizes().equals(sizes[i]), bad[i]);
+        same[i] = given[i];
+        continue;
+      }
+      PyObject* const p = kept(i);
+      if (is_tensor(p, t[i], "buffers must hold tensors")) {
+        fits(i, "a kept buffer is of another type or device, or not contiguous");
+        if (t[i].sizes().equals(sizes[i])) { same[i] = p; continue; }
+        int64_t count = 1;
+        for (int64_t x : sizes[i]) count *= x;
+        if (t[i].numel() >= count) { t[i] = t[i].view(-1).narrow(0, 0, count).view(sizes[i]); serves[i] = true; continue; }
+        let_go(t[i]);
+      }
+      t[i] = at::empty(sizes[i], at::TensorOptions().dtype(types[i]).device(device));
+      if (i == 2) clear_status = 1;
+    }
+  }
+  void workspace(size_t bytes) {                                     // 0: a bad argument, which the call names
+    PyObject* const p = given[3] != Py_None ? given[3] : kept(3);
+    const bool has = is_tensor(p, t[3], "workspace must be a tensor");
+    if (has) fits(3, "workspace must be a contiguous uint8 tensor on the queries' device");
+    if (has && (size_t)t[3].numel() >= bytes) {
+      same[3] = p;
+    } else {
+      if (has) let_go(t[3]);
+      t[3] = at::empty({(int64_t)std::max<size_t>(bytes, 16)}, at::TensorOptions().dtype(at::kByte).device(device));
+    }
+  }
+  template <class A>
+  void put(A& a) const {
+    a.out = t[0].data_ptr();
+    a.lse = t[1].defined() ? static_cast<float*>(t[1].data_ptr()) : nullptr;
+    a.status_word = static_cast<int32_t*>(t[2].data_ptr());
+    a.workspace = t[3].data_ptr();
+    a.workspace_bytes = (size_t)t[3].numel();
+  }
+  PyObject* result(int32_t rc) const {                               // (result code, dict of out, lse, status, workspace)
+    PyObject* const r = PyDict_New();
+    if (r == nullptr) return nullptr;
+    for (int i = 0; i < 4; ++i) {
+      PyObject* const x = same[i] ? (Py_INCREF(same[i]), same[i]) : t[i].defined() ? THPVariable_Wrap(t[i]) : (Py_INCREF(Py_None), Py_None);
+      const bool ok = x != nullptr && PyDict_SetItemString(r, names[i], x) == 0 &&
+                      (rc != PC_OK || !keeps || !t[i].defined() || serves[i] || PyDict_SetItemString(buffers, names[i], x) == 0);
+      Py_XDECREF(x);
+      if (!ok) { Py_DECREF(r); return nullptr; }
+    }
+    return Py_BuildValue("iN", (int)rc, r);
+  }
+};
+
 // cache_attn(ws_bytes, run, stream, need_cuda, q, k_win, v_win, prefix, own, own_len, q_pos, (out, lse, status, workspace), buffers,
 //            n_prefix, n_own, q_pos0, want_lse, rope_theta, softmax_scale)
 // -> (result code, dict of out, lse, status, workspace), or the reason of a refusal.  Every object may be None but q; n = ALL: the capacity.
@@ -412,69 +491,188 @@ PyObject* cache_attn(PyObject*, PyObject* args) {
     }
     a.q_pos = per_sequence(q_pos, B, device, "q_pos must be a contiguous int32 tensor with one entry per sequence");
     a.own_len = per_sequence(own_len, B, device, "own_len must be a contiguous int32 tensor with one entry per sequence");
-    // outputs and workspace: given, kept from an earlier call (through a view where that had other sizes), or new
-    static const char* const names[4] = {"out", "lse", "status", "workspace"};
-    const bool keeps = buffers != Py_None;
-    need(!keeps || PyDict_Check(buffers), "buffers must be a dict");
-    at::Tensor t[4];
-    PyObject* same[4] = {};                                          // objects that are returned as they came
-    bool serves[4] = {};                                             // what is kept stays, though this call may have a view of its first elements alone
-    const int64_t s_out[4] = {B, w, Hq, d}, s_lse[3] = {B, Hq, w}, s_one[1] = {1};
-    const at::IntArrayRef sizes[3] = {s_out, s_lse, s_one};
-    const at::ScalarType types[4] = {at::kBFloat16, at::kFloat, at::kInt, at::kByte};
-    auto kept = [&](int i) { return keeps ? PyDict_GetItemString(buffers, names[i]) : nullptr; };
-    auto fits = [&](int i, const char* why) {
-      need(t[i].scalar_type() == types[i] && t[i].device() == device && t[i].is_contiguous(), why);
-    };
-    auto let_go = [&](at::Tensor& x) { if (x.is_cuda()) x.record_stream(c10::impl::VirtualGuardImpl(x.device().type()).getStream(x.device())); };
-    for (int i = 0; i < 3; ++i) {
-      if (i == 1 && !want_lse && given[1] == Py_None) continue;
-      if (is_tensor(given[i], t[i], "out, lse_out and status must be tensors")) {
-        static const char* const bad[3] = {"out must be contiguous bfloat16 [B, w, Hq, d]", "lse_out must be contiguous float32 [B, Hq, w]",
-                                           "status must be a contiguous int32 tensor"};
-        fits(i, bad[i]);
-        need(i == 2 ? t[i].numel() >= 1 : t[i].sizes().equals(sizes[i]), bad[i]);
-        same[i] = given[i];
-        continue;
-      }
-      PyObject* const p = kept(i);
-      if (is_tensor(p, t[i], "buffers must hold tensors")) {
-        fits(i, "a kept buffer is of another type or device, or not contiguous");
-        if (t[i].sizes().equals(sizes[i])) { same[i] = p; continue; }
-        int64_t count = 1;
-        for (int64_t x : sizes[i]) count *= x;
-        if (t[i].numel() >= count) { t[i] = t[i].view(-1).narrow(0, 0, count).view(sizes[i]); serves[i] = true; continue; }
-        let_go(t[i]);
-      }
-      t[i] = at::empty(sizes[i], at::TensorOptions().dtype(types[i]).device(device));
-      if (i == 2) a.clear_status = 1;
+    AttnOut o(device, given, buffers, want_lse != 0, B, w, Hq, d);
+    a.clear_status = o.clear_status;
+    o.workspace(entry<size_t (*)(const pc_cache_attn_args*)>(ws_bytes)(&a));
+    o.put(a);
+    return o.result(entry<int32_t (*)(const pc_cache_attn_args*, void*)>(run)(&a, entry<void*>(stream)));
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// ------------------------------------------------------------------------------------ paged caches, drafted tokens, log probabilities
+// The launches go to the current device's stream.
+void need_current(at::Device device) {
+  need(device.is_cuda(), "tensors must live on a CUDA device");
+  need(c10::impl::VirtualGuardImpl(device.type()).getDevice() == device, "tensors must live on the current CUDA device");
+}
+// int32 [B,n] with a contiguous last dimension -> address and stride; null: None
+const int32_t* table_of(PyObject* p, int64_t B, int64_t n, at::Device device, int64_t& stride, const char* why) {
+  at::Tensor t;
+  stride = 0;
+  if (!is_tensor(p, t, why)) return nullptr;
+  need(t.dim() == 2 && t.size(0) == B && (n < 0 || t.size(1) == n) && t.size(1) >= 1 && t.size(1) <= INT32_MAX && t.scalar_type() == at::kInt &&
+       t.device() == device && (t.stride(1) == 1 || t.size(1) == 1), why);
+  stride = B > 1 ? t.stride(0) : 0;
+  return static_cast<const int32_t*>(t.data_ptr());
+}
+
+// page_append(run, stream, need_cuda, cache, k, v, table, at, pos, count, pick, parents, status, pos0, rope_theta) -> result code, or the reason of a refusal
+PyObject* page_append(PyObject*, PyObject* args) {
+  HANDLE_TH_ERRORS
+  unsigned long long run, stream;
+  int cuda;
+  long long pos0;
+  double theta;
+  PyObject *dict, *pk, *pv, *table, *at, *pos, *count, *pick, *parents, *status;
+  if (!PyArg_ParseTuple(args, "KKpOOOOOOOOOOLd", &run, &stream, &cuda, &dict, &pk, &pv, &table, &at, &pos, &count, &pick, &parents, &status, &pos0, &theta))
+    return nullptr;
+  return refusing([&]() {
+    const char* const bad = "k and v must be bfloat16 [B, n, Hkv, d] with the Hkv and d of the pages and a contiguous head dimension, on their device";
+    const Cache c(dict);
+    if (cuda) need_current(c.device);
+    at::Tensor k, v, st, t;
+    need(is_tensor(pk, k, bad) && is_tensor(pv, v, bad) && k.dim() == 4 && k.size(0) >= 1 && k.size(0) <= INT32_MAX && k.size(1) <= INT32_MAX, bad);
+    const int64_t B = k.size(0), sizes[4] = {B, k.size(1), c.c.Hkv, c.c.d};
+    pc_page_append_args a = {};
+    a.k = rows_of(k, sizes, c.device, a.k_stride, bad);
+    a.v = rows_of(v, sizes, c.device, a.v_stride, bad);
+    a.pages = &c.c;
+    a.B = (int32_t)B;
+    a.n = a.n_src = (int32_t)k.size(1);
+    const char* const bad_table = "table must be int32 [B, pages of a sequence] with a contiguous last dimension, on the pages' device";
+    need(is_tensor(table, t, bad_table) && t.dim() == 2, bad_table);
+    a.table = table_of(table, B, -1, c.device, a.table_stride, bad_table);
+    a.n_table = (int32_t)t.size(1);
+    const char* const bad_pick = "pick must be int32 [B, tokens to be written] with a contiguous last dimension, on the pages' device";
+    if (is_tensor(pick, t, bad_pick)) {
+      need(t.dim() == 2, bad_pick);
+      a.n = (int32_t)t.size(1);
+      a.pick = table_of(pick, B, -1, c.device, a.pick_stride, bad_pick);
     }
-    const size_t bytes = entry<size_t (*)(const pc_cache_attn_args*)>(ws_bytes)(&a);           // 0: a bad argument, which the call below names
-    PyObject* const p = given[3] != Py_None ? given[3] : kept(3);
-    const bool has_ws = is_tensor(p, t[3], "workspace must be a tensor");
-    if (has_ws) fits(3, "workspace must be a contiguous uint8 tensor on the queries' device");
-    if (has_ws && (size_t)t[3].numel() >= bytes) {
-      same[3] = p;
+    a.parents = table_of(parents, B, a.n, c.device, a.parents_stride, "parents must be int32 [B, n] with a contiguous last dimension, on the pages' device");
+    need(a.parents == nullptr || a.pick == nullptr, "pick and parents do not go together");
+    a.at = start_of(at, B, c.device, a.at0);
+    a.pos = per_sequence(pos, B, c.device, "pos must be a contiguous int32 tensor with one entry per sequence");
+    a.count = per_sequence(count, B, c.device, "count must be a contiguous int32 tensor with one entry per sequence");
+    const char* const bad_status = "status must be an int32 tensor on the pages' device";
+    const bool has = is_tensor(status, st, bad_status);
+    need(!has || (st.scalar_type() == at::kInt && st.numel() >= 1 && st.device() == c.device), bad_status);
+    a.status_word = has ? static_cast<int32_t*>(st.data_ptr()) : nullptr;
+    need(pos0 >= INT32_MIN && pos0 <= INT32_MAX, "pos0 must be a number of 32 bits");
+    a.pos0 = (int32_t)pos0;
+    a.rope_theta = (float)theta;
+    return PyLong_FromLong(entry<int32_t (*)(const pc_page_append_args*, void*)>(run)(&a, entry<void*>(stream)));
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// tree_attn(ws_bytes, run, stream, need_cuda, q, cache, table, lens, pos, parents, (out, lse, status, workspace), buffers, max_len, pos0, want_lse, rope_theta,
+//           softmax_scale) -> (result code, dict of out, lse, status, workspace), or the reason of a refusal.  max_len = ALL: as many as the table holds.
+PyObject* tree_attn(PyObject*, PyObject* args) {
+  HANDLE_TH_ERRORS
+  unsigned long long ws_bytes, run, stream;
+  int cuda, want_lse;
+  long long max_len, pos0;
+  double theta, scale;
+  PyObject *pq, *dict, *table, *lens, *pos, *parents, *given[4], *buffers;
+  if (!PyArg_ParseTuple(args, "KKKpOOOOOO(OOOO)OLLpdd", &ws_bytes, &run, &stream, &cuda, &pq, &dict, &table, &lens, &pos, &parents, &given[0], &given[1],
+                        &given[2], &given[3], &buffers, &max_len, &pos0, &want_lse, &theta, &scale))
+    return nullptr;
+  return refusing([&]() -> PyObject* {
+    const char* const bad_q = "q must be bfloat16 [B, w, Hq, d] with the d of the pages and a contiguous head dimension";
+    const Cache c(dict);
+    at::Tensor q, t;
+    need(is_tensor(pq, q, bad_q) && q.dim() == 4 && q.size(3) == c.c.d, bad_q);
+    if (cuda) need_current(q.device());
+    need(c.device == q.device(), "the pages and the queries must be on one device");
+    const int64_t B = q.size(0), w = q.size(1), Hq = q.size(2);
+    need(B <= INT32_MAX && w <= INT32_MAX && Hq <= INT32_MAX, bad_q);
+    pc_tree_attn_args a = {};
+    a.B = (int32_t)B; a.w = (int32_t)w; a.Hq = (int32_t)Hq;
+    a.q = rows_of(q, q.sizes(), c.device, a.q_stride, bad_q);
+    a.pages = &c.c;
+    const char* const bad_table = "table must be int32 [B, pages of a sequence] with a contiguous last dimension, on the queries' device";
+    need(is_tensor(table, t, bad_table) && t.dim() == 2, bad_table);
+    a.table = table_of(table, B, -1, c.device, a.table_stride, bad_table);
+    a.n_table = (int32_t)t.size(1);
+    const char* const bad_lens = "lens must be a contiguous int32 tensor with one entry per sequence";
+    a.lens = per_sequence(lens, B, c.device, bad_lens);
+    need(a.lens != nullptr, bad_lens);
+    a.pos = per_sequence(pos, B, c.device, "pos must be a contiguous int32 tensor with one entry per sequence");
+    const char* const bad_parents = "parents must be int32 [B, w] or [w] with a contiguous last dimension, on the queries' device";
+    if (is_tensor(parents, t, bad_parents) && t.dim() == 1) {
+      need(t.size(0) == w && t.scalar_type() == at::kInt && t.device() == c.device && (t.stride(0) == 1 || w == 1), bad_parents);
+      a.parents = static_cast<const int32_t*>(t.data_ptr());
     } else {
-      if (has_ws) let_go(t[3]);
-      t[3] = at::empty({(int64_t)std::max<size_t>(bytes, 16)}, at::TensorOptions().dtype(at::kByte).device(device));
+      a.parents = table_of(parents, B, w, c.device, a.parents_stride, bad_parents);
     }
-    a.out = t[0].data_ptr();
-    a.lse = t[1].defined() ? static_cast<float*>(t[1].data_ptr()) : nullptr;
-    a.status_word = static_cast<int32_t*>(t[2].data_ptr());
-    a.workspace = t[3].data_ptr();
-    a.workspace_bytes = (size_t)t[3].numel();
-    const int32_t rc = entry<int32_t (*)(const pc_cache_attn_args*, void*)>(run)(&a, entry<void*>(stream));
-    PyObject* const result = PyDict_New();
-    if (result == nullptr) return nullptr;
-    for (int i = 0; i < 4; ++i) {
-      PyObject* const x = same[i] ? (Py_INCREF(same[i]), same[i]) : t[i].defined() ? THPVariable_Wrap(t[i]) : (Py_INCREF(Py_None), Py_None);
-      const bool ok = x != nullptr && PyDict_SetItemString(result, names[i], x) == 0 &&
-                      (rc != PC_OK || !keeps || !t[i].defined() || serves[i] || PyDict_SetItemString(buffers, names[i], x) == 0);
-      Py_XDECREF(x);
-      if (!ok) { Py_DECREF(result); return nullptr; }
+    const long long room = c.c.capacity * a.n_table - w;             // entries that a sequence can have before its new tokens
+    need(room >= 0, "the table has no room for the new tokens");
+    need(max_len == ALL || (max_len >= 0 && max_len <= room), "max_len is negative or more than the table holds beside the new tokens");
+    const long long most = max_len == ALL ? room : max_len;
+    need(most <= INT32_MAX, "a table of more entries than can be counted");
+    need(pos0 >= INT32_MIN && pos0 <= INT32_MAX, "pos0 must be a number of 32 bits");
+    a.max_len = (int32_t)most; a.pos0 = (int32_t)pos0;
+    a.rope_theta = (float)theta; a.softmax_scale = (float)scale;
+    AttnOut o(c.device, given, buffers, want_lse != 0, B, w, Hq, c.c.d);
+    a.clear_status = o.clear_status;
+    o.workspace(entry<size_t (*)(const pc_tree_attn_args*)>(ws_bytes)(&a));
+    o.put(a);
+    return o.result(entry<int32_t (*)(const pc_tree_attn_args*, void*)>(run)(&a, entry<void*>(stream)));
+  });
+  END_HANDLE_TH_ERRORS
+}
+
+// token_logprobs(run, stream, need_cuda, logits, tokens or None, top, group, want_entropy, scale) -> (result code, dict of logprob, entropy, top_id, top_logprob,
+// nll), or the reason of a refusal
+PyObject* token_logprobs(PyObject*, PyObject* args) {
+  HANDLE_TH_ERRORS
+  unsigned long long run, stream;
+  int cuda, want_entropy;
+  long long top, group;
+  double scale;
+  PyObject *pl, *pt;
+  if (!PyArg_ParseTuple(args, "KKpOOLLpd", &run, &stream, &cuda, &pl, &pt, &top, &group, &want_entropy, &scale)) return nullptr;
+  return refusing([&]() -> PyObject* {
+    const char* const bad = "logits must be float32, bfloat16 or float16 [N, V] with a contiguous last dimension";
+    at::Tensor x, t;
+    need(is_tensor(pl, x, bad) && x.dim() == 2 && (x.stride(1) == 1 || x.size(1) == 1) && x.size(0) <= INT32_MAX && x.size(1) <= INT32_MAX, bad);
+    if (cuda) need_current(x.device());
+    pc_token_logprobs_args a = {};
+    const int64_t N = x.size(0);
+    if (x.scalar_type() == at::kFloat) a.type = PC_LOGITS_F32;
+    else if (x.scalar_type() == at::kBFloat16) a.type = PC_LOGITS_BF16;
+    else { need(x.scalar_type() == at::kHalf, bad); a.type = PC_LOGITS_F16; }
+    a.N = (int32_t)N; a.V = (int32_t)x.size(1);
+    a.stride = N > 1 ? x.stride(0) : 0;
+    a.logits = x.data_ptr();
+    a.tokens = per_sequence(pt, N, x.device(), "tokens must be a contiguous int32 tensor with one entry per row");
+    need(top >= 0 && top <= PC_MOST_ALTERNATIVES && top <= x.size(1), "top must be between 0 and 32 and no more than the logits of a row");
+    need(group >= 0 && (group == 0 || (a.tokens != nullptr && N % group == 0)), "group must divide the rows, and needs tokens");
+    a.top = (int32_t)top; a.group = (int32_t)group; a.scale = (float)scale;
+    at::Tensor o[5];
+    const auto f32 = at::TensorOptions().dtype(at::kFloat).device(x.device());
+    if (a.tokens) { o[0] = at::empty({N}, f32); a.logprob = static_cast<float*>(o[0].data_ptr()); }
+    if (want_entropy) { o[1] = at::empty({N}, f32); a.entropy = static_cast<float*>(o[1].data_ptr()); }
+    if (top) {
+      o[2] = at::empty({N, (int64_t)top}, f32.dtype(at::kInt));
+      o[3] = at::empty({N, (int64_t)top}, f32);
+      a.top_id = static_cast<int32_t*>(o[2].data_ptr());
+      a.top_logprob = static_cast<float*>(o[3].data_ptr());
     }
-    return Py_BuildValue("iN", (int)rc, result);
+    if (group) { o[4] = at::empty({N / group}, f32); a.nll = static_cast<float*>(o[4].data_ptr()); }
+    const int32_t rc = entry<int32_t (*)(const pc_token_logprobs_args*, void*)>(run)(&a, entry<void*>(stream));
+    static const char* const names[5] = {"logprob", "entropy", "top_id", "top_logprob", "nll"};
+    PyObject* const r = PyDict_New();
+    if (r == nullptr) return nullptr;
+    for (int i = 0; i < 5; ++i) {
+      PyObject* const y = o[i].defined() ? THPVariable_Wrap(o[i]) : (Py_INCREF(Py_None), Py_None);
+      const bool ok = y != nullptr && PyDict_SetItemString(r, names[i], y) == 0;
+      Py_XDECREF(y);
+      if (!ok) { Py_DECREF(r); return nullptr; }
+    }
+    return Py_BuildValue("iN", (int)rc, r);
   });
   END_HANDLE_TH_ERRORS
 }
@@ -484,6 +682,9 @@ PyMethodDef methods[] = {{"hot_path", hot_path, METH_VARARGS, "See binding.py."}
                          {"gather_kv_quantize", gather_kv_quantize, METH_VARARGS, "See binding.py."},
                          {"kv_dequantize", kv_dequantize, METH_VARARGS, "See binding.py."},
                          {"cache_attn", cache_attn, METH_VARARGS, "See binding.py."},
+                         {"page_append", page_append, METH_VARARGS, "See binding.py."},
+                         {"tree_attn", tree_attn, METH_VARARGS, "See binding.py."},
+                         {"token_logprobs", token_logprobs, METH_VARARGS, "See binding.py."},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_pc_host", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

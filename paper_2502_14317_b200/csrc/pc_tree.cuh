@@ -1,0 +1,62 @@
+// What the kernels on paged caches and drafted tokens share: positions' angles, places of entries, who sees whom.
+#pragma once
+#include "pc_sm100.cuh"
+#include "pc_tree.h"
+
+namespace pc {
+
+// (cos, sin) of the angle of position p.  p times the fp64 part of a turn is off by 2^-53 of itself, and what is left of it without whole turns
+// goes to fp32: off by 2^-25 of a turn, whatever the position.  Three fp64 operations; sine and cosine are fp32's.
+__device__ __forceinline__ float2 turned(double per, long long p) {
+  const double x = per * (double)p;
+  const float f = (float)(x - rint(x));
+  float2 r;
+  sincospif(2.0f * f, &r.y, &r.x);
+  return r;
+}
+
+__device__ __forceinline__ int page_of(const Pages& p, int e) { return (int)((unsigned long long)(unsigned)e * p.mul >> p.shift); }
+
+// Who sees whom among the w <= 64 tokens of a sequence: lane l holds the tokens l and l + 32, bit j of a token's word: it sees token j (itself
+// among them); 0: it is not there.  A parent in [0, token) or -1 (the context's end) is one; anything else, -2 by custom, says that the
+// token is not there, and so are its descendants.  Every lane jumps to its ancestors in steps that double: log2(w) rounds.  The whole warp calls.
+struct Seen {
+  unsigned long long a, b;
+  __device__ __forceinline__ unsigned long long of(int token) const {
+    const unsigned long long x = __shfl_sync(0xFFFFFFFFu, a, token & 31), y = __shfl_sync(0xFFFFFFFFu, b, token & 31);
+    return token < 32 ? x : y;
+  }
+};
+__device__ __forceinline__ Seen tree_seen(const int* parents, int w, int lane) {
+  Seen s;
+  if (parents == nullptr) {
+    s.a = lane < w ? (2ull << lane) - 1 : 0;
+    s.b = lane + 32 < w ? (lane == 31 ? ~0ull : (2ull << (lane + 32)) - 1) : 0;
+    return s;
+  }
+  auto first = [&](int i) {
+    const int p = i < w ? __ldg(parents + i) : -2;
+    return p < -1 || p >= i ? -2 : p;
+  };
+  int ja = first(lane), jb = first(lane + 32);
+  s.a = 1ull << lane;
+  s.b = 1ull << (lane + 32);
+  for (int reach = 1; reach < w; reach *= 2) {
+    auto jump = [&](int j, unsigned long long& bits) {
+      const int from = j < 0 ? 0 : j;
+      const unsigned long long got = s.of(from);
+      const int x = __shfl_sync(0xFFFFFFFFu, ja, from & 31), y = __shfl_sync(0xFFFFFFFFu, jb, from & 31);
+      if (j < 0) return j;
+      bits |= got;
+      return from < 32 ? x : y;
+    };
+    unsigned long long na = s.a, nb = s.b;
+    const int ka = jump(ja, na), kb = w > 32 ? jump(jb, nb) : jb;
+    s.a = na; s.b = nb; ja = ka; jb = kb;
+  }
+  if (ja != -1) s.a = 0;
+  if (jb != -1) s.b = 0;
+  return s;
+}
+
+}  // namespace pc
