@@ -12,7 +12,8 @@ LIB_PATH = os.path.join(HERE, "libpc.so")
 HOST_SOURCE = "pc_host.cpp"
 SOURCES = ["pc_api.cu", "pc_prefill2.cu", "pc_parallel.cu", "pc_decode.cu", "pc_rope.cu", "pc_select_gather.cu", "pc_queue.cu", "pc_static_scratch.cu",
            "pc_cache_api.cu", "pc_cache_few.cu", "pc_cache_merge.cu", "pc_cache_wide.cu", "pc_kv_quant.cu",
-           "pc_logprob.cu", "pc_page_append.cu", "pc_tree_api.cu", "pc_tree_few.cu", "pc_tree_prepare.cu"]
+           "pc_logprob.cu", "pc_page_append.cu", "pc_tree_api.cu", "pc_tree_few.cu", "pc_tree_prepare.cu",
+           "pc_tree_wide.cu"]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
     "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--expt-relaxed-constexpr",

@@ -27,21 +27,7 @@ __global__ void __launch_bounds__(256) cache_rows_kernel(const CacheRows p) {
     turner.row(p, false, hkv, row, lane, x);
     const size_t at = (size_t)hkv * p.B * p.w * G + row;
     RowTurner<D>::store(p.rows, at, lane, x);
-    if (p.part_ml != nullptr)
-      for (int s = lane; s < p.n_slots; s += 32) p.part_ml[at * p.n_slots + s] = make_float2(-INFINITY, 0.0f);
-    if (p.halves == nullptr) return;
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < E / 2; ++i) m = __vmaxu2(m, x[i] & 0x7FFF7FFFu);
-    float inv;
-    const float f = row_factor(__reduce_max_sync(0xFFFFFFFFu, max(m & 0xFFFFu, m >> 16)), inv);
-#pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
-      const __half2 z = __floats2half2_rn(__uint_as_float(x[i] << 16) * f, __uint_as_float(x[i] & 0xFFFF0000u) * f);
-      x[i] = *reinterpret_cast<const uint32_t*>(&z);
-    }
-    RowTurner<D>::store(p.halves, at, lane, x);
-    if (lane == 0) p.half_scale[at] = p.scale_log2 * inv;
+    leave_beside<D>(p, at, lane, x);
   }
 }
 

@@ -5,6 +5,7 @@
 // computed in fp64.  A caller who wants the fp64 rotation everywhere, as the keys of this library have it, rotates the queries and gives theta 0.
 #pragma once
 #include "pc_cache.h"
+#include "pc_kv8.cuh"
 #include "pc_sm100.cuh"
 
 namespace pc {
@@ -85,5 +86,25 @@ struct RowTurner {
     else reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(rows) + at * D)[lane] = x[0];
   }
 };
+
+// What a launch for the rows leaves beside row `at`: its slots, marked as empty, and the row as halves (for 8-bit codes).
+template <int D>
+__device__ __forceinline__ void leave_beside(const CacheRows& p, size_t at, int lane, uint32_t (&x)[D / 64]) {
+  if (p.part_ml != nullptr)
+    for (int s = lane; s < p.n_slots; s += 32) p.part_ml[at * p.n_slots + s] = make_float2(-INFINITY, 0.0f);
+  if (p.halves == nullptr) return;
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) m = __vmaxu2(m, x[i] & 0x7FFF7FFFu);
+  float inv;
+  const float f = row_factor(__reduce_max_sync(0xFFFFFFFFu, max(m & 0xFFFFu, m >> 16)), inv);
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const __half2 z = __floats2half2_rn(__uint_as_float(x[i] << 16) * f, __uint_as_float(x[i] & 0xFFFF0000u) * f);
+    x[i] = *reinterpret_cast<const uint32_t*>(&z);
+  }
+  RowTurner<D>::store(p.halves, at, lane, x);
+  if (lane == 0) p.half_scale[at] = p.scale_log2 * inv;
+}
 
 }  // namespace pc

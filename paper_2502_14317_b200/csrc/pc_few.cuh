@@ -86,6 +86,9 @@ __device__ __forceinline__ float max_over_keys(float x) {
 __device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, bool there) {      // zero where there is no entry
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const float* src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {                             // once this thread's copies have landed
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
@@ -156,30 +159,47 @@ __device__ __forceinline__ void few_body(const CUtensorMap& tm_k, const CUtensor
     j0 = (int)((long long)n_all * split / prm.n_split);
     nt = (int)((long long)n_all * (split + 1) / prm.n_split) - j0;
   };
-  // TREE: a lane of the producer warp has a box of a tile, of `box` entries of the keys or the values, and looks up its page a tile ahead.
-  [[maybe_unused]] int page_id = 0, page_in = 0;
-  [[maybe_unused]] auto look_up = [&](int i) {
-    if constexpr (C::TREE) {
-      const int per = KEYS / tr.box, e = (j0 + i) * KEYS + lane % per * tr.box;
-      if (lane >= 2 * C::BOXES * per || e >= n) return;
-      const int which = page_of(tr.pages, e);
-      page_in = e - which * tr.pages.page;
-      page_id = page_checked(tr.pages, __ldg(tr.pages.table + seq * tr.pages.stride + which), prm.status);
+  // TREE: a lane of the producer warp has a box of a tile's copies: which of the keys' or the values', or none (KEYS)
+  [[maybe_unused]] int lane_box = C::KEYS, lane_values = 0, lane_col = 0, lane_to = 0;
+  if constexpr (C::TREE) {
+    const int part = lane * (1 << tr.log_box) / KEYS;            // columns of the keys, columns of the values
+    if (part < 2 * C::BOXES) {
+      lane_box = lane - part * (KEYS >> tr.log_box);
+      lane_values = part / C::BOXES;
+      lane_col = part % C::BOXES * C::EPB;
+      lane_to = lane_values * C::HALF_BYTES + (part % C::BOXES * KEYS + (lane_box << tr.log_box)) * C::BOXB;
     }
+  }
+  // pages of the table, 64 at a time in the producer warp's registers, the second half on its way while the first is used
+  [[maybe_unused]] int ids = -1, ids_next = -1, ids_first = 0;
+  [[maybe_unused]] auto ids_at = [&](int first) {
+    if constexpr (C::TREE) {
+      const int which = first + lane;
+      return n > 0 && which <= page_of(tr.pages, n - 1) ? __ldg(tr.pages.table + seq * tr.pages.stride + which) : -1;
+    }
+    return -1;
+  };
+  [[maybe_unused]] auto id_of = [&](int which) {                // of a page of the present tile; the whole warp calls
+    const int at = which - ids_first, x = __shfl_sync(0xFFFFFFFFu, ids, at & 31), y = __shfl_sync(0xFFFFFFFFu, ids_next, at & 31);
+    return at < 32 ? x : y;
   };
   // copies of tile i into its stage; the whole producer warp calls
   auto load = [&](int i) {
     const int st = i % NS, key = (j0 + i) * KEYS;
     if constexpr (C::TREE) {
-      const int per = KEYS / tr.box, some = (n - key + tr.box - 1) / tr.box, boxes = some < per ? some : per;     // boxes with entries
-      if (lane == 0) mbar_arrive_expect_tx(&mi.full[st], 2 * boxes * tr.box * C::ROWB);
-      __syncwarp();
-      const int part = lane / per, j = lane % per;
-      if (part < 2 * C::BOXES && j < boxes) {
-        const int values = part / C::BOXES, b = part % C::BOXES;
-        tma_load_4d(smem + st * C::STAGE_BYTES + values * C::HALF_BYTES + (b * KEYS + j * tr.box) * C::BOXB, values ? &tm_v : &tm_k, &mi.full[st], b * C::EPB,
-                    page_in, hkv, page_id);
+      const int box = 1 << tr.log_box, some = (n - key + box - 1) >> tr.log_box, boxes = some < KEYS >> tr.log_box ? some : KEYS >> tr.log_box;   // with entries
+      const int first = page_of(tr.pages, key);
+      if (first - ids_first >= 32) {
+        ids_first += 32;
+        ids = ids_next;
+        ids_next = ids_at(ids_first + 32);
       }
+      const int e = key + (lane_box << tr.log_box), which = lane_box < boxes ? page_of(tr.pages, e) : first, id = id_of(which);
+      if (lane == 0) mbar_arrive_expect_tx(&mi.full[st], 2 * C::ROWB * boxes << tr.log_box);
+      __syncwarp();
+      if (lane_box < boxes)
+        tma_load_4d(smem + st * C::STAGE_BYTES + lane_to, lane_values ? &tm_v : &tm_k, &mi.full[st], lane_col, e - which * tr.pages.page, hkv,
+                    page_checked(tr.pages, id, prm.status));
     } else if (lane == 0) {
       mbar_arrive_expect_tx(&mi.full[st], C::STAGE_BYTES);
 #pragma unroll
@@ -189,8 +209,22 @@ __device__ __forceinline__ void few_body(const CUtensorMap& tm_k, const CUtensor
       }
     }
     if constexpr (Q8) {
-      const size_t at = ((size_t)seq * prm.Hkv + hkv) * prm.capacity;
       const uint32_t dst = smem_u32(smem + C::OFF_SCALE) + st * (2 * KEYS * 4);
+      if constexpr (C::TREE) {
+        if (tr.scales_by_four) {                                 // (four entries lie in one page)
+          const int e = key + 4 * lane, which = page_of(tr.pages, e < n ? e : key), id = id_of(which);
+          const bool there = e < n && id >= 0 && id < tr.pages.n_pages;
+          if (4 * lane < KEYS) {
+            const size_t from = there ? ((size_t)id * prm.Hkv + hkv) * tr.pages.page + (e - which * tr.pages.page) : 0;
+            cp_async16(dst + lane * 16, prm.k_scale + from, there);
+            cp_async16(dst + KEYS * 4 + lane * 16, prm.v_scale + from, there);
+          }
+          cp_async_arrive(&mi.full[st]);
+          __syncwarp();
+          return;
+        }
+      }
+      const size_t at = ((size_t)seq * prm.Hkv + hkv) * prm.capacity;
       for (int k = lane; k < KEYS; k += 32) {
         bool there = key + k < n;
         size_t e = at + (there ? key + k : 0);
@@ -205,12 +239,15 @@ __device__ __forceinline__ void few_body(const CUtensorMap& tm_k, const CUtensor
       cp_async_arrive(&mi.full[st]);
     }
     __syncwarp();
-    look_up(i + 1);
   };
 
   if (warp == C::WARPS) {
     share();
-    look_up(0);
+    if constexpr (C::TREE) {
+      ids_first = page_of(tr.pages, j0 * KEYS);
+      ids = ids_at(ids_first);
+      ids_next = ids_at(ids_first + 32);
+    }
     for (int i = 0; i < NS && i < nt; ++i) load(i);
   } else {
     // ---- the rows' queries: as they are, and as operands in the order in which the threads hold their keys
@@ -560,7 +597,11 @@ __device__ __forceinline__ void few_body(const CUtensorMap& tm_k, const CUtensor
     bool none = sum == 0.0f || (C::CAUSAL && mi.odd);
     if constexpr (C::TREE) {
       none |= tm.sees[r] == 0;
-      if (tm.odd & tm.sees[r]) add_odd<D, FMT>(tr, prm, hkv, seq, entries, tm.odd & tm.sees[r], 4 * c, o);
+      if (tm.odd & tm.sees[r]) {
+        float x[4] = {o.x, o.y, o.z, o.w};
+        add_odd<D, FMT, 4>(tr, prm, hkv, seq, entries, tm.odd & tm.sees[r], 4 * c, x);
+        o = make_float4(x[0], x[1], x[2], x[3]);
+      }
     }
     const float2 ml = none ? make_float2(-INFINITY, 0.0f) : make_float2(top, sum);
     if (finish) {

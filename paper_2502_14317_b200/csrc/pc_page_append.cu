@@ -43,9 +43,12 @@ __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float 
 // grid: (tokens of a sequence in blocks, heads in fours, sequences)
 template <int D, int FMT>
 __global__ void __launch_bounds__(NT) page_append_kernel(const __grid_constant__ PageWrite p) {
-  chain();
   constexpr int LANES = D / 8, GROUPS = NT / LANES;
   const int lane = threadIdx.x % LANES, h0 = blockIdx.y * HEADS;
+  double part[4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) part[t] = part_of_turn(p.turns, 4 * lane + t);
+  chain();
   for (int b = blockIdx.z; b < p.B; b += gridDim.z) {
     const long long at = (long long)p.at0 + (p.at ? __ldg(p.at + b) : 0);
     if (at < 0) continue;                                      // no such sequence
@@ -100,7 +103,7 @@ __global__ void __launch_bounds__(NT) page_append_kernel(const __grid_constant__
     float2 cs[4];
     if (p.turn) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) cs[t] = turned(p.turns.per[4 * lane + t], pos + step);
+      for (int t = 0; t < 4; ++t) cs[t] = turned(part[t], pos + step);
     }
 #pragma unroll
     for (int u = 0; u < HEADS; ++u) {

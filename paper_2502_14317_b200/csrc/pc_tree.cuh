@@ -5,6 +5,16 @@
 
 namespace pc {
 
+// Part of a turn of pair t.  Every lane has another pair, and the constant cache serves one address at a time: sixteen uniform loads and choices.
+__device__ __forceinline__ double part_of_turn(const Turns& u, int t) {
+  double c = u.coarse[0], f = u.fine[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) {
+    if (t / 8 == i) c = u.coarse[i];
+    if (t % 8 == i) f = u.fine[i];
+  }
+  return c * f;
+}
 // (cos, sin) of the angle of position p.  p times the fp64 part of a turn is off by 2^-53 of itself, and what is left of it without whole turns
 // goes to fp32: off by 2^-25 of a turn, whatever the position.  Three fp64 operations; sine and cosine are fp32's.
 __device__ __forceinline__ float2 turned(double per, long long p) {

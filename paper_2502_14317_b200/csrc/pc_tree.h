@@ -4,8 +4,8 @@
 
 namespace pc {
 
-// Positions turn pair t by theta^(-2t/d) / (2 pi) of a full turn each; the host computes these in fp64.
-struct Turns { double per[64]; };
+// A position turns pair t by theta^(-2t/d) / (2 pi) = coarse[t / 8] * fine[t % 8] of a full turn; the host computes these in fp64.
+struct Turns { double coarse[8], fine[8]; };
 
 // Pages of the sequences: entry e of sequence b is entry e % page of page table[b * stride + e / page].
 struct Pages {
@@ -40,15 +40,18 @@ struct TreePhase {
   const int* parents;                            // [B,w] through a stride, or null: each token the child of the one before
   long long parent_stride;
   int max_len;                                   // of lens
-  int box;                                       // entries of a tensor map's box: a divisor of a page, unless a sequence has one page
+  int log_box;                                   // of the entries of a tensor map's box: a divisor of a page; of a page that has no multiple of 16 entries a tile
+  int scales_by_four;                           // 8-bit formats: four scales of a page are 16 bytes at a multiple of 16
   int turn;                                      // 0: queries as they are
   Turns turns;
   const uint8_t *k, *v;                          // the pool
   unsigned long long* sees;                      // [B,w], written by the launch for the rows: bit j: token j is seen; 0: the token is not there
 };
-// The kernel for few rows (pc_tree_few.cu): as launch_cache_few(), p.len the entries before the new tokens, maps of the pool with boxes of t.box entries.
+// The kernel for few rows (pc_tree_few.cu): as launch_cache_few(), p.len the entries before the new tokens, maps of the pool with boxes of 2^t.log_box entries.
 cudaError_t launch_tree_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, const CachePhase& p, const TreePhase& t, const CacheMerge* finish, int group,
                             bool brief, int format, int d, cudaStream_t st);
+// The kernel for many rows (pc_tree_wide.cu): as launch_cache_wide() on single CTAs.
+cudaError_t launch_tree_wide(const CUtensorMap* maps, const WidePhase& p, const TreePhase& t, int format, int d, int sm_count, cudaStream_t st);
 // Rows into memory, rotated, and t.sees; clears as cache_rows_kernel does (pc_tree_prepare.cu).
 cudaError_t launch_tree_rows(const CacheRows& p, const TreePhase& t, int d, cudaStream_t st);
 

@@ -28,14 +28,12 @@ pc::Pages pages_of(const pc_kv_cache* c, const int32_t* table, int64_t stride, i
   return p;
 }
 
-// theta^(-2t/d) / (2 pi): the product of two powers is off by some 2^-51 of itself, and sixteen of them make all
+// theta^(-2t/d) / (2 pi) as products of two: off by some 2^-51 of themselves, and sixteen powers make all
 void turns_of(float theta, int d, pc::Turns& out) {
   const double step = -2.0 / d, turn = 0.15915494309189535;
-  double fine[8];
-  for (int t = 0; t < 8; ++t) fine[t] = std::pow((double)theta, step * t);
-  for (int t = 0; t < d / 2; t += 8) {
-    const double coarse = std::pow((double)theta, step * t) * turn;
-    for (int i = 0; i < 8; ++i) out.per[t + i] = coarse * fine[i];
+  for (int i = 0; i < 8; ++i) {
+    out.fine[i] = std::pow((double)theta, step * i);
+    out.coarse[i] = std::pow((double)theta, step * 8 * i) * turn;
   }
 }
 bool good_theta(float theta) { return theta >= 0.0f && std::isfinite(theta); }
@@ -78,8 +76,8 @@ struct TreePlan {
   PhasePlan phase;
   int n_slots;                                   // results of a row in memory
   int64_t total_rows;
-  bool rows;                                     // a launch for the rows
-  size_t off_counter, off_sees, off_rows, off_ml, off_o, total;
+  bool rows, halves;                             // a launch for the rows; as halves as well (many rows over 8-bit codes)
+  size_t off_counter, off_sees, off_halves, off_scale, off_rows, off_ml, off_o, total;
 };
 
 int32_t tree_plan(const pc_tree_attn_args* a, int sm_count, TreePlan& p) {
@@ -90,14 +88,24 @@ int32_t tree_plan(const pc_tree_attn_args* a, int sm_count, TreePlan& p) {
   if (a->w > MOST_DRAFTED || a->Hq > (1 << 18) || (int64_t)a->B * a->w * a->Hq > (1 << 24) || a->max_len > MOST_OF_A_SEQUENCE) return PC_ERR_UNSUPPORTED;
   const int G = a->Hq / c->Hkv;
   p.total_rows = (int64_t)a->B * a->w * G;
-  p.phase = few_plan(a->B, (int64_t)a->w * G, c->Hkv, c->d, c->format, a->max_len + a->w, true, sm_count);
+  const int64_t rows = (int64_t)a->w * G;
+  const bool bf16 = c->format == PC_KV_BF16;
+  p.halves = false;
+  if (rows > (!bf16 ? 48 : c->d == 128 || (double)a->B * c->Hkv > 2.0 * sm_count ? 16 : 32)) {
+    p.phase = wide_plan(a->B, rows, c->Hkv, c->d, a->max_len + a->w, sm_count, false);
+    p.halves = !bf16;
+  } else {
+    p.phase = few_plan(a->B, rows, c->Hkv, c->d, c->format, a->max_len + a->w, true, sm_count);
+  }
   if ((int64_t)a->B * c->Hkv * p.phase.n_rg * p.phase.n_split > 0x7FFF0000) return PC_ERR_UNSUPPORTED;
   p.n_slots = p.phase.finish ? 0 : p.phase.n_split;
   // more than a round of CTAs: cheaper than each of them rotating its own (as in pc_cache_attn)
-  p.rows = (double)a->B * c->Hkv * p.phase.n_rg * p.phase.n_split > (p.phase.brief ? p.phase.group == 8 ? 4.0 : 3.0 : 2.0) * sm_count;
+  p.rows = p.phase.wide || (double)a->B * c->Hkv * p.phase.n_rg * p.phase.n_split > (p.phase.brief ? p.phase.group == 8 ? 4.0 : 3.0 : 2.0) * sm_count;
   size_t off = 0;
   p.off_counter = off; off += ALIGN;
   p.off_sees = off; off += align_up((size_t)a->B * a->w * 8);
+  p.off_halves = off; off += p.halves ? align_up((size_t)p.total_rows * c->Hkv * c->d * 2) : 0;
+  p.off_scale = off; off += p.halves ? align_up((size_t)p.total_rows * c->Hkv * sizeof(float)) : 0;
   p.off_rows = off; off += align_up((size_t)p.total_rows * c->Hkv * c->d * 2);
   p.off_ml = off; off += align_up((size_t)p.total_rows * c->Hkv * p.n_slots * sizeof(float2));
   p.off_o = off; off += align_up((size_t)p.total_rows * c->Hkv * p.n_slots * c->d * sizeof(float));
@@ -113,9 +121,9 @@ bool page_maps(const pc_kv_cache* c, int rows, CUtensorMap* tm_k, CUtensorMap* t
   if (c->format == PC_KV_BF16) return pc::make_tmap_bf16_4d(tm_k, c->k, dims, str, box) && pc::make_tmap_bf16_4d(tm_v, c->v, dims, str, box);
   return pc::make_tmap_u8_4d(tm_k, c->k, dims, str, box) && pc::make_tmap_u8_4d(tm_v, c->v, dims, str, box);
 }
-// entries of a box of copies: the largest power of two that divides a page, up to a tile; of sequences of one page a tile
-int box_of(int64_t page, int n_table, int tile) {
-  if (n_table == 1) return tile;
+// entries of a box of copies: the largest power of two that divides a page, up to a tile; of pages that have no multiple of 16, one for each sequence, a tile
+int box_of(int64_t page, int tile) {
+  if (page % 16 != 0) return tile;
   int box = 16;
   while (box < tile && page % (2 * box) == 0) box *= 2;
   return box;
@@ -166,6 +174,8 @@ int32_t pc_tree_attn(const pc_tree_attn_args* a, void* stream) {
   if (plan.rows) {
     rows.clear = reinterpret_cast<int*>(ws + plan.off_counter);
     rows.clear_too = a->clear_status ? a->status_word : nullptr;
+    if (ph.wide) { rows.part_ml = reinterpret_cast<float2*>(ws + plan.off_ml); rows.n_slots = plan.n_slots; }      // (items without keys are left out)
+    if (plan.halves) { rows.halves = ws + plan.off_halves; rows.half_scale = reinterpret_cast<float*>(ws + plan.off_scale); }
     e = pc::launch_tree_rows(rows, tree, c->d, st);
   } else if (a->clear_status && a->status_word) {
     e = cudaMemsetAsync(a->status_word, 0, sizeof(int), st);
@@ -189,11 +199,25 @@ int32_t pc_tree_attn(const pc_tree_attn_args* a, void* stream) {
   p.status = a->status_word;
   p.wait_kcycles = pc::wait_limit_kcycles();
   p.skip_final_publication = pc::skip_final_publication();
-  CUtensorMap tm_k, tm_v;
+  CUtensorMap maps[3];
   if (e == cudaSuccess) {
-    tree.box = box_of(c->capacity, a->n_table, pc::few_keys(c->format, c->d, ph.brief));
-    if (!page_maps(c, tree.box, &tm_k, &tm_v)) { launched(e); return PC_ERR_CUDA; }
-    e = pc::launch_tree_few(tm_k, tm_v, p, tree, ph.finish ? &merge : nullptr, ph.group, ph.brief, c->format, c->d, st);
+    const int box = box_of(c->capacity, ph.wide ? 128 : pc::few_keys(c->format, c->d, ph.brief));
+    while ((1 << tree.log_box) < box) ++tree.log_box;
+    tree.scales_by_four = c->capacity % 16 == 0 && aligned(c->k_scale, 16) && aligned(c->v_scale, 16);
+    if (!page_maps(c, box, &maps[1], &maps[2])) { launched(e); return PC_ERR_CUDA; }
+    if (ph.wide) {
+      pc::WidePhase wp = {};
+      wp.c = p; wp.alt = ph.alt;
+      wp.half_scale = rows.half_scale;
+      wp.counter = rows.clear;
+      const uint64_t d = (uint64_t)c->d, R = (uint64_t)plan.total_rows;
+      const uint64_t dims[4] = {d, R, (uint64_t)c->Hkv, 1}, str[3] = {d, R * d, R * d * (uint64_t)c->Hkv};
+      const uint32_t row_box[4] = {64, 128, 1, 1};
+      if (!pc::make_tmap_bf16_4d(&maps[0], plan.halves ? rows.halves : rows.rows, dims, str, row_box)) { launched(e); return PC_ERR_CUDA; }
+      e = pc::launch_tree_wide(maps, wp, tree, c->format, c->d, sms, st);
+    } else {
+      e = pc::launch_tree_few(maps[1], maps[2], p, tree, ph.finish ? &merge : nullptr, ph.group, ph.brief, c->format, c->d, st);
+    }
   }
   if (e != cudaSuccess || ph.finish) return launched(e);
   return launched(pc::launch_cache_merge(merge, c->d, st));

@@ -22,7 +22,9 @@ __global__ void __launch_bounds__(256) tree_rows_kernel(const __grid_constant__ 
   uint32_t x[D / 64];
   turner.place(p, seq, __ldg(t.lens + seq), __popcll(sees));
   turner.row(p, false, hkv, row, lane, x);
-  TreeTurner<D>::store(p.rows, (size_t)hkv * p.B * p.w * G + row, lane, x);
+  const size_t at = (size_t)hkv * p.B * p.w * G + row;
+  TreeTurner<D>::store(p.rows, at, lane, x);
+  leave_beside<D>(p, at, lane, x);
 }
 
 cudaError_t launch_tree_rows(const CacheRows& p, const TreePhase& t, int d, cudaStream_t st) {

@@ -28,7 +28,7 @@ struct TreeTurner {
   bool turn;
   __device__ __forceinline__ TreeTurner(const TreePhase& t, int lane) : turn(t.turn != 0) {
 #pragma unroll
-    for (int k = 0; k < H; ++k) per[k] = t.turns.per[E * (lane & 15) + (lane >> 4) * H + k];
+    for (int k = 0; k < H; ++k) per[k] = part_of_turn(t.turns, E * (lane & 15) + (lane >> 4) * H + k);
   }
   // sequence, its entries before the new tokens, how many of these the row's token sees
   __device__ __forceinline__ void place(const CacheRows& p, int seq, int entries, int sees) {
@@ -91,32 +91,28 @@ __device__ __forceinline__ uint32_t finite_parts(uint32_t x) {
   return r;
 }
 
-// What the kernels have left out of a row's sum: values that are no number of the new tokens in `odd` that the row sees, columns col .. col + 3 of
-// kv-head hkv.  Their weight is positive, so that an infinity stays one.  Out of line: next to never.
-template <int D, int FMT>
-__device__ __noinline__ void add_odd_(const TreePhase& t, const float* v_scale, int Hkv, int hkv, int seq, int entries, unsigned long long odd, int col, float* o) {
+// What the kernels have left out of a row's sum: values that are no number of the new tokens in `odd` that the row sees, columns col .. col + N - 1 of
+// kv-head hkv.  Their weight is positive, so that an infinity stays one.  Next to never; not unrolled.
+template <int D, int FMT, int N>
+__device__ __forceinline__ void add_odd(const TreePhase& t, const CachePhase& p, int hkv, int seq, int entries, unsigned long long odd, int col, float* o) {
+#pragma unroll 1
   while (odd) {
     const int e = entries + __ffsll((long long)odd) - 1, which = page_of(t.pages, e), id = __ldg(t.pages.table + seq * t.pages.stride + which);
     odd &= odd - 1;
     if (id < 0 || id >= t.pages.n_pages) continue;
-    const size_t row = ((size_t)id * Hkv + hkv) * t.pages.page + (e - which * t.pages.page);
-    for (int i = 0; i < 4; ++i) {
+    const size_t row = ((size_t)id * p.Hkv + hkv) * t.pages.page + (e - which * t.pages.page);
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
       float x;
       if constexpr (FMT == FMT_BF16) {
         x = __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(t.v) + row * D + col + i) << 16);
       } else {
         const uint32_t h = codes_to_half2<FMT, 0>(flip_signs<FMT>(__ldg(t.v + row * D + col + i)));
-        x = __half2float(__ushort_as_half((unsigned short)(h & 0xFFFFu))) * __ldg(v_scale + row);
+        x = __half2float(__ushort_as_half((unsigned short)(h & 0xFFFFu))) * __ldg(p.v_scale + row);
       }
       if (!(fabsf(x) < INFINITY)) o[i] += x;
     }
   }
-}
-template <int D, int FMT>
-__device__ __forceinline__ void add_odd(const TreePhase& t, const CachePhase& p, int hkv, int seq, int entries, unsigned long long odd, int col, float4& o) {
-  float x[4] = {o.x, o.y, o.z, o.w};
-  add_odd_<D, FMT>(t, p.v_scale, p.Hkv, hkv, seq, entries, odd, col, x);
-  o = make_float4(x[0], x[1], x[2], x[3]);
 }
 
 }  // namespace pc
