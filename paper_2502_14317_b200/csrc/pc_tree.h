@@ -42,6 +42,7 @@ struct TreePhase {
   int max_len;                                   // of lens
   int log_box;                                   // of the entries of a tensor map's box: a divisor of a page; of a page that has no multiple of 16 entries a tile
   int scales_by_four;                           // 8-bit formats: four scales of a page are 16 bytes at a multiple of 16
+  int least_tiles;                               // many rows: of a piece of a sequence's keys
   int turn;                                      // 0: queries as they are
   Turns turns;
   const uint8_t *k, *v;                          // the pool

@@ -4,12 +4,15 @@
 #include "pc_tmap.h"
 #include "pc_tree.h"
 
+#include <algorithm>
+
 using namespace pc::plan;
 
 namespace {
 
 constexpr int64_t MOST_OF_A_SEQUENCE = 1 << 28;
 constexpr int MOST_DRAFTED = 64;
+constexpr int LEAST_TILES = 4;                   // of a piece of a sequence's keys, many rows: an item costs some two tiles beside its own
 
 // a pool of pages and the sequences' tables
 int32_t check_pages(const pc_kv_cache* c, const int32_t* table, int64_t stride, int32_t n_table) {
@@ -80,6 +83,52 @@ struct TreePlan {
   size_t off_counter, off_sees, off_halves, off_scale, off_rows, off_ml, off_o, total;
 };
 
+// Few rows: splits of the keys, as few_plan() but for sequences whose lengths may differ and whose copies go by pages.  Least time by a model in us: 7.5 for a CTA's
+// start and join; its tiles, at what a CTA takes for one alone on an SM or beside another, or at the memory's rate (of several sequences, whose lengths the host does not
+// see, as if they had 0.6 of the longest's); beyond a round of the GPU what all have to read, 2 to 4 a round and half of a longest piece for the end, where
+// only the longest sequences are left; slots 1.5 + 0.05 a split.
+PhasePlan tree_few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count, double& least) {
+  PhasePlan p = few_plan(seqs, rows, Hkv, d, format, n_keys, true, sm_count);
+  least = -1.0;
+  if (p.brief) return p;
+  const int keys = pc::few_keys(format, d, false), tiles = (n_keys + keys - 1) / keys;
+  const double items = (double)seqs * Hkv * p.n_rg, bytes = 2.0 * keys * (format == PC_KV_BF16 ? 2 * d : d + 4) / 6.5e6;        // of a tile, us
+  const double units = keys / 16 / (p.group == 8 || d == 64 ? 7.0 : 5.0) * (p.group == 8 ? 1.0 : 1.4);
+  const double alone = (format == PC_KV_BF16 ? 1.05 : 0.8) * units, beside = (format == PC_KV_BF16 ? 1.6 : 1.1) * units;
+  const double part = seqs > 1 ? 0.6 : 1.0, round_us = format == PC_KV_BF16 ? 2.0 : 4.0;
+  auto look = [&](int s, bool finish) {
+    const double fit = 2.0 * sm_count, ctas = items * s, per = std::ceil((double)tiles / s);
+    double t = 7.5 + (finish ? 0.0 : 1.5 + 0.05 * s);
+    if (ctas <= fit) {
+      const double tile = ctas <= sm_count ? alone : beside;
+      t += per * (tile > part * bytes * ctas ? tile : part * bytes * ctas);
+    } else {
+      const double tile = beside > bytes * fit ? beside : bytes * fit;
+      t += part * items * tiles * tile / fit + round_us * (ctas / fit - 1.0) + 0.5 * per * tile;
+    }
+    if (least < 0.0 || t < least) { least = t; p.n_split = s; p.finish = finish; }
+  };
+  for (int s = 1; s <= 64 && s <= tiles; ++s) {
+    if (s == 1 || (s <= 8 && items <= few_fit(s))) look(s, true);
+    look(s, false);
+  }
+  return p;
+}
+
+// Many rows: as wide_plan() on single CTAs; of several sequences, which may differ in length, pieces that are a small part of a CTA's work, drawn from the queue.
+PhasePlan tree_wide_plan(int64_t seqs, int64_t rows, int Hkv, int d, int n_keys, int sm_count) {
+  PhasePlan p = wide_plan(seqs, rows, Hkv, d, n_keys, sm_count, false);
+  if (seqs == 1) return p;
+  const double items = (double)seqs * Hkv * p.n_rg;
+  const int tiles = (n_keys + 127) / 128, most = (tiles + LEAST_TILES - 1) / LEAST_TILES, at_least = p.n_split;
+  double least = -1.0;
+  for (int s = std::min((int)std::ceil(4.0 * sm_count / items), most); s <= 1 + (int)std::ceil(8.0 * sm_count / items) && s <= most && s <= 64; ++s) {
+    const double t = std::ceil(items * s / sm_count) * (1.0 + std::ceil((double)tiles / s));            // rounds; an item takes a tile beside its own
+    if (s > at_least && (least < 0.0 || t < least)) { least = t; p.n_split = s; }
+  }
+  return p;
+}
+
 int32_t tree_plan(const pc_tree_attn_args* a, int sm_count, TreePlan& p) {
   if (a->B < 1 || a->w < 1 || a->Hq < 1 || a->max_len < 0) return PC_ERR_INVALID_ARG;
   if (int32_t rc = check_cache(a->pages, false); rc != PC_OK) return rc;
@@ -90,13 +139,17 @@ int32_t tree_plan(const pc_tree_attn_args* a, int sm_count, TreePlan& p) {
   p.total_rows = (int64_t)a->B * a->w * G;
   const int64_t rows = (int64_t)a->w * G;
   const bool bf16 = c->format == PC_KV_BF16;
-  p.halves = false;
-  if (rows > (!bf16 ? 48 : c->d == 128 || (double)a->B * c->Hkv > 2.0 * sm_count ? 16 : 32)) {
-    p.phase = wide_plan(a->B, rows, c->Hkv, c->d, a->max_len + a->w, sm_count, false);
-    p.halves = !bf16;
-  } else {
-    p.phase = few_plan(a->B, rows, c->Hkv, c->d, c->format, a->max_len + a->w, true, sm_count);
-  }
+  const int n_keys = a->max_len + a->w;
+  double few_us;
+  p.phase = tree_few_plan(a->B, rows, c->Hkv, c->d, c->format, n_keys, sm_count, few_us);
+  const PhasePlan many = tree_wide_plan(a->B, rows, c->Hkv, c->d, n_keys, sm_count);
+  // Many rows on the kernel for many where it takes less time: three launches and its start 15.5 us (head size 128: 17.5), a tile and CTA 1.75 to 2.4 us, over codes
+  // 2.9 to 5.7; by short CTAs as pc_cache_attn.
+  const double tile_us = bf16 ? (c->d == 64 ? 1.75 : 1.95) * (rows > 128 ? 1.25 : 1.0) : (c->d == 64 ? 2.9 : 4.2) * (rows > 128 ? 1.35 : 1.0);
+  const double wide_us = (c->d == 64 ? 15.5 : 17.5) + tile_us * std::ceil((a->B > 1 ? 0.6 : 1.0) * a->B * c->Hkv * many.n_rg * ((n_keys + 127) / 128) / sm_count);
+  bool wide = p.phase.brief ? rows > (!bf16 ? 48 : c->d == 128 || (double)a->B * c->Hkv > 2.0 * sm_count ? 16 : 32) : rows > 8 && wide_us < few_us;
+  if (wide) p.phase = many;
+  p.halves = wide && !bf16;
   if ((int64_t)a->B * c->Hkv * p.phase.n_rg * p.phase.n_split > 0x7FFF0000) return PC_ERR_UNSUPPORTED;
   p.n_slots = p.phase.finish ? 0 : p.phase.n_split;
   // more than a round of CTAs: cheaper than each of them rotating its own (as in pc_cache_attn)
@@ -166,6 +219,7 @@ int32_t pc_tree_attn(const pc_tree_attn_args* a, void* stream) {
   tree.pages = pages_of(c, a->table, a->table_stride, a->n_table);
   tree.lens = a->lens; tree.parents = a->parents; tree.parent_stride = a->parents_stride;
   tree.max_len = a->max_len;
+  tree.least_tiles = LEAST_TILES;
   tree.turn = a->rope_theta > 0.0f;
   if (tree.turn) turns_of(a->rope_theta, c->d, tree.turns);
   tree.k = static_cast<const uint8_t*>(c->k); tree.v = static_cast<const uint8_t*>(c->v);
@@ -220,7 +274,8 @@ int32_t pc_tree_attn(const pc_tree_attn_args* a, void* stream) {
     }
   }
   if (e != cudaSuccess || ph.finish) return launched(e);
-  return launched(pc::launch_cache_merge(merge, c->d, st));
+  // a warp for each row where there are enough of them to fill the GPU, else four
+  return launched(pc::launch_cache_merge(merge, c->d, st, plan.n_slots <= 4 || plan.total_rows * c->Hkv > 16 * sms));
 }
 
 int32_t pc_token_logprobs(const pc_token_logprobs_args* a, void* stream) {

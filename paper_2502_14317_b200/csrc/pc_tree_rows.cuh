@@ -18,6 +18,23 @@ __device__ __forceinline__ int page_checked(const Pages& p, int id, int* status)
   return p.n_pages;
 }
 
+// A row turned by the angles of its pairs: lane l has the elements E l .. E l + E - 1, lanes l and l + 16 those of the same pairs.
+template <int D>
+__device__ __forceinline__ void turn_row(uint32_t (&x)[D / 64], const float (&c)[D / 32], const float (&s)[D / 32], int lane) {
+#pragma unroll
+  for (int i = 0; i < D / 64; ++i) {
+    const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, x[i], 16);     // the other elements of the pairs
+    float z[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const float u = __uint_as_float(e ? x[i] & 0xFFFF0000u : x[i] << 16), v = __uint_as_float(e ? y & 0xFFFF0000u : y << 16);
+      const float sn = lane < 16 ? -s[2 * i + e] : s[2 * i + e];   // x cos - y sin, y cos + x sin
+      z[e] = fmaf(v, sn, u * c[2 * i + e]);
+    }
+    x[i] = pack_bf16x2(z[0], z[1]);
+  }
+}
+
 // Queries as rows, as RowTurner makes them, with the angles of pc_tree.cuh.  A warp has a row, a lane D / 32 elements.
 template <int D>
 struct TreeTurner {
@@ -60,18 +77,7 @@ struct TreeTurner {
         c[H + k] = lane < 16 ? b.x : a.x; s[H + k] = lane < 16 ? b.y : a.y;
       }
     }
-#pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
-      const uint32_t y = __shfl_xor_sync(0xFFFFFFFFu, x[i], 16);     // the other elements of the pairs
-      float z[2];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float u = __uint_as_float(e ? x[i] & 0xFFFF0000u : x[i] << 16), v = __uint_as_float(e ? y & 0xFFFF0000u : y << 16);
-        const float sn = lane < 16 ? -s[2 * i + e] : s[2 * i + e];   // x cos - y sin, y cos + x sin
-        z[e] = fmaf(v, sn, u * c[2 * i + e]);
-      }
-      x[i] = pack_bf16x2(z[0], z[1]);
-    }
+    turn_row<D>(x, c, s, lane);
   }
   static __device__ __forceinline__ void store(void* rows, size_t at, int lane, const uint32_t (&x)[E / 2]) { RowTurner<D>::store(rows, at, lane, x); }
 };

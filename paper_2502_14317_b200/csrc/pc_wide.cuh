@@ -58,8 +58,13 @@ __device__ __forceinline__ Item decode_item(const WidePhase& p, [[maybe_unused]]
     it.keys = max(0, min(it.keys, __ldg(p.c.len + it.seq)));
   }
   const int tiles = (it.keys + TILE - 1) / TILE;
-  it.j0 = (int)((long long)tiles * it.split / p.c.n_split);
-  it.n = (int)((long long)tiles * (it.split + 1) / p.c.n_split) - it.j0;
+  int n_split = p.c.n_split;
+  if constexpr (is_tree<T>()) {                                 // short sequences in fewer pieces
+    n_split = min(n_split, (tiles + tr.least_tiles - 1) / tr.least_tiles);
+    if (it.split >= n_split) { it.j0 = it.n = 0; return it; }
+  }
+  it.j0 = (int)((long long)tiles * it.split / n_split);
+  it.n = (int)((long long)tiles * (it.split + 1) / n_split) - it.j0;
   return it;
 }
 
@@ -74,31 +79,32 @@ __device__ __forceinline__ bool tail_tile(const T& tr, const WidePhase& p, int k
   if constexpr (is_tree<T>()) return (j + 1) * TILE > keys - p.c.q.w;
   return false;
 }
-// Copies of the entries of tile j that a sequence has, in boxes of 2^log_box: `one(box, first entry in its page, page)` issues each.  Page ids come from L1 (32 of
-// them in a line); the line of a later tile is fetched ahead.
+// Boxes of 2^log_box entries that hold entries of tile j.
 __device__ __forceinline__ int tile_boxes(const TreePhase& t, int keys, int j) {
   const int some = (keys - j * TILE + (1 << t.log_box) - 1) >> t.log_box, all = TILE >> t.log_box;
   return some < all ? some : all;
 }
-template <class F>
-__device__ __forceinline__ void for_boxes(const TreePhase& t, int seq, int keys, int j, int* status, const F& one) {
-  const int boxes = tile_boxes(t, keys, j), ahead = j * TILE + 8 * TILE;
-  const int* const table = t.pages.table + seq * t.pages.stride;
-  if (ahead < keys) asm volatile("prefetch.global.L1 [%0];" ::"l"(table + page_of(t.pages, ahead)));
-#pragma unroll 1
-  for (int i = 0; i < boxes; i += 4) {
-    int in[4], id[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int e = j * TILE + ((i + u < boxes ? i + u : i) << t.log_box), which = page_of(t.pages, e);
-      in[u] = e - which * t.pages.page;
-      id[u] = __ldg(table + which);
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i + u < boxes) one(i + u, in[u], page_checked(t.pages, id[u], status));
+// Pages of a sequence's table, 64 at a time in a warp's registers, the second half on its way while the first is used.
+struct PageIds {
+  int ids, next, first;
+  __device__ __forceinline__ int at(const TreePhase& t, const Item& it, int which, int lane) const {
+    return which + lane <= page_of(t.pages, it.keys - 1) ? __ldg(t.pages.table + it.seq * t.pages.stride + which + lane) : -1;
   }
-}
+  __device__ __forceinline__ PageIds(const TreePhase& t, const Item& it, int lane) : first(page_of(t.pages, it.j0 * TILE)) {
+    ids = at(t, it, first, lane);
+    next = at(t, it, first + 32, lane);
+  }
+  __device__ __forceinline__ void reach(const TreePhase& t, const Item& it, int which, int lane) {        // no page before `which` is asked for again
+    if (which - first < 32) return;
+    first += 32;
+    ids = next;
+    next = at(t, it, first + 32, lane);
+  }
+  __device__ __forceinline__ int of(int which) const {                                                   // the whole warp calls
+    const int i = which - first, x = __shfl_sync(0xFFFFFFFFu, ids, i & 31), y = __shfl_sync(0xFFFFFFFFu, next, i & 31);
+    return i < 32 ? x : y;
+  }
+};
 
 // f16 operands, fp32 accumulation
 __host__ __device__ constexpr uint32_t make_idesc_f16_f32(int M, int N) {
@@ -180,13 +186,29 @@ struct Converter {
     int t;
     half_of(h, it.n, lag, values, t);
     const int key = (it.j0 + t) * TILE + warp * 32 + lane;
-    if constexpr (is_tree<T>()) {
-      if (key >= it.keys) return 0.0f;
-      const int which = page_of(tr.pages, key), id = __ldg(tr.pages.table + it.seq * tr.pages.stride + which);
-      if (id < 0 || id >= tr.pages.n_pages) return 0.0f;
-      return __ldg((values ? prm.c.v_scale : prm.c.k_scale) + ((size_t)id * prm.c.Hkv + it.hkv) * tr.pages.page + (key - which * tr.pages.page));
-    }
     return key < it.keys ? __ldg((values ? prm.c.v_scale : prm.c.k_scale) + ((size_t)it.seq * prm.c.Hkv + it.hkv) * prm.c.capacity + key) : 0.0f;
+  }
+  // TREE: page of that key (-1: none), and with it its scale
+  __device__ __forceinline__ int page_of_key(const Item& it, int h, int lag) const {
+    if constexpr (is_tree<T>()) {
+      bool values;
+      int t;
+      half_of(h, it.n, lag, values, t);
+      const int key = (it.j0 + t) * TILE + warp * 32 + lane;
+      if (h < 2 * it.n && key < it.keys) return __ldg(tr.pages.table + it.seq * tr.pages.stride + page_of(tr.pages, key));
+    }
+    return -1;
+  }
+  __device__ __forceinline__ float scale_in(const Item& it, int h, int lag, int id) const {
+    if constexpr (is_tree<T>()) {
+      bool values;
+      int t;
+      half_of(h, it.n, lag, values, t);
+      const int key = (it.j0 + t) * TILE + warp * 32 + lane;
+      if (id >= 0 && id < tr.pages.n_pages)
+        return __ldg((values ? prm.c.v_scale : prm.c.k_scale) + ((size_t)id * prm.c.Hkv + it.hkv) * tr.pages.page + (key - page_of(tr.pages, key) * tr.pages.page));
+    }
+    return 0.0f;
   }
   template <bool VALUES>
   __device__ __forceinline__ bool convert(int t, float scale, int valid, [[maybe_unused]] int mine = 0) {       // valid: rows of the tile that are entries; TREE: from mine on new tokens
@@ -270,10 +292,15 @@ struct Converter {
     return true;
   }
   __device__ __forceinline__ void item(const Item& it, int lag) {
-    float next = scale_of(it, 0, lag);
+    // (a page is looked up two halves ahead, so that no warp waits for it to ask for its scale)
+    [[maybe_unused]] int page = page_of_key(it, 1, lag);
+    float next = is_tree<T>() ? scale_in(it, 0, lag, page_of_key(it, 0, lag)) : scale_of(it, 0, lag);
     for (int h = 0; h < 2 * it.n; ++h) {
       const float scale = next;
-      if (h + 1 < 2 * it.n) next = scale_of(it, h + 1, lag);
+      if constexpr (is_tree<T>()) {
+        next = scale_in(it, h + 1, lag, page);
+        page = page_of_key(it, h + 2, lag);
+      } else if (h + 1 < 2 * it.n) next = scale_of(it, h + 1, lag);
       bool values;
       int t;
       half_of(h, it.n, lag, values, t);
@@ -366,7 +393,90 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
     setmaxnreg_dec<REGS_PARALLEL.service>();
     if (warp == WARP_PRODUCER) {
       // ================================================================ work queue, queries, and for bf16 the cache (both CTAs of a pair)
-      if (elect_one()) {
+      if constexpr (TREE) {
+        // The whole warp: one lane waits, expects and publishes, each has a box of a tile.  (One thread for all boxes: pages of 16 entries 1.5 times as long
+        // as pages of 128.)
+        constexpr int PARTS = Q8 ? 1 : C::ATOMS, ROW = Q8 ? D : 128;                 // copies of a box, bytes of their rows
+        const int lane = tid & 31, n_items = prm.c.seqs * prm.c.Hkv * prm.c.n_rg * prm.c.n_split, lag = alt ? 2 : 1;
+        const int part = lane >> (7 - tr.log_box), lane_box = part < PARTS ? lane - (part << (7 - tr.log_box)) : TILE;
+        const int lane_to = part * 16384 + (lane_box << tr.log_box) * ROW;
+        Prod p;
+        uint32_t raws = 0;                                 // uses of the raw slots
+        while (true) {
+          int item = n_items;
+          if (lane == 0 && !*cx.abort_flag) item = next_item<C>(cx, p, true, prm.counter, n_items);
+          item = __shfl_sync(0xFFFFFFFFu, item, 0);
+          if (item >= n_items) break;
+          const Item it = decode_item(prm, tr, item);
+          if (it.n == 0) continue;                           // (its slots say so already)
+          if (lane == 0) {
+            Desc d;
+            d.kind = KIND_FLASH;
+            d.c = it.seq; d.hkv = it.hkv; d.len = it.split;
+            d.h[0] = it.rg; d.h[1] = it.keys;
+            d.t[0] = it.j0; d.t[1] = it.n;
+            d.n[0] = alt ? (it.n + 1) / 2 : it.n;
+            d.n[1] = alt ? it.n / 2 : (first_row(it.rg, 1, 0) < rows ? it.n : 0);
+            publish<C>(cx, p, d);
+            for (int b = 0; b < (alt ? 1 : 2); ++b) {
+              if (d.n[b] == 0) continue;
+              const int qs = p.q % NQ;
+              WAIT2(&mi.q_free[qs], free_par(p.q / NQ), W2_QFREE);
+              mbar_arrive_expect_tx(&mi.q_full[qs], C::Q_BYTES);
+              for (int a = 0; a < C::ATOMS; ++a)             // (rows behind the last are zeros and count as copied)
+                load_box<C>(cx.sQ + qs * C::Q_BYTES + a * 16384, &tm_q, smem_u32(&mi.q_full[qs]), a * 64, it.seq * rows + first_row(it.rg, b, 0), it.hkv, 0);
+              ++p.q;
+            }
+          }
+          __syncwarp();
+          PageIds ids(tr, it, lane);
+          for (int h = 0; h < 2 * it.n; ++h) {
+            bool values;
+            int t;
+            half_of(h, it.n, lag, values, t);
+            const int j = it.j0 + t, first = page_of(tr.pages, j * TILE), boxes = tile_boxes(tr, it.keys, j);
+            if (values) ids.reach(tr, it, first, lane);      // (keys are ahead of the values)
+            const int e = j * TILE + (lane_box << tr.log_box), which = lane_box < boxes ? page_of(tr.pages, e) : first, id = ids.of(which);
+            uint32_t& n = Q8 ? raws : values ? p.v : p.k;
+            int slot;
+            uint64_t *free_bar, *full_bar;
+            uint8_t* to;
+            uint32_t par;
+            if constexpr (Q8) {
+              slot = raws % C::RAW; par = free_par(raws / C::RAW);
+              free_bar = &ex.raw_free[slot]; full_bar = &ex.raw_full[slot];
+              to = smem + O::RAW + slot * C::RAW_BYTES;
+            } else {
+              slot = values ? stage_of<C, true>(n) : stage_of<C, false>(n);
+              par = free_par(values ? lap_of<C, true>(n) : lap_of<C, false>(n));
+              free_bar = &mi.kv_free[slot]; full_bar = &mi.kv_full[slot];
+              to = cx.ring + slot * C::STAGE_BYTES;
+            }
+            int ok = 1;
+            if (lane == 0) {
+              ok = !*cx.abort_flag && WAIT2I(free_bar, par, W2_KVFREE);
+              if (ok) mbar_arrive_expect_tx(full_bar, (uint32_t)(boxes * PARTS * ROW) << tr.log_box);
+            }
+            if (!__shfl_sync(0xFFFFFFFFu, ok, 0)) break;
+            ++n;
+            if (lane_box < boxes)
+              load_box<C>(to + lane_to, values ? &tm_v : &tm_k, smem_u32(full_bar), Q8 ? 0 : part * 64, e - which * tr.pages.page, it.hkv,
+                          page_checked(tr.pages, id, cx.status));
+            __syncwarp();
+          }
+        }
+        if (lane == 0) {
+          Desc d;
+          d.kind = KIND_DONE; d.c = d.hkv = d.len = 0;
+          publish<C>(cx, p, d);
+          if constexpr (!Q8) drain_copies<C>(cx, p, leader);
+          else if (*cx.abort_flag) {                          // every copy issued has landed before the exit
+            for (uint32_t i = (p.q > NQ ? p.q - NQ : 0); i < p.q; ++i) mbar_wait_drain(&mi.q_full[i % NQ], full_par(i / NQ), cx.abort_flag);
+            for (uint32_t i = (raws > C::RAW ? raws - C::RAW : 0); i < raws; ++i) mbar_wait_drain(&ex.raw_full[i % C::RAW], full_par(i / C::RAW), cx.abort_flag);
+            abort_grace_pause(cx.abort_flag);
+          }
+        }
+      } else if (elect_one()) {
         const int n_items = prm.c.seqs * prm.c.Hkv * prm.c.n_rg * prm.c.n_split;
         Prod p;
         [[maybe_unused]] uint32_t raws = 0;                // uses of the raw slots
@@ -400,32 +510,13 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
               half_of(h, it.n, alt ? 2 : 1, values, t);
               const int slot = raws % C::RAW;
               if (!WAIT2I(&ex.raw_free[slot], free_par(raws / C::RAW), W2_KVFREE)) break;
-              if constexpr (TREE) {
-                mbar_arrive_expect_tx(&ex.raw_full[slot], tile_boxes(tr, it.keys, it.j0 + t) * D << tr.log_box);
-                for_boxes(tr, it.seq, it.keys, it.j0 + t, cx.status, [&](int i, int in, int id) {
-                  tma_load_4d(smem + O::RAW + slot * C::RAW_BYTES + (i << tr.log_box) * D, values ? &tm_v : &tm_k, &ex.raw_full[slot], 0, in, it.hkv, id);
-                });
-                continue;
-              }
               mbar_arrive_expect_tx(&ex.raw_full[slot], C::RAW_BYTES);
               tma_load_4d(smem + O::RAW + slot * C::RAW_BYTES, values ? &tm_v : &tm_k, &ex.raw_full[slot], PAIR && values ? (int)rank * 64 : 0,
                           (it.j0 + t) * TILE + (PAIR && !values ? (int)rank * 64 : 0), it.hkv, it.seq);
             }
           } else {
             uint8_t* dst;
-            [[maybe_unused]] auto load_pages = [&](int t, bool values) {
-              if constexpr (TREE) {
-                const int bytes = tile_boxes(tr, it.keys, it.j0 + t) * 2 * D << tr.log_box;
-                const uint32_t bar = values ? ring_stage<C, true>(cx, p, leader, &dst, bytes) : ring_stage<C, false>(cx, p, leader, &dst, bytes);
-                if (!bar) return;
-                for_boxes(tr, it.seq, it.keys, it.j0 + t, cx.status, [&](int i, int in, int id) {
-                  for (int a = 0; a < C::ATOMS; ++a)
-                    load_box<C>(dst + a * 16384 + (i << tr.log_box) * 128, values ? &tm_v : &tm_k, bar, a * 64, in, it.hkv, id);
-                });
-              }
-            };
             auto load_k = [&](int t) {
-              if constexpr (TREE) { load_pages(t, false); return; }
               const uint32_t bar = ring_stage<C, false>(cx, p, leader, &dst);
               if (!bar) return;
               for (int a = 0; a < C::ATOMS; ++a)
@@ -434,11 +525,6 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
             const int lag = alt ? 2 : 1;
             for (int t = 0; t < lag && t < it.n; ++t) load_k(t);
             for (int t = 0; t < it.n; ++t) {
-              if constexpr (TREE) {
-                load_pages(t, true);
-                if (t + lag < it.n) load_k(t + lag);
-                continue;
-              }
               const uint32_t bar = ring_stage<C, true>(cx, p, leader, &dst);
               if (bar)
                 for (int a = 0; a < (PAIR ? 1 : C::ATOMS); ++a)
@@ -703,6 +789,8 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
           if (row < rows) scale_log2 = __ldg(prm.half_scale + (size_t)d.hkv * prm.c.total_rows + (size_t)d.c * rows + row);
         }
         RowState st = {-INFINITY, 0.0f};
+        // TREE: a warp whose rows are behind the last only keeps the barriers going; what P and the accumulator hold for it reaches no row
+        [[maybe_unused]] const bool idle = TREE && first_row(d.h[0], b, rank) + (r & ~31) >= rows;
 #pragma unroll 1
         for (int i = 0; i < n; ++i) {
           const int t = alt ? 2 * i + b : i, j = d.t[0] + t, vis = d.h[1] - j * TILE;                  // ragged last tile
@@ -714,7 +802,12 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
             hk.scale = ex.key_scale[at % 8];
           }
           tc_fence_after_sync();
-          if constexpr (TREE) {
+          if (TREE && idle) {
+            hk.on_read();
+            hk.before_p();
+            hk.on_half();
+            hk.on_full();
+          } else if constexpr (TREE) {
             hk.tail = tail_tile(tr, prm, d.h[1], j);
             if (hk.tail) {
               const int row = first_row(d.h[0], b, rank) + r, first = d.h[1] - prm.c.q.w - j * TILE;
