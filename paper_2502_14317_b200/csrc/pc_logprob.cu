@@ -1,17 +1,20 @@
 // Log probabilities of given tokens, entropy and the most probable tokens of rows of logits (pc_token_logprobs).
 //
-// One pass over a row x of V logits.  A thread keeps, over its share, a reference maximum m and with c = scale * log2 e, t = (x - m) c, the sums
+// One pass over a row x of V logits.  A thread keeps, over its share, a reference logit m and with c = scale * log2 e, t = x c - m c, the sums
 //     s = sum 2^t,      h = sum 2^t t,
 // and raises m (s and h to be taken along) only where a logit exceeds it by more than 2^8.  With M the largest m, all joined,
 //     log p(x) = (x - M) scale - ln s,      H = ln s - ln 2 h / s.
-// x - m comes before the factor, so that rows of the type's lowest value do not overflow.
+// The sums are taken against R = m c rounded, one fused operation a term, and moved to m c itself at the end.  Logits that are so far below m that their term
+// is 0 are raised to where it still is, so that -inf has no product 0 * inf; in the types of 16 bits two at a time, before they are widened.  While a
+// share has nothing but -inf and values next to the type's lowest, where x c overflows, t = (x - m) c.
 //
-// The top k: a thread also keeps the largest logit of its share and where it stood.  Only the shares with the k largest of these maxima can hold one of
-// the k largest logits, and only logits not below the k-th of them can be one: those k shares, a few 16-byte pieces each, are read once more (from
-// L2) and everything else is left alone.  Keys are (order of the value, lowest index first), 64 bits, all different, so ties
-// need no rule of their own.  Lists of 32 keys are a warp's registers: sorted, merged (largest against smallest), and inserted into.
+// The top k: of each quarter of its share a thread also keeps the largest logit and the piece of 16 bytes in which it first stood.  With keys (order of the value,
+// earlier piece first), of which no two are the same, let T be the k-th largest of the maxima of groups of four threads: k logits in k different pieces
+// are not below T, so only logits that are not can be among the k largest, and only quarters whose own maximum is not below T have any.  Those are read
+// once more (from L2, some k of 1024), everything else is left alone.  What is found, a few more than k, is ranked by counting: keys (order of the
+// value, lower index first) are all different, so ties need no rule of their own.  Lists of a row's parts are merged, a warp's registers each.
 //
-// A row is the work of a cluster of 1 to 8 CTAs: as many as one round of the grid has room for.
+// A row is the work of a cluster of 1 to 8 CTAs (rule at the launch).
 #include "pc_kernels.h"
 #include "pc_logprob.h"
 #include "pc_rank.cuh"
@@ -51,10 +54,34 @@ __device__ __forceinline__ void values(uint4 v, float (&x)[Logit<TYPE>::VEC]) {
     }
   }
 }
-__device__ __forceinline__ uint4 ld_stream(const uint4* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
+// largest of a piece, NaN left out; every element at least `least` (twice, of the type; fp32: the number), NaN kept
+template <int TYPE>
+__device__ __forceinline__ float top_of(uint4 v) {
+  if constexpr (TYPE == LOGITS_F32) return fmaxf(fmax3(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z)), __uint_as_float(v.w));
+  if constexpr (TYPE == LOGITS_BF16) {
+    auto b = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162*>(&x); };
+    const __nv_bfloat162 m = __hmax2(__hmax2(b(v.x), b(v.y)), __hmax2(b(v.z), b(v.w)));
+    return fmaxf(__low2float(m), __high2float(m));
+  } else {
+    auto h = [](uint32_t x) { return *reinterpret_cast<const __half2*>(&x); };
+    const __half2 m = __hmax2(__hmax2(h(v.x), h(v.y)), __hmax2(h(v.z), h(v.w)));
+    return fmaxf(__low2float(m), __high2float(m));
+  }
+}
+template <int TYPE>
+__device__ __forceinline__ uint32_t raised(uint32_t x, uint32_t least) {
+  uint32_t r;
+  if constexpr (TYPE == LOGITS_F32) asm("max.NaN.f32 %0, %1, %2;" : "=f"(*reinterpret_cast<float*>(&r)) : "f"(__uint_as_float(x)), "f"(__uint_as_float(least)));
+  else if constexpr (TYPE == LOGITS_BF16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(least));
+  else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(least));
+  return r;
+}
+template <int TYPE>
+__device__ __forceinline__ uint32_t twice(float x) {
+  if constexpr (TYPE == LOGITS_F32) return __float_as_uint(x);
+  if constexpr (TYPE == LOGITS_BF16) return pack_bf16x2(x, x);
+  const __half2 h = __float2half2_rn(x);
+  return *reinterpret_cast<const uint32_t*>(&h);
 }
 template <int N>
 __device__ __forceinline__ float max_of(const float (&x)[N]) {
@@ -79,16 +106,6 @@ __device__ __forceinline__ Key larger(Key a, Key b) { return a > b ? a : b; }
 __device__ __forceinline__ Key smaller(Key a, Key b) { return a > b ? b : a; }
 
 // Lists: lane l has the l-th largest.
-__device__ __forceinline__ Key sorted(Key x, int lane) {
-#pragma unroll
-  for (int k = 2; k <= 32; k *= 2)
-#pragma unroll
-    for (int j = k / 2; j > 0; j /= 2) {
-      const Key y = __shfl_xor_sync(0xFFFFFFFFu, x, j);
-      x = ((lane & j) == 0) == ((lane & k) == 0) ? larger(x, y) : smaller(x, y);
-    }
-  return x;
-}
 __device__ __forceinline__ Key merged(Key x, Key reversed, int lane) {
   x = larger(x, reversed);
 #pragma unroll
@@ -105,27 +122,56 @@ __device__ __forceinline__ Key inserted(Key x, Key y, int lane) {
 }
 
 struct Sums { float m, s, h; };                              // relative to m (a logit, finite or +inf or NaN)
-__device__ __forceinline__ Sums joined(const Sums& a, const Sums& b, float c) {
-  Sums r = {fmaxf(a.m, b.m), 0.0f, 0.0f};
+// Sums of the lanes (0 and up of them: N, a power of two) to one, in all of these lanes.
+template <int N>
+__device__ __forceinline__ Sums joined(const Sums& a, float c) {
+  Sums r = {a.m, 0.0f, 0.0f};
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const Sums& x = i ? b : a;
-    if (x.s == 0.0f) continue;                               // (nothing, or nothing but -inf)
-    const float t = (x.m - r.m) * c, f = fast_exp2(t);
-    r.s = fmaf(f, x.s, r.s);
-    r.h = fmaf(f, f > 0.0f ? fmaf(x.s, t, x.h) : 0.0f, r.h);
-    if (t != t) r.s = r.h = t;
+  for (int o = N / 2; o > 0; o /= 2) r.m = fmaxf(r.m, __shfl_xor_sync(0xFFFFFFFFu, r.m, o));
+  if (a.s != 0.0f) {                                         // (0: nothing, or nothing but -inf)
+    const float t = (a.m - r.m) * c, f = fast_exp2(t);
+    r.s = t == t ? f * a.s : t;                              // (+inf less +inf)
+    r.h = f > 0.0f ? f * fmaf(a.s, t, a.h) : 0.0f;
+  }
+#pragma unroll
+  for (int o = N / 2; o > 0; o /= 2) {
+    r.s += __shfl_xor_sync(0xFFFFFFFFu, r.s, o);
+    r.h += __shfl_xor_sync(0xFFFFFFFFu, r.h, o);
   }
   return r;
 }
-__device__ __forceinline__ Sums shuffled(const Sums& a, int o) {
-  return {__shfl_xor_sync(0xFFFFFFFFu, a.m, o), __shfl_xor_sync(0xFFFFFFFFu, a.s, o), __shfl_xor_sync(0xFFFFFFFFu, a.h, o)};
-}
 
+constexpr int FOUND = 1024, RING = 3;
 struct __align__(16) Shared {
-  Key list[8][32];
+  union {
+    uint4 ring[RING][U][NT];
+    struct {                                                 // after the stream
+      Key list[8][32];
+      Key found[FOUND];                                      // (first the groups' maxima)
+      Key least;
+      int winners, n_found;
+      uint16_t winner[U * NT];
+    };
+  };
   Sums sums[8];
 };
+__device__ __forceinline__ void copy_async16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+// how many of n different keys are larger
+__device__ __forceinline__ int rank_among(const Key* keys, int n, Key own) {
+  int r = 0;
+#pragma unroll 4
+  for (int i = 0; i + 1 < n; i += 2) {
+    const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(keys + i);
+    r += (y.x > own) + (y.y > own);
+  }
+  if (n % 2) r += keys[n - 1] > own;
+  return r;
+}
 __device__ __forceinline__ Key ld_cluster_key(uint32_t addr) {
   Key x;
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(x) : "r"(addr) : "memory");
@@ -156,7 +202,8 @@ __device__ __forceinline__ Key merge_lists(Shared& sh, Key x, int n, int warp, i
 template <int TYPE>
 __global__ void __launch_bounds__(NT, CTAS) token_logprobs_kernel(const LogProb p, const int split) {
   constexpr int VEC = Logit<TYPE>::VEC, BYTES = Logit<TYPE>::BYTES;
-  __shared__ Shared sh;
+  extern __shared__ __align__(16) uint8_t smem[];
+  Shared& sh = *reinterpret_cast<Shared*>(smem);
   chain();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const long long row = blockIdx.x / split;
@@ -170,72 +217,125 @@ __global__ void __launch_bounds__(NT, CTAS) token_logprobs_kernel(const LogProb 
   const int lo = (int)((long long)n * rank / split), hi = (int)((long long)n * (rank + 1) / split);
   auto whole = [&](int j) { return j * VEC >= head && (long long)(j + 1) * VEC - head <= p.V; };
   auto there = [&](int j, int i) { return j * VEC + i >= head && j * VEC + i - head < p.V; };
-  auto load = [&](int j, float (&x)[VEC]) {                  // -inf in the place of elements that are not the row's
-    if (whole(j)) { values<TYPE>(__ldg(pieces + j), x); return; }
+  auto part = [&](int j) {                                   // a piece that has neighbours' elements beside the row's: -inf in their place
+    uint32_t w[4] = {};
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = there(j, i) ? one_logit<TYPE>(reinterpret_cast<const uint8_t*>(pieces + j) + i * BYTES) : -INFINITY;
+    for (int i = 0; i < VEC; ++i) {
+      constexpr uint32_t NONE = TYPE == LOGITS_F32 ? 0xFF800000u : TYPE == LOGITS_BF16 ? 0xFF80u : 0xFC00u;
+      const uint8_t* const e = reinterpret_cast<const uint8_t*>(pieces + j) + i * BYTES;
+      if constexpr (BYTES == 4) w[i] = there(j, i) ? __ldg(reinterpret_cast<const uint32_t*>(e)) : NONE;
+      else w[i / 2] |= (there(j, i) ? (uint32_t)__ldg(reinterpret_cast<const uint16_t*>(e)) : NONE) << (i % 2 * 16);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
   };
+  auto load = [&](int j, float (&x)[VEC]) { values<TYPE>(whole(j) ? __ldg(pieces + j) : part(j), x); };
 
+  // the present reference: logit m, R, the logit that raises it, what a term is 0 at; low: m is next to the lowest, t = (x - m) c
+  int token = -1;                                            // of warp 0: its logit is on its way while the row goes through
+  float token_logit = 0.0f;
+  if (warp == 0 && rank == 0 && p.logprob != nullptr) {
+    token = __ldg(p.tokens + row);
+    if (token >= 0 && token < p.V) token_logit = one_logit<TYPE>(first + (long long)token * BYTES);
+  }
   Sums a = {-FLT_MAX, 0.0f, 0.0f};
-  float best = -INFINITY;
-  int at = -1;
+  float R = 0.0f, limit = -FLT_MAX;
+  uint32_t floor2 = 0;
+  bool low = true;
+  float best[U];
+  int at[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) { best[u] = -INFINITY; at[u] = -1; }
   uint64_t s2 = 0, h2 = 0;
   const uint64_t c2 = pack_f32x2(c, c);
-  auto take = [&](const float (&x)[VEC], int j) {
-    const float top = max_of(x);
-    if (top > best || at < 0) { best = top; at = j; }
-    if ((top - a.m) * c > 8.0f) {                            // rare after the first pieces
-      const float t = (a.m - top) * c, f = fast_exp2(t);
-      float s0, s1, h0, h1;
-      unpack_f32x2(s2, s0, s1);
-      unpack_f32x2(h2, h0, h1);
-      s2 = pack_f32x2(s0 * f, s1 * f);
-      h2 = f > 0.0f ? pack_f32x2(f * fmaf(s0, t, h0), f * fmaf(s1, t, h1)) : 0;
-      a.m = top;
-    }
-    const uint64_t m2 = pack_f32x2(-a.m, -a.m);
-#pragma unroll
-    for (int i = 0; i < VEC; i += 2) {
-      float t0, t1;
-      unpack_f32x2(mul_f32x2(add_f32x2(pack_f32x2(x[i], x[i + 1]), m2), c2), t0, t1);
-      t0 = max_nan(t0, -200.0f); t1 = max_nan(t1, -200.0f);   // 2^-200 is 0, and 0 times it a number
-      const uint64_t e2 = pack_f32x2(fast_exp2(t0), fast_exp2(t1));
-      s2 = add_f32x2(s2, e2);
-      h2 = fma_f32x2(e2, pack_f32x2(t0, t1), h2);
-    }
+  constexpr float LOWEST = TYPE == LOGITS_F16 ? -65504.0f : -3.3895314e38f;
+  auto raise = [&](float top) {
+    const float R_new = top * c, below = fmaf(fabsf(top), -0.015625f, top - 150.0f / c);       // (under every rounding of itself to the type)
+    const bool low_new = !(top > -1e30f && below > LOWEST);
+    const float t = low ? (a.m - top) * c : low_new ? -INFINITY : R - R_new, f = fast_exp2(t);
+    float s0, s1, h0, h1;
+    unpack_f32x2(s2, s0, s1);
+    unpack_f32x2(h2, h0, h1);
+    s2 = pack_f32x2(s0 * f, s1 * f);
+    h2 = f > 0.0f ? pack_f32x2(f * fmaf(s0, t, h0), f * fmaf(s1, t, h1)) : 0;
+    a.m = top;
+    R = R_new;
+    limit = top + 8.0f / c;
+    low = low_new;
+    floor2 = twice<TYPE>(below);
   };
-  {
-    const int from = lo + (lo < hi && !whole(lo) ? 1 : 0), to = hi - (lo < hi && hi - 1 > lo && !whole(hi - 1) ? 1 : 0);      // whole pieces
-    int j = lo + tid;
-    if (j < from) j += NT;
-    for (; j + (U - 1) * NT < to; j += U * NT) {
-      uint4 v[U];
+  // U pieces at a time, one branch for all: a piece's own branches took a tenth of the instructions
+  auto take = [&](const uint4 (&v)[U], int j) {
+    float top[U], most;
 #pragma unroll
-      for (int u = 0; u < U; ++u) v[u] = ld_stream(pieces + j + u * NT);
+    for (int u = 0; u < U; ++u) top[u] = top_of<TYPE>(v[u]);
+    most = max_of(top);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (top[u] > best[u]) { best[u] = top[u]; at[u] = j + u * NT; }
+    if (most > limit) raise(most);                           // rare after the first pieces
+    if (!low) {
+      const uint64_t r2 = pack_f32x2(-R, -R);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         float x[VEC];
-        values<TYPE>(v[u], x);
-        take(x, j + u * NT);
+        values<TYPE>(make_uint4(raised<TYPE>(v[u].x, floor2), raised<TYPE>(v[u].y, floor2), raised<TYPE>(v[u].z, floor2), raised<TYPE>(v[u].w, floor2)), x);
+#pragma unroll
+        for (int i = 0; i < VEC; i += 2) {
+          const uint64_t t2 = fma_f32x2(pack_f32x2(x[i], x[i + 1]), c2, r2);
+          float t0, t1;
+          unpack_f32x2(t2, t0, t1);
+          const uint64_t e2 = pack_f32x2(fast_exp2(t0), fast_exp2(t1));
+          s2 = add_f32x2(s2, e2);
+          h2 = fma_f32x2(e2, t2, h2);
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < U; ++u) {
+        float x[VEC];
+        values<TYPE>(u == 0 ? v[0] : u == 1 ? v[1] : u == 2 ? v[2] : v[3], x);
+#pragma unroll
+        for (int i = 0; i < VEC; i += 2) {
+          const float t0 = max_nan((x[i] - a.m) * c, -200.0f), t1 = max_nan((x[i + 1] - a.m) * c, -200.0f);
+          const uint64_t e2 = pack_f32x2(fast_exp2(t0), fast_exp2(t1));
+          s2 = add_f32x2(s2, e2);
+          h2 = fma_f32x2(e2, pack_f32x2(t0, t1), h2);
+        }
       }
     }
-    for (; j < to; j += NT) {
-      float x[VEC];
-      values<TYPE>(ld_stream(pieces + j), x);
-      take(x, j);
-    }
-    if (lo < hi && tid == 0 && from > lo) {                  // (the first piece: of its elements none is preferred to an equal one behind it)
-      float x[VEC];
-      load(lo, x);
-      const float was = best;
-      const int stood = at;
-      take(x, lo);
-      if (stood >= 0 && max_of(x) == was) at = lo;
-    }
-    if (to < hi && tid == (hi - 1 - lo) % NT) {
-      float x[VEC];
-      load(hi - 1, x);
-      take(x, hi - 1);
+  };
+  {
+    // Piece lo + tid + i NT, of quarter i % U, U of them at a time through this thread's places of a ring in shared memory: three such groups are on their
+    // way, or being taken, which keeps 190 KB of an SM in flight.
+    const int from = lo + (lo < hi && !whole(lo) ? 1 : 0), to = hi - (lo < hi && hi - 1 > lo && !whole(hi - 1) ? 1 : 0);      // whole pieces
+    const int groups = (hi - lo + U * NT - 1) / (U * NT);
+    auto fetch = [&](int g) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int j = lo + tid + (g * U + u) * NT;
+        if (j >= from && j < to) copy_async16(&sh.ring[g % RING][u][tid], pieces + j);
+      }
+      copy_async_commit();
+    };
+#pragma unroll
+    for (int g = 0; g < RING; ++g) fetch(g);
+    for (int g = 0; g < groups; ++g) {
+      copy_async_wait<RING - 1>();
+      const int j = lo + tid + g * (U * NT);
+      uint4 v[U];
+      if (j >= from && j + (U - 1) * NT < to) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = sh.ring[g % RING][u][tid];
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int k = j + u * NT;
+          constexpr uint32_t NONE = TYPE == LOGITS_F32 ? 0xFF800000u : TYPE == LOGITS_BF16 ? 0xFF80FF80u : 0xFC00FC00u;
+          v[u] = k >= from && k < to ? sh.ring[g % RING][u][tid] : k < hi ? part(k) : make_uint4(NONE, NONE, NONE, NONE);
+        }
+      }
+      take(v, j);
+      fetch(g + RING);
     }
   }
   {
@@ -244,54 +344,93 @@ __global__ void __launch_bounds__(NT, CTAS) token_logprobs_kernel(const LogProb 
     unpack_f32x2(h2, h0, h1);
     a.s = s0 + s1;
     a.h = h0 + h1;
+    if (!low) {                                              // from R to m c
+      const float off = fmaf(a.m, c, -R), f = exp2f(-off);
+      a.h = f * fmaf(-off, a.s, a.h);
+      a.s *= f;
+    }
   }
-#pragma unroll
-  for (int o = 16; o > 0; o /= 2) a = joined(a, shuffled(a, o), c);
+  a = joined<32>(a, c);
   if (lane == 0) sh.sums[warp] = a;
 
   Key x = 0;
   if (p.top > 0) {
-    // the shares' maxima, the k largest of them, and what these shares hold that is not below the last of them
-    if (at >= 0) {
-      float y[VEC];
-      load(at, y);
+    copy_async_wait<0>();
+    __syncthreads();                                         // the ring's place is free
+    Key mine[U], group = 0;                                  // of the quarters' maxima; 0: an empty one
 #pragma unroll
-      for (int i = 0; i < VEC; ++i)
-        if (there(at, i)) x = larger(x, key_of(y[i], at * VEC + i - head));
+    for (int u = 0; u < U; ++u) {
+      const int j = lo + tid + u * NT;                       // (nothing but -inf: its first piece)
+      mine[u] = j >= hi ? 0 : (Key)rank_key(best[u], false) << 32 | (uint32_t)~(at[u] < 0 ? j : at[u]);
+      group = larger(group, mine[u]);
     }
-    merge_lists(sh, sorted(x, lane), WARPS, warp, lane);
-    const Key winner = sh.list[0][lane], least = sh.list[0][p.top - 1];
+    group = larger(group, __shfl_xor_sync(0xFFFFFFFFu, group, 1));
+    group = larger(group, __shfl_xor_sync(0xFFFFFFFFu, group, 2));
+    if (lane % 4 == 0) sh.found[tid / 4] = group;
+    if (tid == 0) { sh.least = 0; sh.winners = sh.n_found = 0; }
     __syncthreads();
-    x = 0;
-    for (int k = warp; k < p.top; k += WARPS) {
-      const Key w = __shfl_sync(0xFFFFFFFFu, winner, k);
-      if (w == 0) break;
-      const int share = ((id_of(w) + head) / VEC - lo) % NT;
-      for (int j0 = lo + share; j0 < hi; j0 += 32 * NT) {
-        const int j = j0 + lane * NT;
+    if (tid < NT / 4) {
+      const Key own = sh.found[tid];
+      if (own != 0 && rank_among(sh.found, NT / 4, own) == p.top - 1) sh.least = own;     // (fewer groups than that: everything is looked at)
+    }
+    __syncthreads();
+    const Key least = sh.least;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (mine[u] != 0 && mine[u] >= least) sh.winner[atomicAdd(&sh.winners, 1)] = (uint16_t)(tid + u * NT);
+    if (warp == 0) sh.list[0][lane] = 0;
+    __syncthreads();
+    // What these quarters hold that is not below `least`, by pieces, half a warp each.  In no order; the counting below puts it into one.
+    const int winners = sh.winners;
+    for (int k = 2 * warp + lane / 16; k < winners; k += 2 * WARPS) {
+      for (int j = lo + sh.winner[k] + lane % 16 * (U * NT); j < hi; j += 16 * U * NT) {
         float y[VEC];
-        if (j < hi) load(j, y);
+        load(j, y);
+        if (((Key)rank_key(max_of(y), false) << 32 | (uint32_t)~j) < least) continue;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-          const Key mine = j < hi && there(j, i) ? key_of(y[i], j * VEC + i - head) : 0;
-          unsigned some = __ballot_sync(0xFFFFFFFFu, mine != 0 && mine >= least);
-          while (some) {
-            const int from = __ffs(some) - 1;
-            some &= some - 1;
-            x = inserted(x, __shfl_sync(0xFFFFFFFFu, mine, from), lane);
+          if (there(j, i) && ((Key)rank_key(y[i], false) << 32 | (uint32_t)~j) >= least) {
+            const int n = atomicAdd(&sh.n_found, 1);
+            if (n < FOUND) sh.found[n] = key_of(y[i], j * VEC + i - head);
           }
         }
       }
     }
-    x = merge_lists(sh, x, WARPS, warp, lane);
+    __syncthreads();
+    const int n_found = sh.n_found;
+    if (n_found <= FOUND) {
+      for (int i = tid; i < n_found; i += NT) {
+        const Key own = sh.found[i];
+        const int r = rank_among(sh.found, n_found, own);
+        if (r < 32) sh.list[0][r] = own;
+      }
+      __syncthreads();
+      if (warp == 0) x = sh.list[0][lane];
+    } else {
+      // far more of them than there is room for: each warp keeps a list of the largest of its part of the row's
+      for (int k = warp; k < winners; k += WARPS) {
+        for (int j0 = lo + sh.winner[k]; j0 < hi; j0 += 32 * U * NT) {
+          const int j = j0 + lane * (U * NT);
+          float y[VEC];
+          if (j < hi) load(j, y);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) {
+            const Key one = j < hi && there(j, i) ? key_of(y[i], j * VEC + i - head) : 0;
+            unsigned some = __ballot_sync(0xFFFFFFFFu, one > __shfl_sync(0xFFFFFFFFu, x, 31));
+            while (some) {
+              const int from = __ffs(some) - 1;
+              some &= some - 1;
+              x = inserted(x, __shfl_sync(0xFFFFFFFFu, one, from), lane);
+            }
+          }
+        }
+      }
+      x = merge_lists(sh, x, WARPS, warp, lane);
+    }
   } else {
     __syncthreads();
   }
-  if (warp == 0) {
-    a = lane < WARPS ? sh.sums[lane] : Sums{-FLT_MAX, 0.0f, 0.0f};
-#pragma unroll
-    for (int o = 16; o > 0; o /= 2) a = joined(a, shuffled(a, o), c);
-  }
+  if (warp == 0) a = joined<WARPS>(sh.sums[lane % WARPS], c);
   if (split > 1) {
     // the other CTAs' lists and sums, a warp each
     if (tid == 0) sh.sums[0] = a;
@@ -306,11 +445,7 @@ __global__ void __launch_bounds__(NT, CTAS) token_logprobs_kernel(const LogProb 
       __syncthreads();
       if (lane == 0) sh.sums[warp] = b;
       x = merge_lists(sh, y, split, warp, lane);
-      if (warp == 0) {
-        a = lane < split ? sh.sums[lane] : Sums{-FLT_MAX, 0.0f, 0.0f};
-#pragma unroll
-        for (int o = 16; o > 0; o /= 2) a = joined(a, shuffled(a, o), c);
-      }
+      if (warp == 0) a = joined<WARPS>(sh.sums[lane % WARPS], c);        // (warps behind the last CTA left nothing)
     }
     cluster_sync_all();                                      // no CTA exits while another may read its shared memory
     if (rank != 0) return;
@@ -321,10 +456,7 @@ __global__ void __launch_bounds__(NT, CTAS) token_logprobs_kernel(const LogProb 
   const float ln_s = none ? 0.0f : odd ? __int_as_float(0x7FC00000) : logf(a.s);
   auto logprob = [&](float y) { return none ? -INFINITY : fmaf(y - a.m, p.scale, -ln_s); };
   if (lane == 0) {
-    if (p.logprob != nullptr) {
-      const int t = __ldg(p.tokens + row);
-      p.logprob[row] = t < 0 ? 0.0f : t >= p.V ? __int_as_float(0x7FC00000) : logprob(one_logit<TYPE>(first + (long long)t * BYTES));
-    }
+    if (p.logprob != nullptr) p.logprob[row] = token < 0 ? 0.0f : token >= p.V ? __int_as_float(0x7FC00000) : logprob(token_logit);
     if (p.entropy != nullptr) p.entropy[row] = none ? 0.0f : ln_s - 0.6931471805599453f * (a.h / a.s);
   }
   if (lane < p.top) {
@@ -345,13 +477,21 @@ __global__ void __launch_bounds__(128) group_nll_kernel(const float* logprob, in
   if (lane == 0) nll[g] = -s;
 }
 
+namespace {
+template <int TYPE>
+cudaError_t logprobs_t(const LogProb& p, int split, cudaStream_t st) {
+  static_assert(CTAS * (sizeof(Shared) + 1024) <= 233472, "CTAs per SM");
+  if (cudaError_t e = cudaFuncSetAttribute(token_logprobs_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)); e != cudaSuccess) return e;
+  return launch_chained(token_logprobs_kernel<TYPE>, dim3((unsigned)((long long)p.N * split)), dim3(NT), sizeof(Shared), st, split, p, split);
+}
+}  // namespace
+
 cudaError_t launch_token_logprobs(const LogProb& p, int type, int sm_count, cudaStream_t st) {
+  // Parts of a row: as many as leave each its SM and 6000 logits.  Measured, us, 1 / 2 / 4 / 8 parts: one row of 128256 in bf16, top 8, 13.5 / 10.9 / 9.0 / 8.4, 32 rows
+  // 13.7 / 11.1 / 10.2 / 10.7, 64 13.8 / 11.3 / 11.6 / 13.5, 148 14.8 / 15.8 / 23.0 / 31.5; one row of 8000 6.3 / 7.5 / 8.0 / 8.2, 64 of 50001 in fp16 9.9 / 9.7 / 10.2 / 11.9.
   int split = 1;
-  while (split < 8 && (long long)p.N * split * 2 <= (long long)CTAS * sm_count && p.V / (2 * split) >= 2 * NT) split *= 2;
-  const dim3 grid((unsigned)((long long)p.N * split));
-  cudaError_t e = type == LOGITS_F32    ? launch_chained(token_logprobs_kernel<LOGITS_F32>, grid, dim3(NT), 0, st, split, p, split)
-                  : type == LOGITS_BF16 ? launch_chained(token_logprobs_kernel<LOGITS_BF16>, grid, dim3(NT), 0, st, split, p, split)
-                                        : launch_chained(token_logprobs_kernel<LOGITS_F16>, grid, dim3(NT), 0, st, split, p, split);
+  while (split < 8 && (long long)p.N * split * 2 <= sm_count && p.V / (2 * split) >= 6000) split *= 2;
+  cudaError_t e = type == LOGITS_F32 ? logprobs_t<LOGITS_F32>(p, split, st) : type == LOGITS_BF16 ? logprobs_t<LOGITS_BF16>(p, split, st) : logprobs_t<LOGITS_F16>(p, split, st);
   if (e != cudaSuccess || p.nll == nullptr) return e;
   const int groups = p.N / p.group;
   return launch_chained(group_nll_kernel, dim3((unsigned)((groups + 3) / 4)), dim3(128), 0, st, 1, (const float*)p.logprob, groups, p.group, p.nll);
