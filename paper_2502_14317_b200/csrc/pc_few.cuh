@@ -86,7 +86,7 @@ __device__ __forceinline__ float max_over_keys(float x) {
 __device__ __forceinline__ void cp_async4(uint32_t dst, const float* src, bool there) {      // zero where there is no entry
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
-__device__ __forceinline__ void cp_async16(uint32_t dst, const float* src, bool there) {
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_async_arrive(uint64_t* bar) {                             // once this thread's copies have landed
@@ -180,7 +180,9 @@ __device__ __forceinline__ void few_body(const CUtensorMap& tm_k, const CUtensor
     return -1;
   };
   [[maybe_unused]] auto id_of = [&](int which) {                // of a page of the present tile; the whole warp calls
-    const int at = which - ids_first, x = __shfl_sync(0xFFFFFFFFu, ids, at & 31), y = __shfl_sync(0xFFFFFFFFu, ids_next, at & 31);
+    const int at = which - ids_first, x = __shfl_sync(0xFFFFFFFFu, ids, at & 31);
+    if (!__any_sync(0xFFFFFFFFu, at >= 32)) return x;             // (does not wait for what is still on its way)
+    const int y = __shfl_sync(0xFFFFFFFFu, ids_next, at & 31);
     return at < 32 ? x : y;
   };
   // copies of tile i into its stage; the whole producer warp calls

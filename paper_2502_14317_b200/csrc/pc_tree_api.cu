@@ -104,7 +104,7 @@ PhasePlan tree_few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, 
       t += per * (tile > part * bytes * ctas ? tile : part * bytes * ctas);
     } else {
       const double tile = beside > bytes * fit ? beside : bytes * fit;
-      t += part * items * tiles * tile / fit + round_us * (ctas / fit - 1.0) + 0.5 * per * tile;
+      t += part * items * tiles * tile / fit + round_us * (ctas / fit - 1.0) + 0.5 * per * beside;
     }
     if (least < 0.0 || t < least) { least = t; p.n_split = s; p.finish = finish; }
   };

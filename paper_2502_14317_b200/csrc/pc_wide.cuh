@@ -74,6 +74,11 @@ struct __align__(16) ExtraTree {
   uint64_t fix_go, fix_done, odd_full;
   unsigned long long odd[2][4];
 };
+// TREE, 8 bits: of a tile's values log2 of the scales and their inverses (softmax_codes_tile); they stay as long as the keys' scales
+struct __align__(16) ExtraValues {
+  float log2[8][TILE], inverse[8][TILE];
+};
+constexpr float LEAST_VALUE_LOG2 = -100.0f;                      // of scales that are 0 or next to it: their entries' values are nothing, their weights count
 template <class T>
 __device__ __forceinline__ bool tail_tile(const T& tr, const WidePhase& p, int keys, int j) {       // whether tile j has new tokens or less than 128 entries
   if constexpr (is_tree<T>()) return (j + 1) * TILE > keys - p.c.q.w;
@@ -101,14 +106,16 @@ struct PageIds {
     next = at(t, it, first + 32, lane);
   }
   __device__ __forceinline__ int of(int which) const {                                                   // the whole warp calls
-    const int i = which - first, x = __shfl_sync(0xFFFFFFFFu, ids, i & 31), y = __shfl_sync(0xFFFFFFFFu, next, i & 31);
+    const int i = which - first, x = __shfl_sync(0xFFFFFFFFu, ids, i & 31);
+    if (!__any_sync(0xFFFFFFFFu, i >= 32)) return x;                                     // (does not wait for what is still on its way)
+    const int y = __shfl_sync(0xFFFFFFFFu, next, i & 31);
     return i < 32 ? x : y;
   }
 };
 
 // f16 operands, fp32 accumulation
-__host__ __device__ constexpr uint32_t make_idesc_f16_f32(int M, int N) {
-  return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
+__host__ __device__ constexpr uint32_t make_idesc_f16_f32(int M, int N, bool b_mn_major = false) {
+  return (1u << 4) | (static_cast<uint32_t>(b_mn_major) << 16) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 
 // hooks of the softmax warps: columns times the scales of their keys (8-bit formats)
@@ -148,11 +155,79 @@ struct TreeHooks : Base {
     for (int i = 0; i < 32; ++i)
       if (!(bits & (1u << i))) c[i] = 0xFF800000u;
   }
-  __device__ __forceinline__ void scale_keys(uint32_t (&c0)[32], uint32_t (&c1)[32], uint32_t (&c2)[32], uint32_t (&c3)[32]) const {
-    Base::scale_keys(c0, c1, c2, c3);
+  __device__ __forceinline__ void scale_keys(uint32_t (&c0)[32], uint32_t (&c1)[32], uint32_t (&c2)[32], uint32_t (&c3)[32]) const { hide(c0, c1, c2, c3); }
+  __device__ __forceinline__ void hide(uint32_t (&c0)[32], uint32_t (&c1)[32], uint32_t (&c2)[32], uint32_t (&c3)[32]) const {
     if (tail) { mask(c0, seen[0]); mask(c1, seen[1]); mask(c2, seen[2]); mask(c3, seen[3]); }
   }
 };
+
+// One tile over 8-bit codes, for TREE: the keys' codes are exact operands, and the values' are too, because their scales go into the logits.  With z
+// the logit of a key in log2 units and v the scale of its value, z' = z + log2 v,
+//     O = sum 2^(z' - m) code,      l = sum 2^(z' - m) / v,
+// where m is a reference for z': what is held to its range is the weight that a code has, so that probabilities can be halves (11 bits; rounded to bf16 beside
+// values rounded to bf16 the error against 64 bits was 1.7 times that of fp32 probabilities, now 1.1), and the conversion of values is that of keys.
+template <int D, class Hooks>
+__device__ __forceinline__ void softmax_codes_tile(uint32_t s_taddr, uint32_t p_taddr, uint32_t o_taddr, bool first_tile, float scale_log2, RowState& st,
+                                                   const Hooks& hk, const float* key_scale, const float* value_log2, const float* value_inverse) {
+  uint32_t c[4][32];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) tmem_ld32(s_taddr + 32 * i, c[i]);
+  tmem_wait_ld();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) loaded(c[i]);
+  hk.on_read();
+  const uint64_t scale2 = dup2(scale_log2);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      const float4 f = *reinterpret_cast<const float4*>(key_scale + 32 * i + j), g = *reinterpret_cast<const float4*>(value_log2 + 32 * i + j);
+      float a, b;
+      unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(c[i][j]), __uint_as_float(c[i][j + 1])), mul_f32x2(pack_f32x2(f.x, f.y), scale2), pack_f32x2(g.x, g.y)), a, b);
+      c[i][j] = __float_as_uint(a); c[i][j + 1] = __float_as_uint(b);
+      unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(c[i][j + 2]), __uint_as_float(c[i][j + 3])), mul_f32x2(pack_f32x2(f.z, f.w), scale2), pack_f32x2(g.z, g.w)), a, b);
+      c[i][j + 2] = __float_as_uint(a); c[i][j + 3] = __float_as_uint(b);
+    }
+  hk.hide(c[0], c[1], c[2], c[3]);
+  const float mx = fmaxf(fmaxf(max32(c[0]), max32(c[1])), fmaxf(max32(c[2]), max32(c[3])));
+  hk.before_p();
+  const bool raise = first_tile || mx > st.m + LAZY_RESCALE_LOG2;
+  if (__any_sync(0xFFFFFFFFu, raise)) {                            // rare; warp-uniform: each warp owns its 32 lanes of O
+    float alpha = 1.0f;
+    if (raise) {
+      const float m_new = fmaxf(st.m, mx);
+      alpha = (st.m == -INFINITY) ? 0.0f : fast_exp2(st.m - m_new);
+      st.m = m_new;
+      st.l *= alpha;
+    }
+    if (!first_tile) rescale_rows<D>(o_taddr, alpha);
+  }
+  const uint64_t negm2 = dup2(st.m == -INFINITY ? 0.0f : -st.m);
+  uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t pk[16];
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+      const float4 g = *reinterpret_cast<const float4*>(value_inverse + 32 * i + j);
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        float x0, x1;
+        unpack_f32x2(add_f32x2(pack_f32x2(__uint_as_float(c[i][j + e]), __uint_as_float(c[i][j + e + 1])), negm2), x0, x1);
+        const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+        sum2[e / 2] = fma_f32x2(pack_f32x2(p0, p1), e ? pack_f32x2(g.z, g.w) : pack_f32x2(g.x, g.y), sum2[e / 2]);
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(pk[(j + e) / 2]) : "f"(p1), "f"(p0));
+      }
+    }
+    tmem_st16(p_taddr + 16 * i, pk);
+    if (i == 1) { tmem_wait_st(); hk.on_half(); }
+  }
+  tmem_wait_st();
+  hk.on_full();
+  float a0, a1;
+  unpack_f32x2(add_f32x2(sum2[0], sum2[1]), a0, a1);
+  st.l += a0 + a1;
+}
 
 // Halves (keys or values of a tile) of an item's n tiles in the order in which the issuers want them: K of the first `lag` tiles, then
 // V of tile t, K of tile t + lag.
@@ -176,9 +251,10 @@ struct Converter {
   int warp, lane;
   uint32_t k = 0, v = 0, raws = 0, tile = 0;               // uses of the stages and of the slots; tiles of earlier items
   const T& tr;
+  ExtraValues* values;                                     // TREE
   unsigned long long odd = 0;                              // TREE: new tokens of the present item with a value that is no number, of this lane's
-  __device__ __forceinline__ Converter(const Ctx2& c, const WidePhase& p, Extra8& e, uint8_t* raw_smem, int w, int l, const T& t)
-      : cx(c), prm(p), ex(e), raw(raw_smem), warp(w), lane(l), tr(t) {}
+  __device__ __forceinline__ Converter(const Ctx2& c, const WidePhase& p, Extra8& e, uint8_t* raw_smem, int w, int l, const T& t, ExtraValues* values_)
+      : cx(c), prm(p), ex(e), raw(raw_smem), warp(w), lane(l), tr(t), values(values_) {}
 
   // scale of key warp * 32 + lane of the tile, 0 behind the last entry
   __device__ __forceinline__ float scale_of(const Item& it, int h, int lag) const {
@@ -188,30 +264,26 @@ struct Converter {
     const int key = (it.j0 + t) * TILE + warp * 32 + lane;
     return key < it.keys ? __ldg((values ? prm.c.v_scale : prm.c.k_scale) + ((size_t)it.seq * prm.c.Hkv + it.hkv) * prm.c.capacity + key) : 0.0f;
   }
-  // TREE: page of that key (-1: none), and with it its scale
-  __device__ __forceinline__ int page_of_key(const Item& it, int h, int lag) const {
+  // TREE: key warp * 32 + lane of tile t: its page (-1: none), and with that the scales of the key and its value
+  __device__ __forceinline__ int page_of_key(const Item& it, int t) const {
     if constexpr (is_tree<T>()) {
-      bool values;
-      int t;
-      half_of(h, it.n, lag, values, t);
       const int key = (it.j0 + t) * TILE + warp * 32 + lane;
-      if (h < 2 * it.n && key < it.keys) return __ldg(tr.pages.table + it.seq * tr.pages.stride + page_of(tr.pages, key));
+      if (t < it.n && key < it.keys) return __ldg(tr.pages.table + it.seq * tr.pages.stride + page_of(tr.pages, key));
     }
     return -1;
   }
-  __device__ __forceinline__ float scale_in(const Item& it, int h, int lag, int id) const {
+  __device__ __forceinline__ float2 scales_in(const Item& it, int t, int id) const {
     if constexpr (is_tree<T>()) {
-      bool values;
-      int t;
-      half_of(h, it.n, lag, values, t);
-      const int key = (it.j0 + t) * TILE + warp * 32 + lane;
-      if (id >= 0 && id < tr.pages.n_pages)
-        return __ldg((values ? prm.c.v_scale : prm.c.k_scale) + ((size_t)id * prm.c.Hkv + it.hkv) * tr.pages.page + (key - page_of(tr.pages, key) * tr.pages.page));
+      if (id >= 0 && id < tr.pages.n_pages) {
+        const int key = (it.j0 + t) * TILE + warp * 32 + lane;
+        const size_t at = ((size_t)id * prm.c.Hkv + it.hkv) * tr.pages.page + (key - page_of(tr.pages, key) * tr.pages.page);
+        return make_float2(__ldg(prm.c.k_scale + at), __ldg(prm.c.v_scale + at));
+      }
     }
-    return 0.0f;
+    return make_float2(0.0f, 0.0f);
   }
   template <bool VALUES>
-  __device__ __forceinline__ bool convert(int t, float scale, int valid, [[maybe_unused]] int mine = 0) {       // valid: rows of the tile that are entries; TREE: from mine on new tokens
+  __device__ __forceinline__ bool convert(int t, float scale, int valid, [[maybe_unused]] int mine = 0, [[maybe_unused]] float value_scale = 0.0f) {       // valid: rows of the tile that are entries; TREE: from mine on new tokens
     Misc2& mi = *cx.mi;
     uint32_t& n = VALUES ? v : k;
     constexpr int FIRST = VALUES ? C::NK : 0, STAGES = VALUES ? C::NV : C::NK;
@@ -232,17 +304,14 @@ struct Converter {
         __syncwarp();
       }
     }
-    if constexpr (VALUES && is_tree<T>()) {                // (one CTA: rows 32 warp + lane)
+    if constexpr (VALUES && is_tree<T>() && FMT == FMT_E4M3) {     // (one CTA: rows 32 warp + lane)
       const int row = warp * 32 + lane;
-      if (mine < TILE && row >= mine && row < valid) {
-        bool is_odd = !(fabsf(scale) < INFINITY);
-        if (is_odd) scale = 0.0f;
-        if constexpr (FMT == FMT_E4M3) {
-          for (int i = 0; i < BYTES; i += 16) {            // (the places of a row's pieces do not matter here)
-            uint4 x = *reinterpret_cast<const uint4*>(from + row * BYTES + i);
-            const uint4 y = make_uint4(x.x & finite_parts<FMT>(x.x), x.y & finite_parts<FMT>(x.y), x.z & finite_parts<FMT>(x.z), x.w & finite_parts<FMT>(x.w));
-            if (x.x != y.x || x.y != y.y || x.z != y.z || x.w != y.w) { is_odd = true; *reinterpret_cast<uint4*>(from + row * BYTES + i) = y; }
-          }
+      if (row >= mine && row < valid) {
+        bool is_odd = false;
+        for (int i = 0; i < BYTES; i += 16) {              // (the places of a row's pieces do not matter here)
+          uint4 x = *reinterpret_cast<const uint4*>(from + row * BYTES + i);
+          const uint4 y = make_uint4(x.x & finite_parts<FMT>(x.x), x.y & finite_parts<FMT>(x.y), x.z & finite_parts<FMT>(x.z), x.w & finite_parts<FMT>(x.w));
+          if (x.x != y.x || x.y != y.y || x.z != y.z || x.w != y.w) { is_odd = true; *reinterpret_cast<uint4*>(from + row * BYTES + i) = y; }
         }
         if (is_odd) odd |= 1ull << (row - mine);
       }
@@ -262,7 +331,7 @@ struct Converter {
         const int local = (i0 + u) * (32 / LPR) + lane_row, row = warp * (ROWS / 4) + local;
         const uint4 x = in[u];
         uint4 a, b;
-        if constexpr (VALUES) {
+        if constexpr (VALUES && !is_tree<T>()) {
           const float s = __shfl_sync(0xFFFFFFFFu, scale, local);
           const uint2 y0 = codes_to_bf16x4<FMT>(x.x, s), y1 = codes_to_bf16x4<FMT>(x.y, s), y2 = codes_to_bf16x4<FMT>(x.z, s), y3 = codes_to_bf16x4<FMT>(x.w, s);
           a = make_uint4(y0.x, y0.y, y1.x, y1.y);
@@ -279,7 +348,15 @@ struct Converter {
     }
     if constexpr (!VALUES) {
       const uint32_t at = tile + t;
-      ex.key_scale[at % 8][warp * 32 + lane] = scale;
+      const int row = warp * 32 + lane;
+      ex.key_scale[at % 8][row] = scale;
+      if constexpr (is_tree<T>()) {
+        float s = value_scale;
+        if (row >= mine && row < valid && !(fabsf(s) < INFINITY)) { odd |= 1ull << (row - mine); s = 0.0f; }       // left out here, added with the output
+        const float l = s == 0.0f ? LEAST_VALUE_LOG2 : log2f(s);
+        values->log2[at % 8][row] = l < LEAST_VALUE_LOG2 ? LEAST_VALUE_LOG2 : l;
+        values->inverse[at % 8][row] = l < LEAST_VALUE_LOG2 ? exp2f(-LEAST_VALUE_LOG2) : exp2f(-l);
+      }
       warp_arrive(&ex.sc_full[at % 8]);
     }
     fence_proxy_async_smem();
@@ -292,20 +369,35 @@ struct Converter {
     return true;
   }
   __device__ __forceinline__ void item(const Item& it, int lag) {
-    // (a page is looked up two halves ahead, so that no warp waits for it to ask for its scale)
-    [[maybe_unused]] int page = page_of_key(it, 1, lag);
-    float next = is_tree<T>() ? scale_in(it, 0, lag, page_of_key(it, 0, lag)) : scale_of(it, 0, lag);
-    for (int h = 0; h < 2 * it.n; ++h) {
-      const float scale = next;
-      if constexpr (is_tree<T>()) {
-        next = scale_in(it, h + 1, lag, page);
-        page = page_of_key(it, h + 2, lag);
-      } else if (h + 1 < 2 * it.n) next = scale_of(it, h + 1, lag);
-      bool values;
-      int t;
-      half_of(h, it.n, lag, values, t);
-      const int valid = it.keys - (it.j0 + t) * TILE;
-      if (!(values ? convert<true>(t, scale, valid, valid - prm.c.q.w) : convert<false>(t, scale, valid))) break;
+    if constexpr (is_tree<T>()) {
+      // (a page is looked up two tiles ahead, so that no warp waits for it to ask for its scales)
+      int page = page_of_key(it, 1);
+      float2 next = scales_in(it, 0, page_of_key(it, 0));
+      for (int h = 0; h < 2 * it.n; ++h) {
+        bool is_values;
+        int t;
+        half_of(h, it.n, lag, is_values, t);
+        const int valid = it.keys - (it.j0 + t) * TILE, mine = valid - prm.c.q.w;
+        if (is_values) {
+          if (!convert<true>(t, 0.0f, valid, mine)) break;
+        } else {
+          const float2 s = next;
+          next = scales_in(it, t + 1, page);
+          page = page_of_key(it, t + 2);
+          if (!convert<false>(t, s.x, valid, mine, s.y)) break;
+        }
+      }
+    } else {
+      float next = scale_of(it, 0, lag);
+      for (int h = 0; h < 2 * it.n; ++h) {
+        const float scale = next;
+        if (h + 1 < 2 * it.n) next = scale_of(it, h + 1, lag);
+        bool is_values;
+        int t;
+        half_of(h, it.n, lag, is_values, t);
+        const int valid = it.keys - (it.j0 + t) * TILE;
+        if (!(is_values ? convert<true>(t, scale, valid) : convert<false>(t, scale, valid))) break;
+      }
     }
     tile += it.n;
   }
@@ -338,7 +430,7 @@ __device__ __forceinline__ void wait_operand(const Ctx2& cx, uint64_t* bar, uint
 template <int D, int FMT, bool PAIR>
 constexpr int extra_tree_at() { return FMT == FMT_BF16 ? Off<Cfg<D, PAIR>>::TOTAL : Off8<Cfg8<D, PAIR>>::EXTRA + (int)sizeof(Extra8); }
 template <int D, int FMT, bool PAIR, class T>
-constexpr int smem_bytes() { return extra_tree_at<D, FMT, PAIR>() + (is_tree<T>() ? (int)sizeof(ExtraTree) : 0); }
+constexpr int smem_bytes() { return extra_tree_at<D, FMT, PAIR>() + (is_tree<T>() ? (int)sizeof(ExtraTree) + (FMT != FMT_BF16 ? (int)sizeof(ExtraValues) : 0) : 0); }
 
 // tensor maps: tm_q (rows of a kv-head, 64 x 128); bf16 (boxes of 64 d): tm_k (64 entries of a pair or 128), tm_v (128); 8 bits: codes of 128
 // entries, of a pair 64 entries of the keys and 64 columns of the values.  Rows behind the end
@@ -370,6 +462,7 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
   Misc2& mi = *cx.mi;
   Extra8& ex = *reinterpret_cast<Extra8*>(smem + Off8<Cfg8<D, PAIR>>::EXTRA);       // (8-bit formats)
   [[maybe_unused]] ExtraTree& et = *reinterpret_cast<ExtraTree*>(smem + extra_tree_at<D, FMT, PAIR>());
+  [[maybe_unused]] ExtraValues& ev = *reinterpret_cast<ExtraValues*>(smem + extra_tree_at<D, FMT, PAIR>() + sizeof(ExtraTree));
   if (tid == 0) {
     if constexpr (TREE) { mbar_init(&et.fix_go, 1); mbar_init(&et.fix_done, 4); mbar_init(&et.odd_full, 4); }
     // Four converting warps, and the peer's word, in the place of a copy.  Test hook: the second message, of a CTA with one item the last, asks
@@ -613,7 +706,7 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
 #pragma unroll 1
             for (int b = first; b <= last; ++b) {
               if constexpr (Q8) {
-                constexpr uint32_t idesc = make_idesc_bf16_f32(TILE * NCTA, D, false, true);
+                constexpr uint32_t idesc = TREE ? make_idesc_f16_f32(TILE * NCTA, D, true) : make_idesc_bf16_f32(TILE * NCTA, D, false, true);
                 const uint32_t tO = cx.tmem + C::TM_O + b * D, tP = cx.tmem + C::TM_P + b * 64;
                 if (t < step) { is.wait_read_out(b); is.blocks ^= 1u << b; }
                 const uint32_t par = full_par(is.tiles >> b);
@@ -648,7 +741,7 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
     const uint32_t lane_sel = static_cast<uint32_t>((warp & 3) * 32) << 16;
     uint32_t nd = 0, nq = 0, no[2] = {0, 0};
     using Conv = Converter<Cfg8<D, PAIR>, Q8 ? FMT : FMT_INT8, T>;
-    Conv conv(cx, prm, ex, smem + Off8<Cfg8<D, PAIR>>::RAW, warp - WARP_EPI, tid & 31, tr);
+    Conv conv(cx, prm, ex, smem + Off8<Cfg8<D, PAIR>>::RAW, warp - WARP_EPI, tid & 31, tr, &ev);
     [[maybe_unused]] uint32_t values_used = 0, fixes = 0, odd_items = 0;
     while (true) {
       const Desc d = next_desc<C>(cx, nd, true);
@@ -815,7 +908,10 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
 #pragma unroll
               for (int i = 0; i < 4; ++i) hk.seen[i] = columns_seen(sees, first, 32 * i);
             }
-            if (i > 0 && !hk.tail) softmax_tile<D, false>(tS, tP, tO, TILE, false, scale_log2, st, hk);
+            if constexpr (Q8) {
+              const uint32_t at = (tile + t) % 8;
+              softmax_codes_tile<D>(tS, tP, tO, i == 0, scale_log2, st, hk, ex.key_scale[at], ev.log2[at], ev.inverse[at]);
+            } else if (i > 0 && !hk.tail) softmax_tile<D, false>(tS, tP, tO, TILE, false, scale_log2, st, hk);
             else softmax_tile<D, true>(tS, tP, tO, TILE, i == 0, scale_log2, st, hk);
           } else if (i > 0 && vis >= TILE) softmax_tile<D, false>(tS, tP, tO, TILE, false, scale_log2, st, hk);
           else softmax_tile<D, true>(tS, tP, tO, vis, i == 0, scale_log2, st, hk);

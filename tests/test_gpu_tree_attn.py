@@ -200,6 +200,30 @@ def test_logits_that_grow_along_the_cache(fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("B,w,Hq", [(2, 1, 8), (1, 6, 8), (3, 40, 8)])
+def test_values_of_any_size_beside_one_another(fmt, B, w, Hq):
+    """Values from 2^-20 to 2^20 and rows of zeros; keys that grow, so that the reference is raised again and again."""
+    Hkv, d, page, n = 2, 128, 32, 700
+    g = torch.Generator().manual_seed(40)
+    pages = (n + w + page - 1) // page
+    k, v = (torch.randn(pages, page, Hkv, d, generator=g) for _ in range(2))
+    at = torch.arange(pages * page).view(pages, page, 1, 1)
+    k, v = (k * (0.01 + 2.5 * at / n)).to(torch.bfloat16), (v * torch.exp2((at * 37 % 41 - 20).float()) * (at % 13 != 5)).to(torch.bfloat16)
+    cache = {"format": "bf16", "k": k.transpose(1, 2).contiguous().cuda(), "v": v.transpose(1, 2).contiguous().cuda()}
+    if fmt != "bf16":
+        cache = pc.kv_cache(pages, Hkv, page, d, fmt)
+        pc.kv_quantize(cache, k.cuda(), v.cuda())
+    q, table = _normal(41, B, w, Hq, d), torch.arange(pages, dtype=torch.int32, device="cuda").expand(B, pages)
+    got = pc.tree_attn(q.cuda(), cache, table, _i32([n] * B), want_lse=True)
+    held, parents = tree.values(cache), [tree.chain(w)] * B
+    want, want_lse = tree.attention(ref.f64(q), held, table.cpu().numpy(), [n] * B, parents, [0] * B, 0)
+    size, _ = tree.attention(ref.f64(q), (held[0], np.abs(held[1])), table.cpu().numpy(), [n] * B, parents, [0] * B, 0)
+    # weights rounded to bf16 (2^-9 each), the output once more
+    assert (np.abs(ref.f64(got["out"]) - want) <= 1.01 * 2.0 ** -8 * size + 2.0 ** -8 * np.abs(want)).all()
+    assert np.abs(got["lse"].cpu().numpy() - want_lse).max() <= 1e-4 + 1e-5 * np.abs(want_lse).max()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("w", [2, 30])
 def test_pages_and_lengths_that_are_none(fmt, w):
     """Page ids outside the pool are not followed, lengths beyond the table or max_len are no sequences; both are reported, other sequences are right."""
