@@ -102,12 +102,12 @@ inline PhasePlan few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format
 // Row groups and splits of the kernel for many rows: least time by a model in microseconds, as for the query windows - rounds
 // of the grid x (5 for an item + a tile), and the partial results through memory twice.  A tile has one price for all formats and head sizes, that of alt 1.2
 // (measured on CTA pairs at head size 128: bf16 0.9, codes 1.3); it weighs rounds against splits and no more.
-inline PhasePlan wide_plan(int64_t seqs, int64_t rows, int Hkv, int d, int n_keys, int sm_count, bool pairs = true) {
+inline PhasePlan wide_plan(int64_t seqs, int64_t rows, int Hkv, int d, int n_keys, int sm_count) {
   PhasePlan p = {};
   p.wide = true;
   // CTA pairs for more rows than a block has.  Measured, us, without / with, 65536 entries: 128 rows bf16 57.5 / 66.9, int8 72.8 / 91.6; 256 rows 78.8 / 73.0,
   // 127.3 / 96.7; 1024 rows 266.0 / 245.4, 314.7 / 268.1.
-  p.pair = pairs && d == 128 && rows > 128 && sm_count >= 2;
+  p.pair = d == 128 && rows > 128 && sm_count >= 2;
   const int64_t block = p.pair ? 256 : 128, blocks = (rows + block - 1) / block, units = p.pair ? sm_count / 2 : sm_count;
   const int tiles = (n_keys + 127) / 128;
   double least = -1.0;

@@ -12,7 +12,7 @@ namespace {
 
 constexpr int64_t MOST_OF_A_SEQUENCE = 1 << 28;
 constexpr int MOST_DRAFTED = 64;
-constexpr int LEAST_TILES = 4;                   // of a piece of a sequence's keys, many rows: an item costs some two tiles beside its own
+int least_tiles(int64_t seqs) { return seqs > 1 ? 4 : 1; }      // of a piece of a sequence's keys, many rows
 
 // a pool of pages and the sequences' tables
 int32_t check_pages(const pc_kv_cache* c, const int32_t* table, int64_t stride, int32_t n_table) {
@@ -115,16 +115,27 @@ PhasePlan tree_few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, 
   return p;
 }
 
-// Many rows: as wide_plan() on single CTAs; of several sequences, which may differ in length, pieces that are a small part of a CTA's work, drawn from the queue.
-PhasePlan tree_wide_plan(int64_t seqs, int64_t rows, int Hkv, int d, int n_keys, int sm_count) {
-  PhasePlan p = wide_plan(seqs, rows, Hkv, d, n_keys, sm_count, false);
-  if (seqs == 1) return p;
-  const double items = (double)seqs * Hkv * p.n_rg;
-  const int tiles = (n_keys + 127) / 128, most = (tiles + LEAST_TILES - 1) / LEAST_TILES, at_least = p.n_split;
-  double least = -1.0;
-  for (int s = std::min((int)std::ceil(4.0 * sm_count / items), most); s <= 1 + (int)std::ceil(8.0 * sm_count / items) && s <= most && s <= 64; ++s) {
-    const double t = std::ceil(items * s / sm_count) * (1.0 + std::ceil((double)tiles / s));            // rounds; an item takes a tile beside its own
-    if (s > at_least && (least < 0.0 || t < least)) { least = t; p.n_split = s; }
+// Many rows, on single CTAs: blocks of 128 rows, two of them to an item, or one whose key tiles go to either half of the CTA (alt), and pieces of the keys that are drawn
+// from a queue.  Least time by a model in us: a tile of two blocks 2.1 (head size 64: 1.55), of one 1.4 (1.1, the memory's rate), a tile more for each piece, the results of the
+// pieces through memory; of several sequences, whose lengths the host does not see, 0.6 of the longest's work and half of a piece for the end.  Measured, one sequence, 256 rows, 32768
+// entries, 18 pieces of two blocks / 9 of one: pages of 128 53.5 / 56.2, of 16 59.6 / 83.7, head size 64 46.3 / 51.9.
+PhasePlan tree_wide_plan(int64_t seqs, int64_t rows, int Hkv, int d, int n_keys, int sm_count, double& least) {
+  PhasePlan p = {};
+  p.wide = true;
+  const int64_t blocks = (rows + 127) / 128;
+  const int tiles = (n_keys + 127) / 128, most = (tiles + least_tiles(seqs) - 1) / least_tiles(seqs);
+  const double part = seqs > 1 ? 0.6 : 1.0;
+  least = -1.0;
+  for (int alt = blocks == 1 ? 1 : 0; alt <= 1; ++alt) {
+    const int64_t n_rg = alt ? blocks : (blocks + 1) / 2;
+    const double items = (double)seqs * Hkv * n_rg, tile = alt ? (d == 64 ? 1.1 : 1.4) : (d == 64 ? 1.55 : 2.1);
+    for (int s = 1; s <= most && s <= 64; ++s) {
+      const double rounds = items * s / sm_count, per = std::ceil((double)tiles / s);
+      double t = (double)seqs * rows * Hkv * s * part * d * 8.0 / 4.0e6;
+      if (rounds <= 1.0 || seqs == 1) t += std::ceil(rounds) * (per + 1.0) * tile;
+      else t += part * rounds * (per + 1.0) * tile + 0.5 * per * tile;
+      if (least < 0.0 || t < least) { least = t; p.alt = alt; p.n_rg = (int)n_rg; p.n_split = s; }
+    }
   }
   return p;
 }
@@ -142,11 +153,11 @@ int32_t tree_plan(const pc_tree_attn_args* a, int sm_count, TreePlan& p) {
   const int n_keys = a->max_len + a->w;
   double few_us;
   p.phase = tree_few_plan(a->B, rows, c->Hkv, c->d, c->format, n_keys, sm_count, few_us);
-  const PhasePlan many = tree_wide_plan(a->B, rows, c->Hkv, c->d, n_keys, sm_count);
-  // Many rows on the kernel for many where it takes less time: three launches and its start 15.5 us (head size 128: 17.5), a tile and CTA 1.75 to 2.4 us, over codes
-  // 2.9 to 5.7; by short CTAs as pc_cache_attn.
-  const double tile_us = bf16 ? (c->d == 64 ? 1.75 : 1.95) * (rows > 128 ? 1.25 : 1.0) : (c->d == 64 ? 2.9 : 4.2) * (rows > 128 ? 1.35 : 1.0);
-  const double wide_us = (c->d == 64 ? 15.5 : 17.5) + tile_us * std::ceil((a->B > 1 ? 0.6 : 1.0) * a->B * c->Hkv * many.n_rg * ((n_keys + 127) / 128) / sm_count);
+  double wide_us;
+  const PhasePlan many = tree_wide_plan(a->B, rows, c->Hkv, c->d, n_keys, sm_count, wide_us);
+  // Many rows on the kernel for many where it takes less time: three launches and its start some 15 us, and over codes, where conversions bound a tile, 1.9 times the plan's;
+  // by short CTAs as pc_cache_attn.
+  wide_us = 15.0 + (bf16 ? 1.0 : 1.9) * wide_us;
   bool wide = p.phase.brief ? rows > (!bf16 ? 48 : c->d == 128 || (double)a->B * c->Hkv > 2.0 * sm_count ? 16 : 32) : rows > 8 && wide_us < few_us;
   if (wide) p.phase = many;
   p.halves = wide && !bf16;
@@ -219,7 +230,7 @@ int32_t pc_tree_attn(const pc_tree_attn_args* a, void* stream) {
   tree.pages = pages_of(c, a->table, a->table_stride, a->n_table);
   tree.lens = a->lens; tree.parents = a->parents; tree.parent_stride = a->parents_stride;
   tree.max_len = a->max_len;
-  tree.least_tiles = LEAST_TILES;
+  tree.least_tiles = least_tiles(a->B);
   tree.turn = a->rope_theta > 0.0f;
   if (tree.turn) turns_of(a->rope_theta, c->d, tree.turns);
   tree.k = static_cast<const uint8_t*>(c->k); tree.v = static_cast<const uint8_t*>(c->v);

@@ -676,6 +676,9 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
             if constexpr (Q8) commit<C>(&mi.kv_free[is.k++ % C::NK]);
             else is.free_k();
           }
+          if constexpr (TREE) {                                // the queries are free behind the last product that reads them: the next item's come under this one's end
+            for (uint32_t i = is.nq - (!alt && d.n[1] > 0 ? 2 : 1); i != is.nq; ++i) commit<C>(&mi.q_free[i % NQ]);
+          }
         }
         commit<C>(&mi.mma_done);
       }
@@ -817,7 +820,7 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
           l = f[0] * lb[0] + f[1] * lb[1];
         }
         tc_fence_after_sync();
-        if (r == 0) mbar_arrive(&mi.q_free[nq % NQ]);                        // every MMA that reads the query slot has completed
+        if (!TREE && r == 0) mbar_arrive(&mi.q_free[nq % NQ]);               // every MMA that reads the query slot has completed
         ++nq;
         const int row = first_row(d.h[0], b0, rank) + r;
         const bool valid = row < rows;
