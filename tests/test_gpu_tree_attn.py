@@ -298,9 +298,11 @@ def test_pages_beyond_2_31_elements():
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-@pytest.mark.parametrize("B,w,Hq,Hkv,d,n,code", [(1, 1, 8, 2, 128, 1500, 411), (4, 1, 8, 2, 64, 2000, 411), (160, 1, 2, 2, 128, 70, 411)])
+@pytest.mark.parametrize("B,w,Hq,Hkv,d,n,code", [(1, 1, 8, 2, 128, 1500, 411), (4, 1, 8, 2, 64, 2000, 411), (160, 1, 2, 2, 128, 70, 411),
+                                                   (1, 32, 32, 8, 128, 12000, 101), (1, 32, 32, 8, 64, 12000, 101)])
 def test_a_wait_that_runs_out_is_reported(fmt, B, w, Hq, Hkv, d, n, code):
-    """The kernels wait for one arrival that nobody makes, with nothing in flight: 2e6 cycles, about a millisecond."""
+    """The kernels wait for one arrival that nobody makes, with nothing in flight: 2e6 cycles, about a millisecond.  (Many rows: the message that there is no
+    more work, behind the one item of each CTA.)"""
     lib = pc.load_library()
     cache, table = tree.pool(pc, 21, B, [n] * B, w, Hkv, 32, d, fmt, spoil=False)
     q, lens = _normal(22, B, w, Hq, d).cuda(), _i32([n] * B)
