@@ -103,7 +103,7 @@ struct WidePhase {
 // maps: rows of queries (box 64 x 128 rows; halves for 8-bit formats), keys (128, of a pair 64 entries) and values (128)
 cudaError_t launch_cache_wide(const CUtensorMap* maps, const WidePhase& p, int format, int d, bool pair, int sm_count, cudaStream_t st);
 
-// Joins the slots of a row and the new tokens' own keys.  alone: a warp for each row however many slots it has, for many rows.
-cudaError_t launch_cache_merge(const CacheMerge& p, int d, cudaStream_t st, bool alone = false);
+// Joins the slots of a row and the new tokens' own keys.
+cudaError_t launch_cache_merge(const CacheMerge& p, int d, cudaStream_t st);
 
 }  // namespace pc

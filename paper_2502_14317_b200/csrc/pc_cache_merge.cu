@@ -72,13 +72,13 @@ cudaError_t launch_cache_rows(const CacheRows& p, int d, cudaStream_t st) {
 }
 namespace {
 template <int D>
-cudaError_t merge_t(const CacheMerge& p, bool alone, cudaStream_t st) {
+cudaError_t merge_t(const CacheMerge& p, cudaStream_t st) {
   const long long rows = (long long)p.q.Hkv * p.total_rows;
   // a row's chain of slots and keys is shared by four warps where it is long
-  if (!alone && (p.n_slots > 4 || p.q.w > 8)) return launch_chained(cache_merge_kernel<D, 4>, dim3((unsigned)rows), dim3(128), 0, st, 1, p);
+  if (p.n_slots > 4 || p.q.w > 8) return launch_chained(cache_merge_kernel<D, 4>, dim3((unsigned)rows), dim3(128), 0, st, 1, p);
   return launch_chained(cache_merge_kernel<D, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, 1, p);
 }
 }  // namespace
-cudaError_t launch_cache_merge(const CacheMerge& p, int d, cudaStream_t st, bool alone) { return d == 128 ? merge_t<128>(p, alone, st) : merge_t<64>(p, alone, st); }
+cudaError_t launch_cache_merge(const CacheMerge& p, int d, cudaStream_t st) { return d == 128 ? merge_t<128>(p, st) : merge_t<64>(p, st); }
 
 }  // namespace pc

@@ -53,6 +53,8 @@ cudaError_t launch_tree_few(const CUtensorMap& tm_k, const CUtensorMap& tm_v, co
                             bool brief, int format, int d, cudaStream_t st);
 // The kernel for many rows (pc_tree_wide.cu): as launch_cache_wide() on single CTAs.
 cudaError_t launch_tree_wide(const CUtensorMap* maps, const WidePhase& p, const TreePhase& t, int format, int d, int sm_count, cudaStream_t st);
+// Joins the slots of a row (pc_tree_prepare.cu).
+cudaError_t launch_tree_merge(const CacheMerge& p, int d, int sm_count, cudaStream_t st);
 // Rows into memory, rotated, and t.sees; clears as cache_rows_kernel does (pc_tree_prepare.cu).
 cudaError_t launch_tree_rows(const CacheRows& p, const TreePhase& t, int d, cudaStream_t st);
 

@@ -285,8 +285,7 @@ int32_t pc_tree_attn(const pc_tree_attn_args* a, void* stream) {
     }
   }
   if (e != cudaSuccess || ph.finish) return launched(e);
-  // a warp for each row where there are enough of them to fill the GPU, else four
-  return launched(pc::launch_cache_merge(merge, c->d, st, plan.n_slots <= 4 || plan.total_rows * c->Hkv > 16 * sms));
+  return launched(pc::launch_tree_merge(merge, c->d, sms, st));
 }
 
 int32_t pc_token_logprobs(const pc_token_logprobs_args* a, void* stream) {

@@ -495,13 +495,14 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
         const int lane_to = part * 16384 + (lane_box << tr.log_box) * ROW;
         Prod p;
         uint32_t raws = 0;                                 // uses of the raw slots
-        while (true) {
-          int item = n_items;
-          if (lane == 0 && !*cx.abort_flag) item = next_item<C>(cx, p, true, prm.counter, n_items);
+        for (bool first_item = true;; first_item = false) {
+          int item = n_items;                              // (the first without asking the queue)
+          if (lane == 0 && !*cx.abort_flag) item = first_item ? (int)blockIdx.x : (int)gridDim.x + atomicAdd(prm.counter, 1);
           item = __shfl_sync(0xFFFFFFFFu, item, 0);
           if (item >= n_items) break;
           const Item it = decode_item(prm, tr, item);
           if (it.n == 0) continue;                           // (its slots say so already)
+          PageIds ids(tr, it, lane);
           if (lane == 0) {
             Desc d;
             d.kind = KIND_FLASH;
@@ -522,7 +523,6 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
             }
           }
           __syncwarp();
-          PageIds ids(tr, it, lane);
           for (int h = 0; h < 2 * it.n; ++h) {
             bool values;
             int t;

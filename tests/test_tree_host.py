@@ -163,7 +163,7 @@ def _short(name):
     few = re.search(r"tree_few_kernel.*3FewILi\d+ELi\dELi(\d)ELb(\d)E", name)
     if few:
         return ("short" if few.group(2) == "1" else "few") + str(8 * int(few.group(1)))
-    return "wide" if "tree_wide_kernel" in name else "rows" if "tree_rows_kernel" in name else "merge" if "cache_merge_kernel" in name else name
+    return "wide" if "tree_wide_kernel" in name else "rows" if "tree_rows_kernel" in name else "merge" if "_merge_kernel" in name else name
 
 
 def launched(lib, c, fmt):
