@@ -131,6 +131,35 @@ def test_a_temperature(scale):
     _check(x, t, 10, pc.token_logprobs(x, t, top=10, want_entropy=True, scale=scale), scale)
 
 
+@pytest.mark.parametrize("type", TYPES)
+@pytest.mark.parametrize("scale", [2.0 ** -100, 1e-20, 1e6, 1e30, 2.0 ** 100])
+def test_temperatures_far_from_one(type, scale):
+    """Scaled logits that are all the same to fp32, and ones whose products with scale * log2 e pass the largest number (a greedy choice by temperature)."""
+    x, t = _rows(24, 5, 9001, type), _tokens(25, 5, 9001)
+    x[1] *= 50.0
+    x[2, 4000] = 6e4
+    if type != "fp16":
+        x[3] = (x[3].float() * 1e9).to(x.dtype)
+        x[4] = (x[4].float() * 1e37).to(x.dtype)
+    x, (want, entropy, ids, lp) = x.contiguous(), tree.logprobs(_f64(x), t.cpu().numpy(), 6, float(np.float32(scale)))
+    got = pc.token_logprobs(x, t, top=6, want_entropy=True, scale=scale)
+    assert np.array_equal(got["top_id"].cpu().numpy(), ids)
+    # as in _check; what is below the lowest number is -inf, and where the largest logit is alone the entropy's sum is less than the least number
+    for a, b in ((got["logprob"], want), (got["top_logprob"], lp), (got["entropy"], entropy)):
+        a, far = _f64(a), np.abs(b) > 3.4e38
+        assert np.isneginf(a[far]).all() and not np.isnan(a).any()
+        assert (np.abs(a - b)[~far] <= ((9001 / 512 + 48) * 2.0 ** -24 * (2 + 2 * np.minimum(np.abs(b), 20)) + 2.0 ** -21 * np.abs(b))[~far]).all()
+
+
+def test_logits_that_lie_further_apart_than_the_largest_number():
+    x = torch.full((2, 5000), -3e38, device="cuda")
+    x[:, 17], x[1, 4999] = 3e38, 2.9e38
+    got = pc.token_logprobs(x, torch.tensor([3, 4999], dtype=torch.int32, device="cuda"), top=2, scale=0.125, want_entropy=True)
+    assert got["top_id"].tolist() == [[17, 0], [17, 4999]] and got["top_logprob"][:, 0].tolist() == [0.0, 0.0] and got["entropy"].tolist() == [0.0, 0.0]
+    want = -(torch.tensor([6e38, 0.1e38], dtype=torch.float64) * 0.125)
+    assert ((got["logprob"].cpu().double() - want).abs() <= 2.0 ** -18 * want.abs()).all()          # (the second: a difference of two that are rounded, 2^-24 of 3e38)
+
+
 def test_groups_and_tokens_that_are_none():
     """Sums over groups, a row that adds nothing, a token behind the last; what is not asked for is not there."""
     C, w, V = 5, 37, 3001
