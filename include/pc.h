@@ -513,8 +513,8 @@ PC_API int32_t pc_cache_attn(const pc_cache_attn_args* args, void* stream);
  *   parents  device int32 [B,n], n <= 64: drafted tokens, as in pc_tree_attn: token j is rotated to the position of its depth, entry by
  *            entry they stand one behind the other; a token that is not there leaves its entry as it was.  Not with pick.
  * A sequence whose first entry is negative is left out.  An entry beyond the table is not written, code 421.  8-bit formats: as pc_kv_quantize, from
- * the fp32 rotation.  k, v [B,n (n_src),Hkv,d] bf16 through element strides (sequence, token, head; 0,0,0 -> contiguous), multiples of 8.  An entry
- * that is named twice in one call holds one of the two.
+ * the fp32 rotation.  k, v [B,n (n_src),Hkv,d] bf16 through element strides (sequence, token, head; 0,0,0 -> contiguous), multiples of 8;
+ * they may not lie in the pool.  Of an entry that is named twice in one call (by two sequences that share a page) the values are undefined.  Hkv <= 2^18 - 4.
  */
 typedef struct {
   int32_t B, n, n_src, at0, pos0, n_table;
@@ -542,6 +542,7 @@ PC_API int32_t pc_page_append(const pc_page_append_args* args, void* stream);
  * near the longest plans the launch best.
  * What a mask hides, what stands behind a sequence's end and in pages that it does not name does not reach a row, whatever it holds, NaN included.
  * Precision as for pc_cache_attn.  q [B,w,Hq,d] through element strides; out [B,w,Hq,d] bf16, lse [B,Hq,w] fp32 (natural log; may be NULL) contiguous.
+ * The scales of 8-bit formats may not be negative (as pc_page_append and pc_kv_quantize leave them).  out and lse may not overlap what is read.
  * d, Hkv: the pool's; any Hq / Hkv, Hq <= 2^18, B * w * Hq <= 2^24.  Workspace: pc_tree_attn_workspace_bytes(args), aligned to 32 bytes; it reads
  * B, w, Hq, max_len and the pool's descriptor alone; 0: a bad argument.
  */
@@ -569,7 +570,8 @@ PC_API int32_t pc_tree_attn(const pc_tree_attn_args* args, void* stream);
 /* ------------------------------------------------------------------------------------
  * Log probabilities.  Paper: Eq. 3, I_c = -log P(X^q | X^c): with the logits of the query window behind every chunk, nll with group = w is the
  * chunk score that pc_select_chunks and pc_hot_path take.  And what a server needs of drafted tokens.
- * logits: N rows of V in fp32, bf16 or fp16, `stride` elements apart (0: one row for all), any alignment.  Of row i, z = scale * logits:
+ * logits: N rows of V in fp32, bf16 or fp16, `stride` elements apart (0: one row for all), any alignment.  2^-100 <= scale <= 2^100.
+ * Of row i, z = scale * logits:
  *   logprob[i]       z[tokens[i]] - log sum exp z (tokens: device int32 [N]; both NULL: not).  A token < 0 gets 0 (it adds nothing to a sum), >= V NaN
  *   entropy[i]       - sum p log p, natural log; NULL: not
  *   top_id, top_logprob [N,top]  the `top` <= 32 largest logits in descending order, equal ones by the lower index

@@ -51,7 +51,8 @@ int32_t pc_page_append(const pc_page_append_args* a, void* stream) {
   if (a->B < 1 || a->n < 1 || !a->k || !a->v || !aligned(a->k, 16) || !aligned(a->v, 16) || !good_theta(a->rope_theta)) return PC_ERR_INVALID_ARG;
   if (a->at == nullptr && (a->at0 < 0 || (int64_t)a->at0 + a->n > a->pages->capacity * a->n_table)) return PC_ERR_INVALID_ARG;
   if ((a->pick != nullptr && (a->parents != nullptr || a->n_src < 1 || a->pick_stride < 0)) || (a->parents != nullptr && a->parents_stride < 0)) return PC_ERR_INVALID_ARG;
-  if (a->n > MOST_OF_A_SEQUENCE || (a->parents != nullptr && a->n > MOST_DRAFTED) || a->B > (1 << 24)) return PC_ERR_UNSUPPORTED;
+  if (a->n > MOST_OF_A_SEQUENCE || (a->parents != nullptr && a->n > MOST_DRAFTED) || a->B > (1 << 24) || a->pages->Hkv > (1 << 18) - 4)
+    return PC_ERR_UNSUPPORTED;
   const pc_kv_cache* const c = a->pages;
   pc::PageWrite w = {};
   const int n_src = a->pick != nullptr ? a->n_src : a->n;
@@ -292,7 +293,7 @@ int32_t pc_token_logprobs(const pc_token_logprobs_args* a, void* stream) {
   if (a == nullptr || a->type < PC_LOGITS_F32 || a->type > PC_LOGITS_F16) return PC_ERR_INVALID_ARG;
   const int bytes = a->type == PC_LOGITS_F32 ? 4 : 2;
   if (a->N < 1 || a->V < 1 || a->top < 0 || a->top > a->V || a->group < 0 || !a->logits || !aligned(a->logits, bytes) || a->stride < 0) return PC_ERR_INVALID_ARG;
-  if (!(a->scale > 0.0f) || !std::isfinite(a->scale) || (a->logprob != nullptr) != (a->tokens != nullptr)) return PC_ERR_INVALID_ARG;
+  if (!(a->scale >= 7.8886091e-31f) || a->scale > 1.2676506e30f || (a->logprob != nullptr) != (a->tokens != nullptr)) return PC_ERR_INVALID_ARG;
   if ((a->top > 0 && (!a->top_logprob || !a->top_id)) || (a->top == 0 && !a->logprob && !a->entropy)) return PC_ERR_INVALID_ARG;
   if (a->nll != nullptr && (a->group < 1 || a->N % a->group != 0 || !a->logprob)) return PC_ERR_INVALID_ARG;
   if (a->top > PC_MOST_ALTERNATIVES || a->V > (1 << 28) || a->N > (1 << 27)) return PC_ERR_UNSUPPORTED;

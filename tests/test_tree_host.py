@@ -118,6 +118,17 @@ def test_log_probabilities_that_are_refused(lib, change, code):
     assert lib.pc_token_logprobs(None, None) == INVALID
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -101, 1e-38, 2.0 ** 100 * 1.001, 3e38])
+def test_temperatures_that_are_refused(lib, scale):
+    assert lib.pc_token_logprobs(byref(logprobs(scale=scale)), None) == INVALID
+
+
+def test_more_heads_than_a_launch_has(lib):
+    pool = cache(B=1, capacity=16)
+    pool.Hkv = 2 ** 18 - 3
+    assert lib.pc_page_append(byref(append(pages=pool, n_table=1)), None) == UNSUPPORTED
+
+
 @pytest.mark.skipif(torch.cuda.is_available(), reason="would launch")
 def test_a_call_in_order_asks_for_the_gpu(lib):
     assert lib.pc_page_append(byref(append()), None) == UNSUPPORTED
@@ -184,8 +195,8 @@ def test_kernels_of_a_call(names, call, fmt):
 
 def test_the_calls_reach_every_build(names):
     seen = {n for c in CALLS for fmt in FORMATS for n in launched(names, c, fmt)}
-    every = {n for n in names.fake_known().decode().split("\n") if re.search("tree_(few|wide|rows)_kernel", n)}
-    assert len(every) == 32 and every == {n for n in seen if "tree_" in n}, sorted(every - seen)
+    every = {n for n in names.fake_known().decode().split("\n") if re.search("tree_(few|wide|rows|merge)_kernel", n)}
+    assert len(every) == 36 and every == {n for n in seen if "tree_" in n}, sorted(every - seen)
 
 
 # ---------------------------------------------------------------- the plain forms of the GPU tests
