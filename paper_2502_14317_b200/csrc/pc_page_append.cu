@@ -4,6 +4,7 @@
 // at a time, keys as four elements of either half, so that a lane has whole pairs and the angles of its four pairs serve all heads.  The angles are
 // computed where they are used (pc_tree.cuh): a table of them would be read as often as the rows of one head.  16 (head size 64: 32) consecutive
 // tokens of a block write 4 KB that lie together, if their page does not end.  A key that goes into 8 bits is not rounded to bf16 before.
+// Measured: 65537 tokens of 8 heads of 128 in bf16 (537 MB) 85 to 88 us = 6.3 to 6.1 TB/s; one token 2.6 us as a graph, in a loop of calls 4.4 (the host).
 #include "pc_kernels.h"
 #include "pc_kv8.cuh"
 #include "pc_tree.cuh"

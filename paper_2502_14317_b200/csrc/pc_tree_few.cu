@@ -1,8 +1,13 @@
 // Attention of few query rows of drafted tokens over pages (pc_tree_attn): the body of pc_cache_few.cu, up to 16 rows of a kv-head at a time.
 //
-// A box of the producer's copies is a page, or as much of one as a tile has: a lane issues each, with the page that it looked up a tile ahead, so that
-// pages of 16 entries take the same time as whole tiles (16 lanes, 2 KB each).  The last w entries of a sequence are its new tokens; a unit that
-// holds any is masked by the rows' words of ancestors, which every CTA makes itself from the parents (some 400 cycles, under the first copies).
+// A box of the producer's copies is a page, or as much of one as a tile has: a lane issues each.  The ids of 64 pages lie in its warp's registers; looked up tile by tile,
+// a load that the copies wait for, 64 sequences of up to 16384 int8 entries took 1.7 times as long.  Small boxes are slower than whole tiles: over 16400 bf16
+// entries 25.5 us with pages of 16, 20.9 with pages of 64 (cp.async of 16 bytes in place of the boxes 30.2).  The last w entries of a sequence are its new tokens;
+// a unit that holds any is masked by the rows' words of ancestors, which every CTA makes itself from the parents (some 400 cycles, under the first copies).
+//
+// Bound by reading the pages, with few sequences by latencies: 64 sequences of 7700 to 16384 int8 entries (1.1 GB), 32/8 heads of 128, 215 to 229 us = 5.1 to 4.8 TB/s (the
+// copies' conversions and an end in which only the longest sequences are left); one sequence of 16400 bf16 entries (67 MB) 20 us: some 8 for the start, rows
+// and join, then a tile at a time.
 #include "pc_few.cuh"
 
 namespace pc {

@@ -20,6 +20,7 @@ def _calls():
         yield Call(4, 40, 8, 2, d, 64, 6000, True, ["rows", "wide", "merge"])            # two blocks of rows
         yield Call(8, 30, 8, 2, d, 16, 5000, False, ["rows", "wide", "merge"])           # one
         yield Call(6, 64, 12, 2, d, 256, 2500, True, ["rows", "wide", "merge"])          # three
+        yield Call(10, 64, 16, 2, d, 64, 1500, True, ["rows", "wide", "merge"])          # more rows than the join takes one a warp
 
 
 CALLS = list(_calls())
