@@ -18,7 +18,7 @@
 //
 // Bound, many rows, by the exponentials and the issue of instructions beside the reading: at 1024 x 128256 in bf16 with 8 alternatives (263 MB) the exponentials' unit
 // is busy for 65 %, issue 70, memory 63: 54 us = 4.9 TB/s; without alternatives 6 us less, with 32 of them 11 more.  276 rows of 50001 in fp16 whose pitch is odd
-// 12 us as a graph; one row of 128256 in fp32 with 20 alternatives 8.5, a chain of latencies.
+// 12 us; one row of 128256 in fp32 with 20 alternatives 8.5, a chain of latencies.
 #include "pc_kernels.h"
 #include "pc_logprob.h"
 #include "pc_rank.cuh"
@@ -484,10 +484,14 @@ __global__ void __launch_bounds__(128) group_nll_kernel(const float* logprob, in
 
 namespace {
 template <int TYPE>
-cudaError_t logprobs_t(const LogProb& p, int split, cudaStream_t st) {
+cudaError_t logprobs_t(const LogProb& p, int split, int sm_count, cudaStream_t st) {
   static_assert(CTAS * (sizeof(Shared) + 1024) <= 233472, "CTAs per SM");
-  if (cudaError_t e = cudaFuncSetAttribute(token_logprobs_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared)); e != cudaSuccess) return e;
-  return launch_chained(token_logprobs_kernel<TYPE>, dim3((unsigned)((long long)p.N * split)), dim3(NT), sizeof(Shared), st, split, p, split);
+  const long long ctas = (long long)p.N * split, each = (ctas + sm_count - 1) / sm_count;
+  // Two or three CTAs an SM: no SM takes more.  CTAs that start while the kernel ahead still runs would go where there is room, four to some SMs and none to
+  // others.  Measured, 276 / 300 / 400 rows of 50001 in fp16, one call behind the other, 12.1 / 15.3 / 16.0 us against 15.0 / 18.3 / 19.1 with room for four everywhere.
+  const size_t smem = each == 2 || each == 3 ? 233472 / (size_t)each - 1024 : sizeof(Shared);
+  if (cudaError_t e = cudaFuncSetAttribute(token_logprobs_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
+  return launch_chained(token_logprobs_kernel<TYPE>, dim3((unsigned)ctas), dim3(NT), smem, st, split, p, split);
 }
 }  // namespace
 
@@ -496,7 +500,9 @@ cudaError_t launch_token_logprobs(const LogProb& p, int type, int sm_count, cuda
   // 13.7 / 11.1 / 10.2 / 10.7, 64 13.8 / 11.3 / 11.6 / 13.5, 148 14.8 / 15.8 / 23.0 / 31.5; one row of 8000 6.3 / 7.5 / 8.0 / 8.2, 64 of 50001 in fp16 9.9 / 9.7 / 10.2 / 11.9.
   int split = 1;
   while (split < 8 && (long long)p.N * split * 2 <= sm_count && p.V / (2 * split) >= 6000) split *= 2;
-  cudaError_t e = type == LOGITS_F32 ? logprobs_t<LOGITS_F32>(p, split, st) : type == LOGITS_BF16 ? logprobs_t<LOGITS_BF16>(p, split, st) : logprobs_t<LOGITS_F16>(p, split, st);
+  cudaError_t e = type == LOGITS_F32    ? logprobs_t<LOGITS_F32>(p, split, sm_count, st)
+                  : type == LOGITS_BF16 ? logprobs_t<LOGITS_BF16>(p, split, sm_count, st)
+                                        : logprobs_t<LOGITS_F16>(p, split, sm_count, st);
   if (e != cudaSuccess || p.nll == nullptr) return e;
   const int groups = p.N / p.group;
   return launch_chained(group_nll_kernel, dim3((unsigned)((groups + 3) / 4)), dim3(128), 0, st, 1, (const float*)p.logprob, groups, p.group, p.nll);
