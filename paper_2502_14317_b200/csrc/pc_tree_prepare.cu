@@ -16,11 +16,15 @@ __global__ void __launch_bounds__(256) tree_rows_kernel(const __grid_constant__ 
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = p.Hq / p.Hkv;
   const int seq = blockIdx.x / p.w, i = blockIdx.x - seq * p.w;
   const double part = threadIdx.x < D / 2 ? part_of_turn(t.turns, threadIdx.x) : 0.0;
-  chain();
+  // as chain(), but what is cleared is so before the next kernel starts: that looks at lengths and pages before it waits for this one, and may have a code to leave
+  cudaGridDependencySynchronize();
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
     if (p.clear != nullptr) p.clear[0] = p.clear[1] = 0;
     if (p.clear_too != nullptr) *p.clear_too = 0;
+    __threadfence();
   }
+  __syncthreads();
+  cudaTriggerProgrammaticLaunchCompletion();
   uint32_t x[4][E / 2];
 #pragma unroll
   for (int u = 0; u < 4; ++u) {

@@ -480,7 +480,7 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
   if constexpr (PAIR) cluster_sync_all();
   tc_fence_after_sync();
   cx.tmem = mi.tmem_base;
-  chain();
+  if (!TREE || warp != WARP_PRODUCER) chain();
 
   if (warp >= WARP_PRODUCER) {
     setmaxnreg_dec<REGS_PARALLEL.service>();
@@ -501,8 +501,24 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
           item = __shfl_sync(0xFFFFFFFFu, item, 0);
           if (item >= n_items) break;
           const Item it = decode_item(prm, tr, item);
-          if (it.n == 0) continue;                           // (its slots say so already)
+          if (it.n == 0) {                                   // (its slots say so already)
+            if (first_item) chain();
+            continue;
+          }
           PageIds ids(tr, it, lane);
+          auto queries = [&]() {
+            if (lane == 0) {
+              for (int b = 0; b < (!alt && first_row(it.rg, 1, 0) < rows ? 2 : 1); ++b) {
+                const int qs = p.q % NQ;
+                WAIT2(&mi.q_free[qs], free_par(p.q / NQ), W2_QFREE);
+                mbar_arrive_expect_tx(&mi.q_full[qs], C::Q_BYTES);
+                for (int a = 0; a < C::ATOMS; ++a)           // (rows behind the last are zeros and count as copied)
+                  load_box<C>(cx.sQ + qs * C::Q_BYTES + a * 16384, &tm_q, smem_u32(&mi.q_full[qs]), a * 64, it.seq * rows + first_row(it.rg, b, 0), it.hkv, 0);
+                ++p.q;
+              }
+            }
+            __syncwarp();
+          };
           if (lane == 0) {
             Desc d;
             d.kind = KIND_FLASH;
@@ -512,18 +528,13 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
             d.n[0] = alt ? (it.n + 1) / 2 : it.n;
             d.n[1] = alt ? it.n / 2 : (first_row(it.rg, 1, 0) < rows ? it.n : 0);
             publish<C>(cx, p, d);
-            for (int b = 0; b < (alt ? 1 : 2); ++b) {
-              if (d.n[b] == 0) continue;
-              const int qs = p.q % NQ;
-              WAIT2(&mi.q_free[qs], free_par(p.q / NQ), W2_QFREE);
-              mbar_arrive_expect_tx(&mi.q_full[qs], C::Q_BYTES);
-              for (int a = 0; a < C::ATOMS; ++a)             // (rows behind the last are zeros and count as copied)
-                load_box<C>(cx.sQ + qs * C::Q_BYTES + a * 16384, &tm_q, smem_u32(&mi.q_full[qs]), a * 64, it.seq * rows + first_row(it.rg, b, 0), it.hkv, 0);
-              ++p.q;
-            }
           }
-          __syncwarp();
+          // The first item's first copies go out before the rows are made: all that stands before the launch for the rows is done when that lets this one
+          // start.  (64 tokens of one sequence over 32768 entries 52.6 -> 51.1 us.)
+          const int early = first_item ? lag + 1 < 2 * it.n ? lag + 1 : 2 * it.n : 0;
+          if (!first_item) queries();
           for (int h = 0; h < 2 * it.n; ++h) {
+            if (first_item && h == early) { chain(); queries(); }
             bool values;
             int t;
             half_of(h, it.n, lag, values, t);
@@ -557,6 +568,7 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
                           page_checked(tr.pages, id, cx.status));
             __syncwarp();
           }
+          if (first_item && early == 2 * it.n) { chain(); queries(); }
         }
         if (lane == 0) {
           Desc d;
