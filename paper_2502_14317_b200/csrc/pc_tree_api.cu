@@ -84,28 +84,33 @@ struct TreePlan {
   size_t off_counter, off_sees, off_halves, off_scale, off_rows, off_ml, off_o, total;
 };
 
-// Few rows: splits of the keys, as few_plan() but for sequences whose lengths may differ and whose copies go by pages.  Least time by a model in us: 7.5 for a CTA's
-// start and join; its tiles, at what a CTA takes for one alone on an SM or beside another, or at the memory's rate (of several sequences, whose lengths the host does not
-// see, as if they had 0.6 of the longest's); beyond a round of the GPU what all have to read, 2 to 4 a round and half of a longest piece for the end, where
-// only the longest sequences are left; slots 1.5 + 0.05 a split.
+// Few rows: splits of the keys, as few_plan() but for sequences whose lengths may differ and whose copies go by pages.  Least time by a model in us, fitted to 1500 measured times (1 to 64
+// sequences of 1500 to 120000 entries, 4 to 48 rows of 2 and 8 kv-heads, 1 to 64 splits; off by 8 % on average, and the splits that it chooses by 0.7 % of the best): 6.7 for a CTA's start and
+// join, 2 more for 16 rows; its tiles, at what a unit of 16 keys takes a warp of a CTA alone on an SM or beside another, or at the memory's rate (of several sequences, whose lengths the
+// host does not see, as if they had 0.53 of the longest's); beyond a round of the GPU the launch for the rows, what all have to read, 5 to 6 a round and a third of a longest piece for
+// the end, where only the longest sequences are left; slots 1.25 + 0.03 a split.
 PhasePlan tree_few_plan(int64_t seqs, int64_t rows, int Hkv, int d, int format, int n_keys, int sm_count, double& least) {
   PhasePlan p = few_plan(seqs, rows, Hkv, d, format, n_keys, true, sm_count);
   least = -1.0;
   if (p.brief) return p;
+  const bool bf16 = format == PC_KV_BF16;
   const int keys = pc::few_keys(format, d, false), tiles = (n_keys + keys - 1) / keys;
-  const double items = (double)seqs * Hkv * p.n_rg, bytes = 2.0 * keys * (format == PC_KV_BF16 ? 2 * d : d + 4) / 6.5e6;        // of a tile, us
-  const double units = keys / 16 / (p.group == 8 || d == 64 ? 7.0 : 5.0) * (p.group == 8 ? 1.0 : 1.4);
-  const double alone = (format == PC_KV_BF16 ? 1.05 : 0.8) * units, beside = (format == PC_KV_BF16 ? 1.6 : 1.1) * units;
-  const double part = seqs > 1 ? 0.6 : 1.0, round_us = format == PC_KV_BF16 ? 2.0 : 4.0;
+  static const double unit_us[2][2][2][2] = {{{{0.47, 0.53}, {0.71, 0.85}}, {{1.03, 1.52}, {0.86, 1.18}}},            // 8 rows, head size 64: bf16, codes; 128
+                                             {{{0.50, 0.66}, {0.78, 1.14}}, {{1.09, 1.19}, {1.10, 1.25}}}};           // 16
+  const auto& us = unit_us[p.group == 16][d == 128][!bf16];
+  const double units = keys / 16 / (p.group == 8 || d == 64 ? 7.0 : 5.0), alone = us[0] * units, beside = us[1] * units;
+  const double items = (double)seqs * Hkv * p.n_rg, bytes = 2.0 * keys * (bf16 ? 2 * d : d + 4) / 7.3e6 / p.n_rg;           // of a tile, us (row groups share it)
+  const double part = seqs > 1 ? 0.53 : 1.0, round_us = bf16 ? 4.6 : 6.0, start = p.group == 8 ? 6.7 : 8.7;
   auto look = [&](int s, bool finish) {
-    const double fit = 2.0 * sm_count, ctas = items * s, per = std::ceil((double)tiles / s);
-    double t = 7.5 + (finish ? 0.0 : 1.5 + 0.05 * s);
+    const double fit = 2.0 * sm_count, ctas = items * s, most = std::ceil((double)tiles / s), mean = (double)tiles / s;
+    const double per = seqs > 1 ? 0.2 * most + 0.8 * mean : most;
+    double t = start + (finish ? 0.0 : 1.25 + 0.03 * s);
     if (ctas <= fit) {
-      const double tile = ctas <= sm_count ? alone : beside;
-      t += per * (tile > part * bytes * ctas ? tile : part * bytes * ctas);
+      const double work = per * (ctas <= sm_count ? alone : beside), read = (seqs > 1 ? per : mean) * part * bytes * ctas;
+      t += work > read ? work : read;
     } else {
       const double tile = beside > bytes * fit ? beside : bytes * fit;
-      t += part * items * tiles * tile / fit + round_us * (ctas / fit - 1.0) + 0.5 * per * beside;
+      t += 7.9 + part * items * tiles * tile / fit + round_us * (ctas / fit - 1.0) + 0.3 * per * beside;
     }
     if (least < 0.0 || t < least) { least = t; p.n_split = s; p.finish = finish; }
   };
@@ -156,9 +161,10 @@ int32_t tree_plan(const pc_tree_attn_args* a, int sm_count, TreePlan& p) {
   p.phase = tree_few_plan(a->B, rows, c->Hkv, c->d, c->format, n_keys, sm_count, few_us);
   double wide_us;
   const PhasePlan many = tree_wide_plan(a->B, rows, c->Hkv, c->d, n_keys, sm_count, wide_us);
-  // Many rows on the kernel for many where it takes less time: three launches and its start some 15 us, and over codes, where conversions bound a tile, 1.9 times the plan's;
-  // by short CTAs as pc_cache_attn.
-  wide_us = 15.0 + (bf16 ? 1.0 : 1.9) * wide_us;
+  // Many rows on the kernel for many where it takes less time: its launches and start some 10, and what the plan's tiles take beside 16 to 48 rows of which a block has 128 (over codes
+  // conversions bound a tile); by short CTAs as pc_cache_attn.  Measured, few / many, 16 rows: one sequence of 120000 bf16 entries, head size 64, 22 / 33, 64 of up to 6000 31 / 58; 48 rows: 16 of
+  // up to 6000, head size 128, 98 / 63, int8 105 / 97.
+  wide_us = c->d == 128 ? (bf16 ? 12.0 + 1.1 * wide_us : 9.5 + 1.85 * wide_us) : (bf16 ? 10.5 + 1.3 * wide_us : 9.5 + 1.75 * wide_us);
   bool wide = p.phase.brief ? rows > (!bf16 ? 48 : c->d == 128 || (double)a->B * c->Hkv > 2.0 * sm_count ? 16 : 32) : rows > 8 && wide_us < few_us;
   if (wide) p.phase = many;
   p.halves = wide && !bf16;

@@ -16,7 +16,8 @@ def _calls():
         yield Call(160, 2, 16, 2, d, 32, 100, True, ["short16"])
         yield Call(310, 1, 4, 2, d, 16, 90, True, ["rows", "short8"])
         yield Call(300, 2, 16, 2, d, 16, 90, True, ["rows", "short16"])
-        yield Call(40, 1, 32, 4, d, 128, 3000, True, ["rows", "few8", "merge"])
+        slots = ["rows", "few8", "merge"]
+        yield Call(40, 1, 32, 4, d, 128, 3000, True, slots if d == 128 else {"bf16": ["few8"], "8 bits": slots})
         yield Call(4, 40, 8, 2, d, 64, 6000, True, ["rows", "wide", "merge"])            # two blocks of rows
         yield Call(8, 30, 8, 2, d, 16, 5000, False, ["rows", "wide", "merge"])           # one
         yield Call(6, 64, 12, 2, d, 256, 2500, True, ["rows", "wide", "merge"])          # three
