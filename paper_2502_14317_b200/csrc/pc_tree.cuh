@@ -16,13 +16,14 @@ __device__ __forceinline__ double part_of_turn(const Turns& u, int t) {
   return c * f;
 }
 // (cos, sin) of the angle of position p.  p times the fp64 part of a turn is off by 2^-53 of itself, and what is left of it without whole turns
-// goes to fp32: off by 2^-25 of a turn, whatever the position.  Three fp64 operations; sine and cosine are fp32's.
+// goes to fp32 in two parts, the second, under 2^-25 of a turn, as a step along the circle: what is left is the error of fp32's sine and cosine, whatever the
+// position.  (Without the second part 2.8 % of random calls had a query's element on the other side of a border between two bf16 numbers than in 64 bits, with it 1.8 %.)
 __device__ __forceinline__ float2 turned(double per, long long p) {
-  const double x = per * (double)p;
-  const float f = (float)(x - rint(x));
-  float2 r;
-  sincospif(2.0f * f, &r.y, &r.x);
-  return r;
+  const double x = per * (double)p, y = x - rint(x);
+  const float f = (float)y, step = (float)(y - (double)f) * 6.2831853f;
+  float s, c;
+  sincospif(2.0f * f, &s, &c);
+  return make_float2(fmaf(-s, step, c), fmaf(c, step, s));
 }
 
 __device__ __forceinline__ int page_of(const Pages& p, int e) { return (int)((unsigned long long)(unsigned)e * p.mul >> p.shift); }

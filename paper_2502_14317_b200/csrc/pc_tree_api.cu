@@ -84,7 +84,7 @@ struct TreePlan {
   size_t off_counter, off_sees, off_halves, off_scale, off_rows, off_ml, off_o, total;
 };
 
-// Few rows: splits of the keys, as few_plan() but for sequences whose lengths may differ and whose copies go by pages.  Least time by a model in us, fitted to 1500 measured times (1 to 64
+// Few rows: splits of the keys, as few_plan() but for sequences whose lengths may differ and whose copies go by pages.  Least time by a model in us, fitted to 2458 measured times (1 to 64
 // sequences of 1500 to 120000 entries, 4 to 48 rows of 2 and 8 kv-heads, 1 to 64 splits; off by 8 % on average, and the splits that it chooses by 0.7 % of the best): 6.7 for a CTA's start and
 // join, 2 more for 16 rows; its tiles, at what a unit of 16 keys takes a warp of a CTA alone on an SM or beside another, or at the memory's rate (of several sequences, whose lengths the
 // host does not see, as if they had 0.53 of the longest's); beyond a round of the GPU the launch for the rows, what all have to read, 5 to 6 a round and a third of a longest piece for
