@@ -5,7 +5,7 @@
 // shared memory before the product takes them.  Single CTAs, not pairs: what the pair shares is the keys, which the two blocks of an item share already.
 // A tile of 128 keys takes 2.05 to 2.35 us of two blocks, the softmax of 256 rows and the matrix products one behind the other, and 1.4 of one block, the rate at
 // which its copies come.  Around it 20 us that do not depend on the keys: rows kernel 5, the CTA's start, slots and their join 6 to 10.
-// Measured, 32/8 heads of 128, bf16: 64 tokens of one sequence over 32768 entries (134 MB) 51 to 54 us; 40 tokens of each of 16 sequences of up to 12000 entries
+// Measured, 32/8 heads of 128, bf16: 64 tokens of one sequence over 32768 entries (134 MB) 51 to 57 us; 40 tokens of each of 16 sequences of up to 12000 entries
 // 134 to 152 (160 rows cost what 256 do).  Codes: one stage of converted keys, 4 to 5 us a tile.
 #include "pc_wide.cuh"
 
