@@ -74,11 +74,14 @@ struct __align__(16) ExtraTree {
   uint64_t fix_go, fix_done, odd_full;
   unsigned long long odd[2][4];
 };
-// TREE, 8 bits: of a tile's values log2 of the scales and their inverses (softmax_codes_tile); they stay as long as the keys' scales
+// TREE, 8 bits: of a tile's values log2 of the scales and their inverses (softmax_codes_tile), and for each of the converting warps' quarters of the tile whether a scale
+// is not between 2^-40 and 2^40; they stay as long as the keys' scales.  sums: as lm of Misc2, [block][maximum / sum][row], weights_apart.
 struct __align__(16) ExtraValues {
   float log2[8][TILE], inverse[8][TILE];
+  uint8_t far[8][4];
+  float sums[2][2][TILE];
 };
-constexpr float LEAST_VALUE_LOG2 = -100.0f;                      // of scales that are 0 or next to it: their entries' values are nothing, their weights count
+constexpr float NEAR_VALUE = 0x1p40f;
 template <class T>
 __device__ __forceinline__ bool tail_tile(const T& tr, const WidePhase& p, int keys, int j) {       // whether tile j has new tokens or less than 128 entries
   if constexpr (is_tree<T>()) return (j + 1) * TILE > keys - p.c.q.w;
@@ -228,6 +231,30 @@ __device__ __forceinline__ void softmax_codes_tile(uint32_t s_taddr, uint32_t p_
   unpack_f32x2(add_f32x2(sum2[0], sum2[1]), a0, a1);
   st.l += a0 + a1;
 }
+// The weights of a tile's keys by themselves, from z and relative to their own maximum.  2^(z' - m) is 0 below 2^-126, and with it the weight of a key whose value is that
+// much smaller than another's, or zeros.  While all scales are between 2^-40 and 2^40 those are weights below 2^-46 of the row's; from an item's first tile with another
+// scale on a row is summed here, by another 128 exponentials (16 tokens of 16 sequences of up to 12000 int8 entries, 32/8 heads of 128: 163 us, with a row of zeros in four 219).
+static __device__ __noinline__ float2 weights_apart(uint32_t s_taddr, float scale_log2, float m, float l, const float* key_scale, bool tail, uint4 seen) {
+#pragma unroll 1
+  for (int i = 0; i < 4; ++i) {
+    uint32_t c[32];
+    tmem_ld32(s_taddr + 32 * i, c);
+    tmem_wait_ld();
+    loaded(c);
+    const uint32_t bits = !tail ? 0xFFFFFFFFu : i == 0 ? seen.x : i == 1 ? seen.y : i == 2 ? seen.z : seen.w;
+#pragma unroll
+    for (int j = 0; j < 32; ++j) {
+      const float z = __uint_as_float(c[j]) * (key_scale[32 * i + j] * scale_log2);
+      c[j] = bits >> j & 1 ? __float_as_uint(z) : 0xFF800000u;
+    }
+    const float top = fmaxf(m, max32(c)), base = top == -INFINITY ? 0.0f : top;
+    l = m == -INFINITY ? 0.0f : l * fast_exp2(m - base);
+#pragma unroll
+    for (int j = 0; j < 32; ++j) l += fast_exp2(__uint_as_float(c[j]) - base);
+    m = top;
+  }
+  return make_float2(m, l);
+}
 
 // Halves (keys or values of a tile) of an item's n tiles in the order in which the issuers want them: K of the first `lag` tiles, then
 // V of tile t, K of tile t + lag.
@@ -352,10 +379,13 @@ struct Converter {
       ex.key_scale[at % 8][row] = scale;
       if constexpr (is_tree<T>()) {
         float s = value_scale;
-        if (row >= mine && row < valid && !(fabsf(s) < INFINITY)) { odd |= 1ull << (row - mine); s = 0.0f; }       // left out here, added with the output
-        const float l = s == 0.0f ? LEAST_VALUE_LOG2 : log2f(s);
-        values->log2[at % 8][row] = l < LEAST_VALUE_LOG2 ? LEAST_VALUE_LOG2 : l;
-        values->inverse[at % 8][row] = l < LEAST_VALUE_LOG2 ? exp2f(-LEAST_VALUE_LOG2) : exp2f(-l);
+        if (row >= mine && row < valid && !(fabsf(s) < INFINITY)) { odd |= 1ull << (row - mine); s = 1.0f; }       // added with the output: whatever is summed here
+        const bool near = s >= 1.0f / NEAR_VALUE && s <= NEAR_VALUE;
+        const float l = log2f(s);                          // (zeros: -infinity.  What is no number must not raise the reference.)
+        values->log2[at % 8][row] = s < INFINITY ? l : __int_as_float(0x7FC00000);
+        values->inverse[at % 8][row] = near ? exp2f(-l) : 0.0f;
+        const bool far = __any_sync(0xFFFFFFFFu, !near && row < valid);
+        if (lane == 0) values->far[at % 8][warp] = far;
       }
       warp_arrive(&ex.sc_full[at % 8]);
     }
@@ -814,6 +844,7 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
         float m = -INFINITY, f[2] = {0.0f, 0.0f}, l = 0.0f;
         {
           float mb[2] = {-INFINITY, -INFINITY}, lb[2] = {0.0f, 0.0f};
+          [[maybe_unused]] float ms[2] = {-INFINITY, -INFINITY}, ls[2] = {0.0f, 0.0f};             // weights by themselves
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
             const int b = alt ? i : b0;
@@ -822,14 +853,21 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
             WAIT2(&mi.lm_full[b], full_par(ph), W2_LM);
             mb[i] = mi.lm[b][0][r];
             lb[i] = mi.lm[b][1][r];
+            if constexpr (TREE && Q8) { ms[i] = ev.sums[b][0][r]; ls[i] = ev.sums[b][1][r]; }
             warp_arrive(&mi.lm_free[b]);
             WAIT2S(&mi.o_full[b], full_par(ph), W2_OFULL);
             if (b) ++no[1]; else ++no[0];
           }
           m = fmaxf(mb[0], mb[1]);
+          if constexpr (TREE && Q8) m = fmaxf(m, fmaxf(ms[0], ms[1]));
 #pragma unroll
           for (int i = 0; i < 2; ++i) f[i] = mb[i] == -INFINITY ? 0.0f : fast_exp2(mb[i] - m);
           l = f[0] * lb[0] + f[1] * lb[1];
+          if constexpr (TREE && Q8) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              if (ms[i] != -INFINITY) l = fmaf(fast_exp2(ms[i] - m), ls[i], l);
+          }
         }
         tc_fence_after_sync();
         if (!TREE && r == 0) mbar_arrive(&mi.q_free[nq % NQ]);               // every MMA that reads the query slot has completed
@@ -897,25 +935,12 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
           if (row < rows) scale_log2 = __ldg(prm.half_scale + (size_t)d.hkv * prm.c.total_rows + (size_t)d.c * rows + row);
         }
         RowState st = {-INFINITY, 0.0f};
+        [[maybe_unused]] float2 sums = make_float2(-INFINITY, 0.0f);             // weights by themselves
         // TREE: a warp whose rows are behind the last only keeps the barriers going; what P and the accumulator hold for it reaches no row
         [[maybe_unused]] const bool idle = TREE && first_row(d.h[0], b, rank) + (r & ~31) >= rows;
-#pragma unroll 1
-        for (int i = 0; i < n; ++i) {
-          const int t = alt ? 2 * i + b : i, j = d.t[0] + t, vis = d.h[1] - j * TILE;                  // ragged last tile
-          WAIT2S(&mi.s_full[b], full_par(n_s), W2_SFULL);
-          ++n_s;
-          if constexpr (Q8) {
-            const uint32_t at = tile + t;
-            WAIT2S(&ex.sc_full[at % 8], full_par(at / 8), W2_KVFULL);
-            hk.scale = ex.key_scale[at % 8];
-          }
-          tc_fence_after_sync();
-          if (TREE && idle) {
-            hk.on_read();
-            hk.before_p();
-            hk.on_half();
-            hk.on_full();
-          } else if constexpr (TREE) {
+        // TREE: tile j has new tokens: which columns the row sees
+        [[maybe_unused]] auto look_at = [&](int j) {
+          if constexpr (TREE) {
             hk.tail = tail_tile(tr, prm, d.h[1], j);
             if (hk.tail) {
               const int row = first_row(d.h[0], b, rank) + r, first = d.h[1] - prm.c.q.w - j * TILE;
@@ -923,19 +948,72 @@ __device__ __forceinline__ void wide_body(const CUtensorMap& tm_q, const CUtenso
 #pragma unroll
               for (int i = 0; i < 4; ++i) hk.seen[i] = columns_seen(sees, first, 32 * i);
             }
+          }
+        };
+        if constexpr (TREE && Q8) {
+          // Tiles up to the first whose values' scales lie far from 1, and the rest, in loops of their own: the call in the first one's loop cost 3 to 5 % of the time.
+          int i = 0;
+          auto tiles = [&](auto by_themselves) {
+            constexpr bool APART = decltype(by_themselves)::value;
+#pragma unroll 1
+            for (; i < n; ++i) {
+              const int t = alt ? 2 * i + b : i, at = (tile + t) % 8;
+              WAIT2S(&mi.s_full[b], full_par(n_s), W2_SFULL);
+              WAIT2S(&ex.sc_full[at], full_par((tile + t) / 8), W2_KVFULL);
+              if (!APART && !idle && *reinterpret_cast<const uint32_t*>(ev.far[at]) != 0) return;
+              ++n_s;
+              tc_fence_after_sync();
+              if (idle) {
+                hk.on_read();
+                hk.before_p();
+                hk.on_half();
+                hk.on_full();
+              } else {
+                look_at(d.t[0] + t);
+                if constexpr (APART)
+                  sums = weights_apart(tS, scale_log2, sums.x, sums.y, ex.key_scale[at], hk.tail, make_uint4(hk.seen[0], hk.seen[1], hk.seen[2], hk.seen[3]));
+                softmax_codes_tile<D>(tS, tP, tO, i == 0, scale_log2, st, hk, ex.key_scale[at], ev.log2[at], ev.inverse[at]);
+              }
+              ++hk.tiles;
+            }
+          };
+          tiles(std::false_type());
+          if (i < n) {
+            sums = make_float2(st.m, st.l);                      // (of the tiles before)
+            tiles(std::true_type());
+            st.l = 0.0f;
+          }
+        } else {
+#pragma unroll 1
+          for (int i = 0; i < n; ++i) {
+            const int t = alt ? 2 * i + b : i, j = d.t[0] + t, vis = d.h[1] - j * TILE;                  // ragged last tile
+            WAIT2S(&mi.s_full[b], full_par(n_s), W2_SFULL);
+            ++n_s;
             if constexpr (Q8) {
-              const uint32_t at = (tile + t) % 8;
-              softmax_codes_tile<D>(tS, tP, tO, i == 0, scale_log2, st, hk, ex.key_scale[at], ev.log2[at], ev.inverse[at]);
-            } else if (i > 0 && !hk.tail) softmax_tile<D, false>(tS, tP, tO, TILE, false, scale_log2, st, hk);
-            else softmax_tile<D, true>(tS, tP, tO, TILE, i == 0, scale_log2, st, hk);
-          } else if (i > 0 && vis >= TILE) softmax_tile<D, false>(tS, tP, tO, TILE, false, scale_log2, st, hk);
-          else softmax_tile<D, true>(tS, tP, tO, vis, i == 0, scale_log2, st, hk);
-          ++hk.tiles;
+              const uint32_t at = tile + t;
+              WAIT2S(&ex.sc_full[at % 8], full_par(at / 8), W2_KVFULL);
+              hk.scale = ex.key_scale[at % 8];
+            }
+            tc_fence_after_sync();
+            if (TREE && idle) {
+              hk.on_read();
+              hk.before_p();
+              hk.on_half();
+              hk.on_full();
+            } else if constexpr (TREE) {
+              look_at(j);
+              if (i > 0 && !hk.tail) softmax_tile<D, false>(tS, tP, tO, TILE, false, scale_log2, st, hk);
+              else softmax_tile<D, true>(tS, tP, tO, TILE, i == 0, scale_log2, st, hk);
+            } else if (i > 0 && vis >= TILE) softmax_tile<D, false>(tS, tP, tO, TILE, false, scale_log2, st, hk);
+            else softmax_tile<D, true>(tS, tP, tO, vis, i == 0, scale_log2, st, hk);
+            ++hk.tiles;
+          }
         }
         WAIT2S(&mi.lm_free[b], free_par(n_blk), W2_LMFREE);
         ++n_blk;
         mi.lm[b][0][r] = st.m;
         mi.lm[b][1][r] = st.l;
+        if constexpr (TREE && Q8) { ev.sums[b][0][r] = sums.x; ev.sums[b][1][r] = sums.y; }
         warp_arrive(&mi.lm_full[b]);
       }
       tile += d.t[1];

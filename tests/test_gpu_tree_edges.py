@@ -1,0 +1,122 @@
+"""Attention of drafted tokens over paged caches at its edges, on both kernels: positions before the first, values that are no number, values of any size."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2502_14317_b200 as pc
+from tests import cache_ref as ref
+from tests import tree_ref as tree
+from tests.tree_edges import SHAPES
+
+pytestmark = pytest.mark.gpu
+FORMATS = ["bf16", "int8", "e4m3"]
+NAN, INF = float("nan"), float("inf")
+
+
+def _normal(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16)
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _room(table, page, most):
+    """the table with room for `most` entries, by pages that are none, which no sequence comes to"""
+    more = max((most + page - 1) // page - table.shape[1], 0)
+    return torch.cat([table, torch.full((len(table), more), -7, dtype=torch.int32, device="cuda")], 1)
+
+
+# size of every seventh entry's values and of the others', as powers of two; every `zeros`-th row is zeros
+SIZES = [(0, 0, 2), (20, 20, 2), (28, 28, 3), (60, 60, 2), (60, -60, 3), (100, 100, 5), (100, 0, 3), (100, -95, 4), (0, -95, 5000), (-60, -60, 2), (-92, -92, 3),
+         (-97, -97, 5000), (-99, -99, 2)]
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,w,Hq,most,kernel", SHAPES[1:4])
+def test_sizes_of_values_weigh_nothing(fmt, d, B, w, Hq, most, kernel):
+    """An entry's weight is its key's, however large or small its value is, zeros among them, and the output is right relative to its own size."""
+    Hkv, page, n = 2, 64, 900
+    g = torch.Generator().manual_seed(60)
+    pages = (n + w + page - 1) // page
+    k, x = (torch.randn(pages, page, Hkv, d, generator=g) for _ in range(2))
+    q = _normal(61, 1, w, Hq, d)
+    table = _room(torch.arange(pages, dtype=torch.int32, device="cuda").view(1, pages), page, most + w).expand(B, -1)
+    k, at = (k * 0.7).to(torch.bfloat16).cuda(), torch.arange(pages * page).view(pages, page, 1, 1)
+    for big, rest, zeros in SIZES:
+        v = (x * torch.exp2(torch.where(at % 7 == 3, float(big), float(rest))) * (at % zeros != 1)).to(torch.bfloat16)
+        cache = pc.kv_cache(pages, Hkv, page, d, fmt)
+        pc.kv_quantize(cache, k, v.cuda())
+        got = pc.tree_attn(q.cuda().expand(B, -1, -1, -1), cache, table, _i32([n] * B), max_len=most, want_lse=True)
+        held = tree.values(cache)
+        want, want_lse = tree.attention(ref.f64(q), held, table.cpu().numpy(), [n], [tree.chain(w)], [0], 0)
+        size, _ = tree.attention(ref.f64(q), (held[0], np.abs(held[1])), table.cpu().numpy(), [n], [tree.chain(w)], [0], 0)
+        # Weights rounded to bf16 or halves (2^-9 at most), the output to bf16 (2^-9): twice that.  What a half loses below 2^-14 of the largest product, 2^-25 of
+        # 448 codes for 900 entries, is 2^-6 of a code, of sums of at least 100 that large ones have: 2^-12 of them.
+        off, room = np.abs(ref.f64(got["out"]) - want), 1.01 * 2.0 ** -8 * size + 2.0 ** -8 * np.abs(want)
+        assert (off <= room).all(), ((big, rest, zeros), np.nanmax(off / room))
+        off = np.abs(got["lse"].cpu().numpy() - want_lse)
+        assert (off <= 1e-4 + 1e-5 * np.abs(want_lse)).all(), ((big, rest, zeros), off.max())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("B,w,Hq,most,kernel", SHAPES[1:])
+@pytest.mark.parametrize("n", [0, 100, 128, 1000])
+def test_new_tokens_that_are_no_number_stay_where_they_are_seen(fmt, B, w, Hq, most, kernel, n):
+    """Values and keys of drafted tokens that are no number: only the rows that see them have them, an infinity keeps its sign."""
+    d, G = 128, Hq // 2
+    lens = [max(n - b, 0) for b in range(B)]
+    cache, table = tree.pool(pc, 54, B, lens, w, 2, 16, d, fmt)
+    g = np.random.default_rng(55)
+    parents = [[int(g.integers(max(-1, i - 4), i)) for i in range(w)] for _ in range(B)]
+    q = _normal(56, B, w, Hq, d).cuda()
+    call = lambda: pc.tree_attn(q, cache, _room(table, 16, most + w), _i32(lens), parents=_i32(parents), max_len=most, want_lse=True)       # noqa: E731
+    clean, paths = call(), [tree.seen(p) for p in parents]
+    was, lse = ref.f64(clean["out"]), clean["lse"].cpu().numpy()
+    b, value, key = B - 1, min(w - 1, 2), w // 2
+    at = lambda i: (int(table[b, (lens[b] + i) // 16]), (lens[b] + i) % 16)                             # noqa: E731
+    (p0, e0), (p1, e1) = at(value), at(key)
+    columns = list(range(d))
+    if fmt == "bf16":
+        cache["v"][p0, 1, e0, 7], cache["v"][p0, 1, e0, 8], cache["k"][p1, 0, e1, 3] = -INF, NAN, NAN
+        columns = [7, 8]
+    elif fmt == "int8":
+        cache["v_scale"][p0, 1, e0], cache["k_scale"][p1, 0, e1] = NAN, NAN
+    else:
+        cache["v"].view(torch.uint8)[p0, 1, e0, 8], cache["k"].view(torch.uint8)[p1, 0, e1, 3] = 0xFF, 0x7F
+        columns = [8]
+    got = call()
+    out, sees = ref.f64(got["out"]), [i for i in range(w) if value in paths[b][i]]
+    if fmt == "bf16":
+        assert np.isneginf(out[b][sees][:, G:, 7]).all()
+    assert np.isnan(out[b][sees][:, G:][:, :, [8]]).all() and (len(columns) < d or np.isnan(out[b][sees][:, G:]).all())
+    for i in sees:
+        out[b][i, G:, columns] = was[b][i, G:, columns]
+    for i in range(w):
+        if key in paths[b][i]:
+            assert np.isnan(out[b][i, :G]).all() and np.isnan(got["lse"][b, :G, i].cpu().numpy()).all()
+            out[b][i, :G] = was[b][i, :G]
+    assert np.array_equal(out, was)
+    assert np.array_equal(got["lse"].cpu().numpy()[:, G:], lse[:, G:]) or np.abs(got["lse"].cpu().numpy() - lse)[:, G:].max() <= 264 * 2.0 ** -24 + 2.0 ** -18
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 48), (128, 256)])
+@pytest.mark.parametrize("B,w,Hq,most,kernel", SHAPES[2:])
+def test_many_rows_over_short_sequences(fmt, d, page, B, w, Hq, most, kernel):
+    """The kernel for many rows where pieces, tiles and pages end: no entries, a few, a tile and its neighbours; sequences and tokens that are not there."""
+    lens = [0, 1, 127 - w, 128, 129, -1, 700, 1100][:B]
+    cache, table = tree.pool(pc, 57, B, lens, w, 2, page, d, fmt)
+    g = np.random.default_rng(58)
+    parents = [[int(g.integers(max(-1, i - 4), i)) for i in range(w)] for _ in range(B)]
+    parents[1] = [p if i < w // 3 else -2 for i, p in enumerate(parents[1])]
+    q = _normal(59, B, w, Hq, d)
+    got = pc.tree_attn(q.cuda(), cache, _room(table, page, most + w), _i32(lens), parents=_i32(parents), max_len=most, want_lse=True)
+    assert got["status"].item() == 0
+    want, want_lse = tree.attention(ref.f64(q), tuple(np.nan_to_num(x) for x in tree.values(cache)), table.cpu().numpy(), lens, parents, [0] * B, 0)
+    there, lse, out = np.isfinite(want_lse), got["lse"].cpu().numpy(), ref.f64(got["out"])
+    assert np.array_equal(there, np.isfinite(lse)) and (lse[~there] == -INF).all()
+    # weights and, over codes, nothing else to bf16 or halves: 2 * 2^-9 of sum p |v| <= 4.5, the output half a step
+    assert (np.abs(out - want) <= 1.8e-2 + 2.0 ** -8 * np.abs(want)).all()
+    assert (np.abs(lse - want_lse)[there] <= 1e-4 + 1e-5 * np.abs(want_lse[there])).all()
