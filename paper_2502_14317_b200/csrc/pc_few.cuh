@@ -442,8 +442,8 @@ __device__ __forceinline__ void few_body(const CUtensorMap& tm_k, const CUtensor
             unsigned long long odd = 0;
             auto out = [&](int key) { if (key >= mine && key < left) odd |= 1ull << (key - mine); };
             if constexpr (Q8) {
-              if (!(fabsf(sv0) < INFINITY)) { out(g); sv0 = 0.0f; }
-              if (!(fabsf(sv1) < INFINITY)) { out(g + 8); sv1 = 0.0f; }
+              if (g >= mine && !(fabsf(sv0) < INFINITY)) { out(g); sv0 = 0.0f; }
+              if (g + 8 >= mine && !(fabsf(sv1) < INFINITY)) { out(g + 8); sv1 = 0.0f; }
             }
             if constexpr (FMT != FMT_INT8) {
 #pragma unroll

@@ -120,3 +120,31 @@ def test_many_rows_over_short_sequences(fmt, d, page, B, w, Hq, most, kernel):
     # weights and, over codes, nothing else to bf16 or halves: 2 * 2^-9 of sum p |v| <= 4.5, the output half a step
     assert (np.abs(out - want) <= 1.8e-2 + 2.0 ** -8 * np.abs(want)).all()
     assert (np.abs(lse - want_lse)[there] <= 1e-4 + 1e-5 * np.abs(want_lse[there])).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("B,w,Hq,most,kernel", SHAPES)
+def test_values_that_are_no_number_beside_the_new_tokens_reach_all(fmt, B, w, Hq, most, kernel):
+    """A value of the context that is no number reaches every row, wherever it stands: of 200 entries the last eight share a unit of 16, and those from 128 on a tile,
+    with the new tokens.  Weights do not depend on values: lse stays, and so does the other kv-head."""
+    q, parents, G = _normal(53, B, w, Hq, 64).cuda(), _i32([-1] + [0] * (w - 1)), Hq // 2
+    for n, spoiled in ((200, 89), (200, 150), (200, 191), (200, 192), (200, 199), (5, 0), (5, 4), (16, 15)):
+        cache, table = tree.pool(pc, 52, B, [n] * B, w, 2, 16, 64, fmt)
+        call = lambda c: pc.tree_attn(q, c, _room(table, 16, most + w), _i32([n] * B), parents=parents, max_len=most, want_lse=True)       # noqa: E731
+        clean = call(cache)
+        p, e, was = int(table[0, spoiled // 16]), spoiled % 16, ref.f64(clean["out"])
+        for what in (NAN, INF) + (("code",) if fmt == "e4m3" else ()):
+            spoil = {name: x.clone() if torch.is_tensor(x) else x for name, x in cache.items()}
+            if what == "code":
+                spoil["v"].view(torch.uint8)[p, 1, e, 5] = 0x7F
+            elif fmt == "bf16":
+                spoil["v"][p, 1, e] = what
+            else:
+                spoil["v_scale"][p, 1, e] = what
+            got = call(spoil)
+            out, hit = ref.f64(got["out"]), [5] if what == "code" else list(range(64))
+            assert not np.isfinite(out[0][:, G:, hit]).any(), (n, spoiled, what)
+            out[0][:, G:, hit] = was[0][:, G:, hit]
+            assert np.array_equal(out, was) and torch.equal(got["lse"][1:], clean["lse"][1:]) and torch.equal(got["lse"][0, :G], clean["lse"][0, :G]), (n, spoiled, what)
+            # sums of up to 264 positive terms in another order and with other roundings, 2^-24 each, of terms that fp32 exponents up to 2^5 make right to 2^-19
+            assert (got["lse"] - clean["lse"]).abs().max() <= 264 * 2.0 ** -24 + 2.0 ** -18, (n, spoiled, what)
