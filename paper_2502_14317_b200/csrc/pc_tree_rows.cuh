@@ -3,6 +3,7 @@
 #include "pc_cache_rows.cuh"
 #include "pc_kv8.cuh"
 #include "pc_tree.cuh"
+#include <climits>
 
 namespace pc {
 
@@ -41,7 +42,7 @@ struct TreeTurner {
   static constexpr int E = D / 32, H = E / 2;
   double per[H];
   float c[E], s[E];
-  long long pos = 0, held = -1;                               // position of the row that comes, and whose angles are held
+  long long pos = 0, held = LLONG_MIN;                        // position of the row that comes, and whose angles are held (no position is LLONG_MIN)
   bool turn;
   __device__ __forceinline__ TreeTurner(const TreePhase& t, int lane) : turn(t.turn != 0) {
 #pragma unroll

@@ -148,3 +148,21 @@ def test_values_that_are_no_number_beside_the_new_tokens_reach_all(fmt, B, w, Hq
             assert np.array_equal(out, was) and torch.equal(got["lse"][1:], clean["lse"][1:]) and torch.equal(got["lse"][0, :G], clean["lse"][0, :G]), (n, spoiled, what)
             # sums of up to 264 positive terms in another order and with other roundings, 2^-24 each, of terms that fp32 exponents up to 2^5 make right to 2^-19
             assert (got["lse"] - clean["lse"]).abs().max() <= 264 * 2.0 ** -24 + 2.0 ** -18, (n, spoiled, what)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("w,Hq,first", [(1, 4, -1), (1, 4, -2), (4, 4, -4), (3, 14, -2), (20, 8, -9)])
+def test_positions_before_the_first(fmt, d, w, Hq, first):
+    """pos0 + pos + depth may be any number, -1 among them: the rows get what queries that come rotated get."""
+    lens, theta = [50, 33], 1e4
+    cache, table = tree.pool(pc, 50, 2, lens, w, 2, 16, d, fmt)
+    q = _normal(51, 2, w, Hq, d)
+    at = np.array([[first + i for i in range(w)], [first + 3 + i for i in range(w)]])
+    border = tree.near_a_border(ref.f64(q), at, theta)                # no element that fp32 may round either way
+    q[torch.from_numpy(np.concatenate([border, border], -1))] = 0
+    turned = torch.from_numpy(ref.to_bf16(tree.turned(ref.f64(q), at, theta)).astype(np.float32)).to(torch.bfloat16)
+    want = pc.tree_attn(turned.cuda(), cache, table, _i32(lens), want_lse=True)
+    for pos, pos0 in (([first, first + 3], 0), ([0, 3], first)):
+        got = pc.tree_attn(q.cuda(), cache, table, _i32(lens), pos=_i32(pos), pos0=pos0, rope_theta=theta, want_lse=True)
+        assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
