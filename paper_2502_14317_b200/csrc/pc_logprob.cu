@@ -490,7 +490,8 @@ cudaError_t logprobs_t(const LogProb& p, int split, int sm_count, cudaStream_t s
   // Two or three CTAs an SM: no SM takes more.  CTAs that start while the kernel ahead still runs would go where there is room, four to some SMs and none to
   // others.  Measured, 276 / 300 / 400 rows of 50001 in fp16, one call behind the other, 12.1 / 15.3 / 16.0 us against 15.0 / 18.3 / 19.1 with room for four everywhere.
   const size_t smem = each == 2 || each == 3 ? 233472 / (size_t)each - 1024 : sizeof(Shared);
-  if (cudaError_t e = cudaFuncSetAttribute(token_logprobs_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem); e != cudaSuccess) return e;
+  constexpr int MOST = 233472 / 2 - 1024;                    // one number for all calls: another thread's call may come between this line and the launch
+  if (cudaError_t e = cudaFuncSetAttribute(token_logprobs_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST); e != cudaSuccess) return e;
   return launch_chained(token_logprobs_kernel<TYPE>, dim3((unsigned)ctas), dim3(NT), smem, st, split, p, split);
 }
 }  // namespace
