@@ -517,6 +517,15 @@ const int32_t* table_of(PyObject* p, int64_t B, int64_t n, at::Device device, in
   return static_cast<const int32_t*>(t.data_ptr());
 }
 
+// drafted tokens' parents: int32 [B,n], or [n] for all sequences (stride 0); null: None
+const int32_t* parents_of(PyObject* p, int64_t B, int64_t n, at::Device device, int64_t& stride, const char* why) {
+  at::Tensor t;
+  stride = 0;
+  if (!is_tensor(p, t, why) || t.dim() != 1) return table_of(p, B, n, device, stride, why);
+  need(t.size(0) == n && t.scalar_type() == at::kInt && t.device() == device && (t.stride(0) == 1 || n == 1), why);
+  return static_cast<const int32_t*>(t.data_ptr());
+}
+
 // page_append(run, stream, need_cuda, cache, k, v, table, at, pos, count, pick, parents, status, pos0, rope_theta) -> result code, or the reason of a refusal
 PyObject* page_append(PyObject*, PyObject* args) {
   HANDLE_TH_ERRORS
@@ -550,7 +559,7 @@ PyObject* page_append(PyObject*, PyObject* args) {
       a.n = (int32_t)t.size(1);
       a.pick = table_of(pick, B, -1, c.device, a.pick_stride, bad_pick);
     }
-    a.parents = table_of(parents, B, a.n, c.device, a.parents_stride, "parents must be int32 [B, n] with a contiguous last dimension, on the pages' device");
+    a.parents = parents_of(parents, B, a.n, c.device, a.parents_stride, "parents must be int32 [B, n] or [n] with a contiguous last dimension, on the pages' device");
     need(a.parents == nullptr || a.pick == nullptr, "pick and parents do not go together");
     a.at = start_of(at, B, c.device, a.at0);
     a.pos = per_sequence(pos, B, c.device, "pos must be a contiguous int32 tensor with one entry per sequence");
@@ -600,13 +609,7 @@ PyObject* tree_attn(PyObject*, PyObject* args) {
     a.lens = per_sequence(lens, B, c.device, bad_lens);
     need(a.lens != nullptr, bad_lens);
     a.pos = per_sequence(pos, B, c.device, "pos must be a contiguous int32 tensor with one entry per sequence");
-    const char* const bad_parents = "parents must be int32 [B, w] or [w] with a contiguous last dimension, on the queries' device";
-    if (is_tensor(parents, t, bad_parents) && t.dim() == 1) {
-      need(t.size(0) == w && t.scalar_type() == at::kInt && t.device() == c.device && (t.stride(0) == 1 || w == 1), bad_parents);
-      a.parents = static_cast<const int32_t*>(t.data_ptr());
-    } else {
-      a.parents = table_of(parents, B, w, c.device, a.parents_stride, bad_parents);
-    }
+    a.parents = parents_of(parents, B, w, c.device, a.parents_stride, "parents must be int32 [B, w] or [w] with a contiguous last dimension, on the queries' device");
     const long long room = c.c.capacity * a.n_table - w;             // entries that a sequence can have before its new tokens
     need(room >= 0, "the table has no room for the new tokens");
     need(max_len == ALL || (max_len >= 0 && max_len <= room), "max_len is negative or more than the table holds beside the new tokens");

@@ -166,3 +166,16 @@ def test_positions_before_the_first(fmt, d, w, Hq, first):
     for pos, pos0 in (([first, first + 3], 0), ([0, 3], first)):
         got = pc.tree_attn(q.cuda(), cache, table, _i32(lens), pos=_i32(pos), pos0=pos0, rope_theta=theta, want_lse=True)
         assert torch.equal(got["out"], want["out"]) and torch.equal(got["lse"], want["lse"])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_one_tree_for_all_sequences(fmt):
+    """page_append takes the parents that tree_attn takes: [w] for all sequences."""
+    B, w, parents = 3, 6, _i32([-1, 0, 0, 1, -2, 3])
+    k, v, table = _normal(70, B, w, 2, 64).cuda(), _normal(71, B, w, 2, 64).cuda(), _i32([[0, 1], [2, 3], [4, 5]])
+    pools = [pc.kv_cache(6, 2, 16, 64, fmt) for _ in range(2)]
+    for pool, p in zip(pools, (parents, parents.repeat(B, 1))):
+        pc.page_append(pool, k, v, table, at=_i32([0, 13, 20]), parents=p, rope_theta=1e4)
+    for name, x in pools[0].items():
+        if torch.is_tensor(x):
+            assert torch.equal(x.view(torch.uint8), pools[1][name].view(torch.uint8)) and x.view(torch.uint8).any()
