@@ -179,3 +179,110 @@ def test_one_tree_for_all_sequences(fmt):
     for name, x in pools[0].items():
         if torch.is_tensor(x):
             assert torch.equal(x.view(torch.uint8), pools[1][name].view(torch.uint8)) and x.view(torch.uint8).any()
+
+
+WIDE = [s[:4] for s in SHAPES if s[4] == "wide"]
+
+
+def _near(got, want, want_lse):
+    """weights rounded to bf16 or halves: 2 * 2^-9 of sum p |v| <= 4.5, the output half a step; lse: logits in fp32"""
+    there, lse = np.isfinite(want_lse), got["lse"].cpu().numpy().astype(np.float64)
+    assert np.array_equal(there, np.isfinite(lse)) and (lse[~there] == -INF).all()
+    assert (np.abs(ref.f64(got["out"]) - want) <= 1.8e-2 + 2.0 ** -8 * np.abs(want)).all()
+    assert (np.abs(np.where(there, lse, 0) - np.where(there, want_lse, 0)) <= 1e-4 + 1e-5 * np.abs(np.where(there, want_lse, 0))).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("theta,far", [(1e4, -40), (5e5, 100000), (1e6, 2 ** 28)])
+@pytest.mark.parametrize("B,w,Hq,most", WIDE)
+def test_many_rows_are_rotated(fmt, theta, far, B, w, Hq, most):
+    """Positions of depths in a tree, from given starts, before the first and far ones; queries out of a projection, tables and parents with a pitch."""
+    d, page, lens = 128, 32, [90 + 7 * b for b in range(B)]
+    cache, table = tree.pool(pc, 80, B, lens, w, 2, page, d, fmt)
+    g = np.random.default_rng(81)
+    parents = [[int(g.integers(max(-1, i - 4), i)) for i in range(w)] for _ in range(B)]
+    pos = [far + 5 * b for b in range(B)]
+    q = _normal(82, B, w, 3 * Hq, d)
+    depth = np.array([[len(p) - 1 for p in tree.seen(row)] for row in parents])
+    border = tree.near_a_border(ref.f64(q), np.array(pos)[:, None] + depth, theta)            # no element that fp32 may round either way
+    q[torch.from_numpy(np.concatenate([border, border], -1))] = 0
+    room, wide = _room(table, page, most + w), torch.full((B, w + 3), -9, dtype=torch.int32, device="cuda")
+    wide[:, 2:2 + w] = _i32(parents)
+    pitch = torch.full((B, room.shape[1] + 5), -3, dtype=torch.int32, device="cuda")
+    pitch[:, 1:1 + room.shape[1]] = room
+    got = pc.tree_attn(q.cuda()[:, :, Hq:2 * Hq], cache, pitch[:, 1:1 + room.shape[1]], _i32(lens), parents=wide[:, 2:2 + w], pos=_i32([5 * b for b in range(B)]), pos0=far,
+                       rope_theta=theta, max_len=most, softmax_scale=0.11, want_lse=True)
+    assert got["status"].item() == 0
+    want = tree.attention(ref.f64(q[:, :, Hq:2 * Hq]), tuple(np.nan_to_num(x) for x in tree.values(cache)), table.cpu().numpy(), lens, parents, pos, theta, 0.11)
+    _near(got, *want)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,w,Hq,most", WIDE)
+def test_many_rows_over_one_page_of_any_size(fmt, d, B, w, Hq, most):
+    """A page of an odd number of entries, one for each sequence, to its last entry."""
+    page = most + w + 3
+    lens = [page - w, 129, 300, 0, 1, 77, 500, 128][:B]
+    cache, table = tree.pool(pc, 83, B, lens, w, 2, page, d, fmt)
+    q, parents = _normal(84, B, w, Hq, d), [tree.chain(w)] * B
+    got = pc.tree_attn(q.cuda(), cache, table, _i32(lens), want_lse=True)
+    rows = [0, w // 2, w - 1]                                          # (the longest by a few rows: the reference goes row by row)
+    held = tuple(np.nan_to_num(x) for x in tree.values(cache))
+    for b in range(B):
+        which = rows if lens[b] > 1000 else list(range(w))
+        qs = np.zeros((1, w, Hq, d))
+        qs[0, which] = ref.f64(q[b])[which]
+        chain = [p if any(i <= r for r in which) else -2 for i, p in enumerate(parents[b])]
+        want, want_lse = tree.attention(qs, held, table[b:b + 1].cpu().numpy(), [lens[b]], [chain], [0], 0)
+        part = {"out": got["out"][b:b + 1, which], "lse": got["lse"][b:b + 1][:, :, which]}
+        _near(part, want[:, which], want_lse[:, :, which])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("B,w,Hq,most", WIDE)
+def test_many_rows_and_what_is_no_page_or_length(fmt, B, w, Hq, most):
+    """Reported, not followed, and nothing to the other sequences; zeros for a length that is none, entries of zeros for a page."""
+    lens, page = [40 + 10 * b for b in range(B)], 16
+    cache, table = tree.pool(pc, 85, B, lens, w, 2, page, 64, fmt)
+    q, others = _normal(86, B, w, Hq, 64).cuda(), [b for b in range(B) if b != 1]
+    call = lambda t, n: pc.tree_attn(q, cache, _room(t, page, most + w), _i32(n), max_len=most, want_lse=True)        # noqa: E731
+    good, held = call(table, lens), tuple(np.nan_to_num(x) for x in tree.values(cache))
+    for bad in (-1, -2 ** 31, cache["k"].shape[0], 2 ** 31 - 1):
+        other = table.clone()
+        other[1, 1] = bad
+        got = call(other, lens)
+        assert got["status"].item() == 421 and torch.equal(got["out"][others], good["out"][others]) and torch.equal(got["lse"][others], good["lse"][others])
+    none = tuple(np.concatenate([x, np.zeros_like(x[:1])]) for x in held)
+    ids = table.cpu().numpy().copy()
+    ids[1, 1] = len(held[0])
+    want, want_lse = tree.attention(ref.f64(q), none, ids, lens, [tree.chain(w)] * B, [0] * B, 0)
+    _near(got, want, want_lse)
+    for bad in (most + 1, 2 ** 31 - 1):
+        got = call(table, [bad if b == 1 else n for b, n in enumerate(lens)])
+        assert got["status"].item() == 422 and not got["out"][1].any() and (got["lse"][1] == -INF).all()
+        assert torch.equal(got["out"][others], good["out"][others]) and torch.equal(got["lse"][others], good["lse"][others])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("B,w,Hq,most", WIDE)
+def test_many_rows_again_on_any_stream_in_a_graph_with_kept_buffers(fmt, B, w, Hq, most):
+    lens, page = [300 + 90 * b for b in range(B)], 16
+    cache, table = tree.pool(pc, 87, B, lens, w, 2, page, 128, fmt)
+    table, q, n, kept = _room(table, page, most + w), _normal(88, B, w, Hq, 128).cuda(), _i32(lens), {}
+    call = lambda **kw: pc.tree_attn(q, cache, table, n, rope_theta=1e4, max_len=most, want_lse=True, **kw)            # noqa: E731
+    first, side = call(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        call(buffers=kept)
+        pc.tree_attn(q[:1, :1], cache, table[:1], n[:1], max_len=most, buffers=kept)
+        with torch.cuda.graph(graph, stream=side):
+            second = call(buffers=kept)
+        for _ in range(3):
+            second["out"].zero_()
+            graph.replay()
+            third = call()                                              # (another call's memory, beside the replays)
+    torch.cuda.synchronize()
+    for r in (second, third):
+        assert torch.equal(r["out"], first["out"]) and torch.equal(r["lse"], first["lse"]) and r["status"].item() == 0
