@@ -277,13 +277,13 @@ __device__ __forceinline__ uint32_t lap_of(uint32_t n) { return n / (V ? C::NV :
 // expects a stage's bytes over both CTAs on the leader's barrier of the ring's next stage; returns that barrier's address
 // for the copies and the stage's place; 0 once a wait has run out (no copy is issued into a ring that nobody drains)
 template <class C, bool V>
-__device__ __forceinline__ uint32_t ring_stage(const Ctx2& cx, Prod& p, bool leader, uint8_t** dst, uint32_t bytes = C::NCTA * C::STAGE_BYTES) {
+__device__ __forceinline__ uint32_t ring_stage(const Ctx2& cx, Prod& p, bool leader, uint8_t** dst) {
   Misc2& mi = *cx.mi;
   if (*cx.abort_flag) return 0;
   uint32_t& n = V ? p.v : p.k;
   const int s = stage_of<C, V>(n);
   if (!WAIT2(&mi.kv_free[s], free_par((lap_of<C, V>(n))), W2_KVFREE)) return 0;
-  if (leader) mbar_arrive_expect_tx(&mi.kv_full[s], bytes);
+  if (leader) mbar_arrive_expect_tx(&mi.kv_full[s], C::NCTA * C::STAGE_BYTES);
   *dst = cx.ring + s * C::STAGE_BYTES;
   ++n;
   return in_cta<C>(&mi.kv_full[s], 0);
