@@ -541,7 +541,8 @@ PC_API int32_t pc_page_append(const pc_page_append_args* args, void* stream);
  * lens[b] + w > page * n_table: as if there were no such sequence, and status_word gets the code 422.  max_len + w <= page * n_table; a max_len
  * near the longest plans the launch best.
  * What a mask hides, what stands behind a sequence's end and in pages that it does not name does not reach a row, whatever it holds, NaN included.
- * Precision as for pc_cache_attn.  q [B,w,Hq,d] through element strides; out [B,w,Hq,d] bf16, lse [B,Hq,w] fp32 (natural log; may be NULL) contiguous.
+ * Logits, maxima, sums and accumulators are fp32; probabilities are rounded to bf16, over codes, which are exact operands, to half precision.
+ * q [B,w,Hq,d] through element strides; out [B,w,Hq,d] bf16, lse [B,Hq,w] fp32 (natural log; may be NULL) contiguous.
  * Scaled logits stay below 2^30 in size.  The scales of 8-bit formats may not be negative (pc_page_append and pc_kv_quantize leave none that are).  out
  * and lse may not overlap what is read.
  * d, Hkv: the pool's; any Hq / Hkv, Hq <= 2^18, B * w * Hq <= 2^24.  Workspace: pc_tree_attn_workspace_bytes(args), aligned to 32 bytes; it reads

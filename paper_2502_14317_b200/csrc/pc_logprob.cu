@@ -17,7 +17,7 @@
 // A row is the work of a cluster of 1 to 8 CTAs (rule at the launch).
 //
 // Bound, many rows, by the exponentials and the issue of instructions beside the reading: at 1024 x 128256 in bf16 with 8 alternatives (263 MB) the exponentials' unit
-// is busy for 65 %, issue 70, memory 63: 54 us = 4.9 TB/s; without alternatives 6 us less, with 32 of them 11 more.  276 rows of 50001 in fp16 whose pitch is odd
+// is busy for 65 %, issue 70, memory 63: 53 to 59 us by the board = 5.0 to 4.5 TB/s; without alternatives 6 us less, with 32 of them 11 more.  276 rows of 50001 in fp16 whose pitch is odd
 // 12 us; one row of 128256 in fp32 with 20 alternatives 8.5, a chain of latencies.
 #include "pc_kernels.h"
 #include "pc_logprob.h"

@@ -5,7 +5,7 @@
 // entries 25.5 us with pages of 16, 20.9 with pages of 64 (cp.async of 16 bytes in place of the boxes 30.2).  The last w entries of a sequence are its new tokens;
 // a unit that holds any is masked by the rows' words of ancestors, which every CTA makes itself from the parents (some 400 cycles, under the first copies).
 //
-// Bound by reading the pages, with few sequences by latencies: 64 sequences of 7700 to 16384 int8 entries (1.1 GB), 32/8 heads of 128, 214 to 230 us = 5.1 to 4.8 TB/s (the
+// Bound by reading the pages, with few sequences by latencies: 64 sequences of up to 16384 int8 entries, 8145 on average (1.1 GB), 32/8 heads of 128, 214 to 230 us = 5.1 to 4.8 TB/s (the
 // copies' conversions and an end in which only the longest sequences are left); one sequence of 16400 bf16 entries (67 MB) 20 us: some 8 for the start, rows
 // and join, then a tile at a time.
 #include "pc_few.cuh"
